@@ -1,5 +1,5 @@
 """Performance cases of the feed-forward network in 8-bit floating point: the
-operators of paper_2510_11331_amd.ffn8, called as a serving program calls them.
+operators of paper_2510_11331_amd.ffn_q, called as a serving program calls them.
 
 A case is a dict of plain values with a "kind":
 
@@ -207,18 +207,18 @@ def run(s):
     case = s["case"]
     kind = case["kind"]
     if own:
-        from paper_2510_11331_amd import ffn8
+        from paper_2510_11331_amd import ffn_q
         if kind == "pack":
-            w8 = ffn8.pack_linear8(s["w"])
-            return {"codes": w8.codes, "exps": w8.exps}
+            wq = ffn_q.pack_linear_q(s["w"])
+            return {"codes": wq.codes, "exps": wq.exps}
         if kind == "norm":
-            x, q, exps = ffn8.add_rmsnorm8(s["x"], s["gain"], EPS, add=s["add"])
+            x, q, exps = ffn_q.add_rmsnorm_q(s["x"], s["gain"], EPS, add=s["add"])
             return {"x": x, "q": q, "exps": exps}
         if kind == "linear":
-            w8 = ffn8.Linear8(s["packed"], case["n"], case["k"])
-            return {"out": ffn8.linear8(s["q"], s["exps"], w8, add=s["add"], dtype=_type(case))}
-        w8 = ffn8.Linear8(s["packed"], 2 * case["f"], case["k"])
-        q, exps = ffn8.gate_up8(s["q"], s["exps"], w8)
+            wq = ffn_q.LinearQ(s["packed"], case["n"], case["k"])
+            return {"out": ffn_q.linear_q(s["q"], s["exps"], wq, add=s["add"], dtype=_type(case))}
+        wq = ffn_q.LinearQ(s["packed"], 2 * case["f"], case["k"])
+        q, exps = ffn_q.gate_up_q(s["q"], s["exps"], wq)
         return {"q": q, "exps": exps}
     if kind == "pack":
         codes, exps = _pack(*_quantise_weight(s["w"]))
