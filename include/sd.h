@@ -300,6 +300,62 @@ int sd_force_draft(sd_ctx *ctx, int B, const int32_t *slots, int gamma, int i,
                    const int32_t *cont, int cont_len, const uint32_t *u, double alpha,
                    int32_t *draft_tok, void *stream);
 
+/* ---- The feed-forward network in 8-bit floating point (eq. f31 with 8-bit
+ * operands).  Context-free like sd_accept_resample: every call only enqueues
+ * on the stream of the current device, keeps no state, and is safe to capture
+ * and to call from several streams at once (with buffers of their own).
+ *
+ * Format.  Numbers are e4m3 codes (one sign, four exponent, three fraction
+ * bits; largest 448) with a power-of-two scale 2^(E - 127), E a byte, per
+ * block.  E is the smallest E >= 1 with amax <= 448 2^(E - 127), amax the
+ * largest magnitude of the block's finite entries; a code is the value times
+ * 2^(127 - E) rounded to nearest even.  NaN and infinities become the code of
+ * NaN (which makes NaN of every sum it enters).
+ *   Rows (activations)  [M, K]: codes uint8 [M, K8], K8 = K rounded up to a
+ *     multiple of 128, entries past K zero; exponents uint8 [M, Ke], one per
+ *     128 entries, Ke = K8 / 128 rounded up to a multiple of 4, padding 0.
+ *     Codes start on 16 bytes.  A buffer written here can be read as it is.
+ *   Weights [N, K] (y = x W^T), one scale per 128 x 128 block, packed by
+ *     sd_pack_linear_q: 2 KB tiles of 16 rows x 128 columns, row tiles major;
+ *     inside a tile 16-byte unit 64 h + 16 g + r holds row r, columns 64 h +
+ *     16 g .. + 15 (zeros past N and K); then exponents [ceil(N / 128), Ke].
+ * Sizes: 1 <= N <= 2^22, 1 <= K <= 2^18, 0 <= M <= 2^22 (M = 0 enqueues
+ * nothing and reads no pointer). */
+
+/* Bytes of a packed [N, K] matrix (0 on an invalid size). */
+size_t sd_linear_q_bytes(int N, int K);
+
+/* Quantise and pack a row-major [N, K] matrix of dtype (SD_DTYPE_*) into dst
+ * (sd_linear_q_bytes(N, K) bytes, 16-byte aligned).  Once per weight. */
+int sd_pack_linear_q(const void *src, void *dst, int N, int K, int dtype, void *stream);
+
+/* Residual addition and RMSNorm with an 8-bit output: s = x + add_0 + .. +
+ * add_(n_add - 1), y = s / sqrt(mean(s^2) + eps) * gain, written as rows of d
+ * entries (q, exps).  x [M, d] and add [n_add, M, d] (0 <= n_add <= 6) are of
+ * dtype; with n_add > 0, s is written to x_out [M, d] in that type and the norm
+ * is of the value written; x_out may be x (else it must not overlap an
+ * input).  gain [d] is of gain_dtype.  Sums and the norm are taken in 64 bits, y is rounded to fp32 and
+ * then to its code.  d <= 16384, eps > 0. */
+int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const void *add, void *x_out,
+                    const void *gain, int gain_dtype, float eps, uint8_t *q, uint8_t *exps, void *stream);
+
+/* out = [add +] rows W^T: rows (q, exps) [M, K], w a packed [N, K].  out
+ * [M, N] of dtype with row stride ldo >= N (entries); add NULL or fp32 with
+ * the same stride; with dtype fp32 it may be out itself (else no overlap). */
+int sd_linear_q(int M, int N, int K, const uint8_t *q, const uint8_t *exps, const void *w, const float *add,
+               void *out, int ldo, int dtype, void *stream);
+
+/* SwiGLU of the gate/up product with an 8-bit output: w is the packed [2 F, K]
+ * with gate and up rows interleaved in blocks of 16 (see wgu of sd_weights), h
+ * = silu(gate) * up is written as rows of F entries (q_out, exps_out), the
+ * input of a down projection with K = F.  F a multiple of 16, at most 2^18.
+ * The workspace (16-byte aligned, sd_gate_up_q_workspace_bytes(M, F)) is scratch
+ * of this call alone until its work is done: calls that may overlap, graphs
+ * among them, need one each. */
+size_t sd_gate_up_q_workspace_bytes(int M, int F);
+int sd_gate_up_q(int M, int F, int K, const uint8_t *q, const uint8_t *exps, const void *w, uint8_t *q_out,
+                uint8_t *exps_out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Copy slot state to out [B, 4] int32 (device): committed target length
  * P, next input token x0, pending draft input (-1 if none), KV capacity. */
 int sd_slot_state(sd_ctx *ctx, int B, const int32_t *slots, int32_t *out,

@@ -7,3 +7,4 @@ device memory and streams through PyTorch.
 from ._lib import SDError, lib  # noqa: F401
 from .engine import (SDEngine, Batch, GPUModel, StepGraph, generate, generate_graph,  # noqa: F401
                      emitted_tokens, accept_resample, resume_prompts)
+from .ffn_q import LinearQ, add_rmsnorm_q, gate_up_q, linear_q, pack_linear_q  # noqa: F401

@@ -20,7 +20,8 @@ SD_DTYPE_BF16, SD_DTYPE_F32 = 0, 1
 EXPORTS = ("sd_kv_pool_bytes", "sd_workspace_bytes", "sd_plan_projection", "sd_init", "sd_init_static", "sd_prefill", "sd_release",
            "sd_draft_step", "sd_verify", "sd_accept_resample", "sd_kv_commit", "sd_force_draft", "sd_slot_state",
            "sd_check", "sd_profile", "sd_profile_read", "sd_destroy", "sd_strerror", "sd_last_error",
-           "sd_pack_linear", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
+           "sd_pack_linear", "sd_linear_q_bytes", "sd_pack_linear_q", "sd_add_rmsnorm_q", "sd_linear_q",
+           "sd_gate_up_q_workspace_bytes", "sd_gate_up_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
 
 
 class ModelCfg(C.Structure):
@@ -114,6 +115,12 @@ def lib():
         "sd_strerror": (C.c_char_p, [I]),
         "sd_last_error": (C.c_char_p, []),
         "sd_pack_linear": (I, [P, P, I, I, I, P]),
+        "sd_linear_q_bytes": (C.c_size_t, [I, I]),
+        "sd_pack_linear_q": (I, [P, P, I, I, I, P]),
+        "sd_add_rmsnorm_q": (I, [I, I, I, P, I, P, P, P, I, F, P, P, P]),
+        "sd_linear_q": (I, [I, I, I, P, P, P, P, P, I, I, P]),
+        "sd_gate_up_q_workspace_bytes": (C.c_size_t, [I, I]),
+        "sd_gate_up_q": (I, [I, I, I, P, P, P, P, P, P, C.c_size_t, P]),
         "sd_sched_latency": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32), I,
                                  C.POINTER(C.c_double)]),
         "sd_sched_batching": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32),

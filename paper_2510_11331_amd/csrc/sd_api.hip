@@ -1193,6 +1193,82 @@ int sd_pack_linear(const void* src, void* dst, int N, int K, int dtype, void* st
   return SD_OK;
 }
 
+size_t sd_linear_q_bytes(int N, int K) {
+  if (N < 1 || N > LINEAR8_MAX_MN || K < 1 || K > LINEAR8_MAX_K) return 0;
+  return (size_t)((N + 15) / 16) * blocks8(K) * 2048 + (size_t)((N + 127) / 128) * ke8(K);
+}
+
+int sd_pack_linear_q(const void* src, void* dst, int N, int K, int dtype, void* stream) {
+  if (!src || !dst || !sd_linear_q_bytes(N, K) || (dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32)) return SD_EINVAL;
+  if ((uintptr_t)src % esize(dtype) || (uintptr_t)dst % 16) return SD_EINVAL;
+  HIPCHK(launch_pack_linear8(dtype == SD_DTYPE_F32 ? 1 : 0, src, dst, N, K, (hipStream_t)stream));
+  return SD_OK;
+}
+
+int sd_add_rmsnorm_q(int M, int d, int dtype, const void* x, int n_add, const void* add, void* x_out, const void* gain,
+                    int gain_dtype, float eps, uint8_t* q, uint8_t* exps, void* stream) {
+  if (M < 0 || M > LINEAR8_MAX_MN || d < 1 || d > NORM8_MAX_D || n_add < 0 || n_add > NORM8_MAX_ADD || !(eps > 0.f))
+    return SD_EINVAL;
+  if ((dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32) || (gain_dtype != SD_DTYPE_BF16 && gain_dtype != SD_DTYPE_F32))
+    return SD_EINVAL;
+  if (M == 0) return SD_OK;
+  if (!x || !gain || !q || !exps || (n_add && (!add || !x_out))) return SD_EINVAL;
+  if ((uintptr_t)x % esize(dtype) || (uintptr_t)gain % esize(gain_dtype) || (uintptr_t)q % 16) return SD_EINVAL;
+  if (n_add && ((uintptr_t)add | (uintptr_t)x_out) % esize(dtype)) return SD_EINVAL;
+  Norm8Params np{x, add, gain, x_out, q, exps, M, d, n_add, eps};
+  HIPCHK(launch_add_rmsnorm8(dtype == SD_DTYPE_F32 ? 1 : 0, gain_dtype == SD_DTYPE_F32 ? 1 : 0, np, (hipStream_t)stream));
+  return SD_OK;
+}
+
+int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add, void* out,
+               int ldo, int dtype, void* stream) {
+  if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K) || ldo < N || (dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32))
+    return SD_EINVAL;
+  if (M == 0) return SD_OK;
+  if (!q || !exps || !w || !out || ((uintptr_t)q | (uintptr_t)w) % 16) return SD_EINVAL;
+  if ((uintptr_t)add % 4 || (uintptr_t)out % esize(dtype)) return SD_EINVAL;
+  Gemm8Params gp{};
+  gp.q = q;
+  gp.exps = exps;
+  gp.w = (const uint8_t*)w;
+  gp.wexps = gp.w + (size_t)((N + 15) / 16) * blocks8(K) * 2048;
+  gp.M = M;
+  gp.N = N;
+  gp.K = K;
+  gp.add = add;
+  gp.out = out;
+  gp.ldo = ldo;
+  gp.bf16 = dtype == SD_DTYPE_BF16;
+  HIPCHK(launch_gemm8(EPI8_STORE, gp, (hipStream_t)stream));
+  return SD_OK;
+}
+
+size_t sd_gate_up_q_workspace_bytes(int M, int F) {
+  if (M < 0 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_MN / 2) return 0;
+  return std::max<size_t>(256, (size_t)M * F * sizeof(float));
+}
+
+int sd_gate_up_q(int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
+                uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
+  const size_t need = sd_gate_up_q_workspace_bytes(M, F);
+  if (!need || !sd_linear_q_bytes(2 * F, K) || F > LINEAR8_MAX_K) return SD_EINVAL;
+  if (M == 0) return SD_OK;
+  if (!q || !exps || !w || !q_out || !exps_out || !workspace || workspace_bytes < need) return SD_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)w | (uintptr_t)q_out | (uintptr_t)workspace) % 16) return SD_EINVAL;
+  Gemm8Params gp{};
+  gp.q = q;
+  gp.exps = exps;
+  gp.w = (const uint8_t*)w;
+  gp.wexps = gp.w + (size_t)(2 * F / 16) * blocks8(K) * 2048;
+  gp.M = M;
+  gp.N = 2 * F;
+  gp.K = K;
+  gp.out = workspace;
+  HIPCHK(launch_gemm8(EPI8_SWIGLU, gp, (hipStream_t)stream));
+  HIPCHK(launch_quantise_rows8((const float*)workspace, q_out, exps_out, M, F, (hipStream_t)stream));
+  return SD_OK;
+}
+
 const char* sd_last_error(void) { return g_last_error; }
 
 const char* sd_strerror(int code) {

@@ -245,6 +245,45 @@ struct ForceParams {
 // out[(y * M + m) * ldo + n], the residual add happens in the next RMSNorm
 enum GemmEpi { EPI_STORE = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_QKV = 3, EPI_PART = 4 };
 
+// ---------------------------------------------------------------- 8-bit feed-forward
+
+// Operands in 8 bits (format: rows8.hip).  Activations: codes [M, K8] with K8 =
+// K rounded up to 128 (zero codes past K), exponents [M, ke8(K)].  Weights:
+// 2 KB tiles of 16 rows x 128 columns (tile of rows 16 t .., column block b at
+// (t blocks + b) 2048; inside it 16-byte unit 64 h + 16 g + r holds row r,
+// columns 64 h + 16 g .. + 16), then exponents [rows / 128, ke8(K)].
+__host__ __device__ __forceinline__ int blocks8(int K) { return (K + 127) / 128; }
+__host__ __device__ __forceinline__ int ke8(int K) { return (blocks8(K) + 3) & ~3; }
+
+constexpr int NORM8_MAX_ADD = 6;       // addends of a norm: the K ranges of a residual projection
+constexpr int NORM8_MAX_D = 16384;     // row kept in registers
+constexpr int LINEAR8_MAX_K = 1 << 18;   // 32-bit offsets inside 256 rows
+constexpr int LINEAR8_MAX_MN = 1 << 22;
+
+struct Norm8Params {
+  const void* x;       // [M, d]
+  const void* add;     // [n_add, M, d] in x's type
+  const void* gain;    // [d]
+  void* x_out;         // [M, d] in x's type, written if n_add > 0 (may be x)
+  uint8_t* q;          // [M, 128 blocks8(d)]
+  uint8_t* exps;       // [M, ke8(d)]
+  int M, d, n_add;
+  float eps;
+};
+
+struct Gemm8Params {
+  const uint8_t* q;      // activations [M, K]
+  const uint8_t* exps;
+  const uint8_t* w;      // packed weight [N, K]
+  const uint8_t* wexps;  // its exponents
+  int M, N, K;
+  const float* add;      // STORE: null, or [M, ldo] added to the product
+  void* out;             // STORE: [M, ldo] fp32 or bf16; SWIGLU: h [M, N / 2] fp32
+  int ldo;
+  int bf16;              // STORE: out is bf16
+};
+enum Gemm8Epi { EPI8_STORE = 0, EPI8_SWIGLU = 1 };
+
 // ---------------------------------------------------------------- launchers
 // dtype: 0 bf16, 1 fp32 (same values as SD_DTYPE_*)
 
@@ -289,6 +328,10 @@ hipError_t launch_accept(const AcceptParams& p, hipStream_t s);
 hipError_t launch_commit(const CommitParams& p, hipStream_t s);
 hipError_t launch_force_draft(const ForceParams& p, hipStream_t s);
 hipError_t launch_fill_i32(int32_t* p, int32_t v, size_t n, hipStream_t s);
+hipError_t launch_add_rmsnorm8(int x_dtype, int gain_dtype, const Norm8Params& p, hipStream_t s);
+hipError_t launch_quantise_rows8(const float* h, uint8_t* q, uint8_t* exps, int M, int F, hipStream_t s);
+hipError_t launch_pack_linear8(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
+hipError_t launch_gemm8(int epi, const Gemm8Params& p, hipStream_t s);
 hipError_t launch_pack_linear(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 
 // GEMM geometry (shared by host planning and the kernel)
