@@ -79,7 +79,7 @@ enum {
     SD_EHIP = -4      /* a HIP runtime call failed                      */
 };
 
-enum { SD_DTYPE_BF16 = 0, SD_DTYPE_F32 = 1 };
+enum { SD_DTYPE_BF16 = 0, SD_DTYPE_F32 = 1, SD_DTYPE_BF16_FFN_Q = 2 };
 
 /* Decoder-only model (LLaMA layout of the paper's decoder block, eqs. f11,
  * f21, f31): RMSNorm -> QKV -> rotary embedding -> causal attention over the
@@ -93,10 +93,15 @@ enum { SD_DTYPE_BF16 = 0, SD_DTYPE_F32 = 1 };
  * rounded to fp16 and the KV cache holds fp16; embedding rows and norm gains
  * are read as bf16; the residual stream, norms, rotary embedding and softmax
  * are fp32.  fp16 has the memory cost and matrix-instruction rate of bf16
- * and three more significant bits. */
+ * and three more significant bits.  SD_DTYPE_BF16_FFN_Q (a model's dtype
+ * only): as SD_DTYPE_BF16, but the feed-forward network runs in 8-bit floating
+ * point (sd_add_rmsnorm_q, sd_gate_up_q, sd_linear_q below): wgu and wdown are
+ * packed by sd_pack_linear_q, and the inputs of both products are rounded to
+ * 8-bit rows.  Half the weight bytes of two thirds of the layer; each code is
+ * within 2^-4 of its value. */
 typedef struct {
     int n_layers, d_model, n_heads, n_kv_heads, head_dim, d_ffn, vocab;
-    int dtype;              /* SD_DTYPE_BF16 or SD_DTYPE_F32                */
+    int dtype;              /* SD_DTYPE_*                                   */
     float rope_theta;       /* rotary base, e.g. 10000                      */
     float rms_eps;          /* RMSNorm epsilon, e.g. 1e-5                   */
 } sd_model_cfg;
@@ -167,7 +172,8 @@ size_t sd_workspace_bytes(const sd_config *cfg);
  * the LM head: B (gamma + 1) when verifying, B when drafting).  SD_PROJ_KV is
  * the QKV projection of a prefill pass's last layer, which has no query
  * columns.  SD_EINVAL: invalid configuration, more rows than the pass's
- * workspace holds, SD_PROJ_KV outside prefill, SD_PROJ_LM_HEAD in it. */
+ * workspace holds, SD_PROJ_KV outside prefill, SD_PROJ_LM_HEAD in it,
+ * SD_PROJ_GATEUP and SD_PROJ_DOWN of an SD_DTYPE_BF16_FFN_Q model. */
 enum { SD_PASS_VERIFY = 0, SD_PASS_DRAFT = 1, SD_PASS_PREFILL = 2, SD_PASS_PREFILL_DRAFT = 3 };
 enum { SD_PROJ_QKV = 0, SD_PROJ_KV = 1, SD_PROJ_O = 2, SD_PROJ_GATEUP = 3, SD_PROJ_DOWN = 4, SD_PROJ_LM_HEAD = 5 };
 typedef struct sd_proj_plan {
@@ -314,7 +320,7 @@ int sd_force_draft(sd_ctx *ctx, int B, const int32_t *slots, int gamma, int i,
  *   Rows (activations)  [M, K]: codes uint8 [M, K8], K8 = K rounded up to a
  *     multiple of 128, entries past K zero; exponents uint8 [M, Ke], one per
  *     128 entries, Ke = K8 / 128 rounded up to a multiple of 4, padding 0.
- *     Codes start on 16 bytes.  A buffer written here can be read as it is.
+ *     Codes start on 16 bytes, exponents on 4.  A buffer written here can be read as it is.
  *   Weights [N, K] (y = x W^T), one scale per 128 x 128 block, packed by
  *     sd_pack_linear_q: 2 KB tiles of 16 rows x 128 columns, row tiles major;
  *     inside a tile 16-byte unit 64 h + 16 g + r holds row r, columns 64 h +
@@ -341,18 +347,20 @@ int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const vo
 
 /* out = [add +] rows W^T: rows (q, exps) [M, K], w a packed [N, K].  out
  * [M, N] of dtype with row stride ldo >= N (entries); add NULL or fp32 with
- * the same stride; with dtype fp32 it may be out itself (else no overlap). */
+ * the same stride; with dtype fp32 it may be out itself (else no overlap).
+ * The workspace (16-byte aligned, sd_linear_q_workspace_bytes(M, N, K)) is
+ * scratch of this call alone until its work is done: calls that may overlap,
+ * graphs among them, need one each. */
+size_t sd_linear_q_workspace_bytes(int M, int N, int K);
 int sd_linear_q(int M, int N, int K, const uint8_t *q, const uint8_t *exps, const void *w, const float *add,
-               void *out, int ldo, int dtype, void *stream);
+                void *out, int ldo, int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* SwiGLU of the gate/up product with an 8-bit output: w is the packed [2 F, K]
  * with gate and up rows interleaved in blocks of 16 (see wgu of sd_weights), h
  * = silu(gate) * up is written as rows of F entries (q_out, exps_out), the
  * input of a down projection with K = F.  F a multiple of 16, at most 2^18.
- * The workspace (16-byte aligned, sd_gate_up_q_workspace_bytes(M, F)) is scratch
- * of this call alone until its work is done: calls that may overlap, graphs
- * among them, need one each. */
-size_t sd_gate_up_q_workspace_bytes(int M, int F);
+ * Workspace as for sd_linear_q, of sd_gate_up_q_workspace_bytes(M, F, K). */
+size_t sd_gate_up_q_workspace_bytes(int M, int F, int K);
 int sd_gate_up_q(int M, int F, int K, const uint8_t *q, const uint8_t *exps, const void *w, uint8_t *q_out,
                 uint8_t *exps_out, void *workspace, size_t workspace_bytes, void *stream);
 
@@ -368,7 +376,8 @@ int sd_check(sd_ctx *ctx, void *stream, int32_t *flags_out);
 /* Timing with HIP events (off by default).  kind: SD_PROF_* below.  The
  * GEMM and attention kinds time each kernel with start/stop events that its
  * own dispatch timestamps (kernel begin to end, the interval a profiler
- * reports); the VERIFY and DRAFT kinds time the whole call with events
+ * reports), the 8-bit products of an SD_DTYPE_BF16_FFN_Q model each with events
+ * around it; the VERIFY and DRAFT kinds time the whole call with events
  * recorded on its stream.  bytes: algorithmic HBM bytes of the timed GEMMs
  * (weights + activations read + outputs written).  sd_profile_read
  * synchronises the recorded events and returns the number of timed

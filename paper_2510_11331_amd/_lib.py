@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsd.so")
 
 SD_OK, SD_EINVAL, SD_ENOMEM, SD_ESTATE, SD_EHIP = 0, -1, -2, -3, -4
-SD_DTYPE_BF16, SD_DTYPE_F32 = 0, 1
+SD_DTYPE_BF16, SD_DTYPE_F32, SD_DTYPE_BF16_FFN_Q = 0, 1, 2
 (SD_PROF_GEMM_VERIFY_GATEUP, SD_PROF_GEMM_VERIFY_ALL, SD_PROF_ATTN_VERIFY,
  SD_PROF_VERIFY, SD_PROF_DRAFT) = range(5)
 
@@ -20,7 +20,7 @@ SD_DTYPE_BF16, SD_DTYPE_F32 = 0, 1
 EXPORTS = ("sd_kv_pool_bytes", "sd_workspace_bytes", "sd_plan_projection", "sd_init", "sd_init_static", "sd_prefill", "sd_release",
            "sd_draft_step", "sd_verify", "sd_accept_resample", "sd_kv_commit", "sd_force_draft", "sd_slot_state",
            "sd_check", "sd_profile", "sd_profile_read", "sd_destroy", "sd_strerror", "sd_last_error",
-           "sd_pack_linear", "sd_linear_q_bytes", "sd_pack_linear_q", "sd_add_rmsnorm_q", "sd_linear_q",
+           "sd_pack_linear", "sd_linear_q_bytes", "sd_linear_q_workspace_bytes", "sd_pack_linear_q", "sd_add_rmsnorm_q", "sd_linear_q",
            "sd_gate_up_q_workspace_bytes", "sd_gate_up_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
 
 
@@ -118,8 +118,9 @@ def lib():
         "sd_linear_q_bytes": (C.c_size_t, [I, I]),
         "sd_pack_linear_q": (I, [P, P, I, I, I, P]),
         "sd_add_rmsnorm_q": (I, [I, I, I, P, I, P, P, P, I, F, P, P, P]),
-        "sd_linear_q": (I, [I, I, I, P, P, P, P, P, I, I, P]),
-        "sd_gate_up_q_workspace_bytes": (C.c_size_t, [I, I]),
+        "sd_linear_q_workspace_bytes": (C.c_size_t, [I, I, I]),
+        "sd_linear_q": (I, [I, I, I, P, P, P, P, P, I, I, P, C.c_size_t, P]),
+        "sd_gate_up_q_workspace_bytes": (C.c_size_t, [I, I, I]),
         "sd_gate_up_q": (I, [I, I, I, P, P, P, P, P, P, C.c_size_t, P]),
         "sd_sched_latency": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32), I,
                                  C.POINTER(C.c_double)]),

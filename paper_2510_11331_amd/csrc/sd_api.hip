@@ -35,6 +35,7 @@ struct ModelRT {
   int n_blocks = 0;
   float2* rope_tab = nullptr;   // [rope_pos, head_dim/2] rotary (cos, sin), in the workspace
   int rope_pos = 0;
+  bool ffn_q = false;       // feed-forward products in 8 bits (SD_DTYPE_BF16_FFN_Q; c.dtype is then SD_DTYPE_BF16)
   size_t layer_bytes = 0;   // bytes of one layer's pool
   int nqkv() const { return (c.n_heads + 2 * c.n_kv_heads) * c.head_dim; }
   int nq() const { return c.n_heads * c.head_dim; }
@@ -48,6 +49,9 @@ struct Lane {
   int rb_cap = 0;
   float *x = nullptr, *q = nullptr, *logits = nullptr;
   void *xn = nullptr, *att = nullptr, *hmid = nullptr;
+  // 8-bit feed-forward: codes and exponents of the normed and the SwiGLU rows, and fp32 scratch of short passes
+  uint8_t *q8 = nullptr, *e8 = nullptr, *qh8 = nullptr, *eh8 = nullptr;
+  float* h8 = nullptr;
   float* part = nullptr;        // [MAX_KSPLIT, part_rows, d] K-split partial sums
   int part_rows = 0;
   float *attn_o = nullptr, *attn_ml = nullptr;
@@ -117,7 +121,7 @@ size_t esize(int dtype) { return dtype == SD_DTYPE_F32 ? 4 : 2; }
 bool model_ok(const sd_model_cfg& m) {
   if (m.n_layers < 1 || m.d_model < 1 || m.n_heads < 1 || m.n_kv_heads < 1 || m.d_ffn < 1 || m.vocab < 1)
     return false;
-  if (m.dtype != SD_DTYPE_BF16 && m.dtype != SD_DTYPE_F32) return false;
+  if (m.dtype != SD_DTYPE_BF16 && m.dtype != SD_DTYPE_F32 && m.dtype != SD_DTYPE_BF16_FFN_Q) return false;
   if (m.head_dim != 64 && m.head_dim != 128) return false;
   if (m.n_heads * m.head_dim != m.d_model) return false;
   if (m.n_heads % m.n_kv_heads) return false;
@@ -170,6 +174,7 @@ struct Alloc {
 struct Dims {
   int d = 0, nqkv = 0, nq = 0, F = 0, V = 0, KV = 0, hd = 0, G = 1;
   size_t esz = 2;
+  bool ffn_q = false;
 };
 
 Dims dims_max(const sd_model_cfg& a, const sd_model_cfg* b) {
@@ -184,6 +189,7 @@ Dims dims_max(const sd_model_cfg& a, const sd_model_cfg* b) {
     r.hd = std::max(r.hd, m.head_dim);
     r.G = std::max(r.G, m.n_heads / m.n_kv_heads);
     r.esz = std::max(r.esz, esize(m.dtype));
+    r.ffn_q = r.ffn_q || m.dtype == SD_DTYPE_BF16_FFN_Q;
   };
   upd(a);
   if (b) upd(*b);
@@ -207,6 +213,13 @@ void lay_lane(Alloc& al, Lane& ln, int rows, const Dims& D, int decode_rb, int q
   ln.q = al.take<float>(sizeof(float) * rows * D.nq);
   ln.att = al.take<void>(D.esz * rows * D.nq);
   ln.hmid = al.take<void>(D.esz * rows * D.F);
+  if (D.ffn_q) {
+    ln.q8 = al.take<uint8_t>((size_t)rows * 128 * blocks8(D.d));
+    ln.e8 = al.take<uint8_t>((size_t)rows * ke8(D.d));
+    ln.qh8 = al.take<uint8_t>((size_t)rows * 128 * blocks8(D.F));
+    ln.eh8 = al.take<uint8_t>((size_t)rows * ke8(D.F));
+    ln.h8 = al.take<float>(sizeof(float) * std::min(rows, 64) * D.F);
+  }
   ln.part_rows = std::min(rows, 640);   // K splits of longer passes: as many as fit
   ln.part = al.take<float>(sizeof(float) * MAX_KSPLIT * ln.part_rows * D.d);
   ln.logits = logits_rows ? al.take<float>(sizeof(float) * logits_rows * D.V) : nullptr;
@@ -222,7 +235,7 @@ void lay_lane(Alloc& al, Lane& ln, int rows, const Dims& D, int decode_rb, int q
 // workgroup and (fp32) the default 64 KB of dynamic LDS
 int prefill_qb(const sd_model_cfg& m) {
   const int G = m.n_heads / m.n_kv_heads;
-  if (m.dtype == SD_DTYPE_BF16) return std::max(1, ATTN_PREFILL_Q / G);
+  if (m.dtype != SD_DTYPE_F32) return std::max(1, ATTN_PREFILL_Q / G);
   int qb = std::max(1, ATTN_QMAX / G);
   while (qb > 1 && attention_lds_bytes(m.head_dim, esize(m.dtype), qb * G) > 64 * 1024) --qb;
   return qb;
@@ -490,6 +503,52 @@ int gemm(sd_ctx* ctx, const ModelRT& m, int epi, const void* A, const void* W, i
   return SD_OK;
 }
 
+// The feed-forward of one layer in 8 bits: the norm (which adds the O
+// projection's ns partial sums), gate/up with SwiGLU, and the down projection,
+// whose K ranges' partial sums are left in ln.part for the next RMSNorm (*nsplit
+// of them) or which is added to the residual stream (0).  The sums feed a
+// residual stream that 8-bit operands already put some 2 % off, so row tiles run
+// on the 8-bit matrix instruction.
+int ffn_q(sd_ctx* ctx, const ModelRT& m, Lane& ln, int l, int M, int ns, bool verify, hipStream_t s, int* nsplit) {
+  const int d = m.c.d_model, F = m.c.d_ffn;
+  Norm8Params np{ln.x, ln.part, m.ffn_norm[l], ln.x, ln.q8, ln.e8, M, d, ns, m.c.rms_eps};
+  HIPCHK(launch_add_rmsnorm8(1, 0, np, s));
+  Gemm8Params g{};
+  g.q = ln.q8;
+  g.exps = ln.e8;
+  g.w = (const uint8_t*)m.wgu[l];
+  g.wexps = g.w + codes8_bytes(2 * F, d);
+  g.M = M;
+  g.N = 2 * F;
+  g.K = d;
+  g.q_out = ln.qh8;
+  g.exps_out = ln.eh8;
+  ProfRec r;
+  prof_begin(ctx, s, r, verify ? SD_PROF_GEMM_VERIFY_ALL : -1, verify ? SD_PROF_GEMM_VERIFY_GATEUP : -1,
+             (double)sd_linear_q_bytes(2 * F, d) + (double)M * (d + F), false);
+  HIPCHK(launch_gate_up8(g, ln.h8, s));
+  prof_end(ctx, s, r);
+  g = Gemm8Params{};
+  g.q = ln.qh8;
+  g.exps = ln.eh8;
+  g.w = (const uint8_t*)m.wdown[l];
+  g.wexps = g.w + codes8_bytes(d, F);
+  g.M = M;
+  g.N = d;
+  g.K = F;
+  g.add = ln.x;
+  g.out = ln.x;
+  g.ldo = d;
+  g.part = ln.part;
+  const Gemm8Plan plan = plan_gemm8(M, d, F, false, (size_t)MAX_KSPLIT * ln.part_rows * d);
+  prof_begin(ctx, s, r, verify ? SD_PROF_GEMM_VERIFY_ALL : -1, -1,
+             (double)sd_linear_q_bytes(d, F) + (double)M * F + (double)M * d * 4 * std::max(2, plan.ksplit), false);
+  HIPCHK(launch_gemm8(plan.ksplit > 1 ? EPI8_PART : EPI8_STORE, plan, g, s));
+  prof_end(ctx, s, r);
+  *nsplit = plan.ksplit > 1 ? plan.ksplit : 0;
+  return SD_OK;
+}
+
 // One forward pass of a model over the rows set up by `rows` (or already in
 // the lane for prefill).  lm_M > 0: final norm over rows r*lm_stride+lm_off
 // and LM head into `logits` [lm_M, V]; lm_M = 0: the pass only extends the KV
@@ -585,13 +644,17 @@ int forward(sd_ctx* ctx, ModelRT& m, Lane& ln, RowsParams rows, int M, int nrb, 
     rc = gemm(ctx, m, EPI_RESID, ln.att, m.wo[l], M, d, m.nq(), ln.x, d, nullptr, s, pk_all, -1, nullptr,
               ln.part, max_split, &ns);
     if (rc) return rc;
-    NormParams np{ln.x, ns ? ln.part : nullptr, ns, m.ffn_norm[l], ln.xn, M, d, 1, 0, M, c.rms_eps};
-    HIPCHK(launch_rmsnorm(dt, np, s));
-    rc = gemm(ctx, m, EPI_SWIGLU, ln.xn, m.wgu[l], M, 2 * c.d_ffn, d, nullptr, 0, ln.hmid, s, pk_all,
-              verify ? SD_PROF_GEMM_VERIFY_GATEUP : -1);
-    if (rc) return rc;
-    rc = gemm(ctx, m, EPI_RESID, ln.hmid, m.wdown[l], M, d, c.d_ffn, ln.x, d, nullptr, s, pk_all, -1, nullptr,
-              ln.part, max_split, &ns);
+    if (m.ffn_q) {
+      rc = ffn_q(ctx, m, ln, l, M, ns, verify, s, &ns);
+    } else {
+      NormParams np{ln.x, ns ? ln.part : nullptr, ns, m.ffn_norm[l], ln.xn, M, d, 1, 0, M, c.rms_eps};
+      HIPCHK(launch_rmsnorm(dt, np, s));
+      rc = gemm(ctx, m, EPI_SWIGLU, ln.xn, m.wgu[l], M, 2 * c.d_ffn, d, nullptr, 0, ln.hmid, s, pk_all,
+                verify ? SD_PROF_GEMM_VERIFY_GATEUP : -1);
+      if (rc) return rc;
+      rc = gemm(ctx, m, EPI_RESID, ln.hmid, m.wdown[l], M, d, c.d_ffn, ln.x, d, nullptr, s, pk_all, -1, nullptr,
+                ln.part, max_split, &ns);
+    }
     if (rc) return rc;
     if (l + 1 < c.n_layers) {
       NormParams nn{ln.x, ns ? ln.part : nullptr, ns, m.attn_norm[l + 1], ln.xn, M, d, 1, 0, M, c.rms_eps};
@@ -620,6 +683,8 @@ bool model_ptrs_ok(const sd_weights* w, int L) {
 
 void load_model(ModelRT& m, const sd_model_cfg& c, const sd_weights* w, void* pool, int blocks) {
   m.c = c;
+  m.ffn_q = c.dtype == SD_DTYPE_BF16_FFN_Q;
+  if (m.ffn_q) m.c.dtype = SD_DTYPE_BF16;
   m.esz = esize(c.dtype);
   m.embed = w->embed;
   m.lm_head = w->lm_head;
@@ -728,8 +793,11 @@ int sd_plan_projection(const sd_config* cfg, int pass, int proj, int rows, sd_pr
     default: return SD_EINVAL;
   }
   if ((proj == SD_PROJ_KV && !prefill) || (proj == SD_PROJ_LM_HEAD && prefill)) return SD_EINVAL;
+  const bool ffn_q = c.dtype == SD_DTYPE_BF16_FFN_Q;
+  if (ffn_q && (proj == SD_PROJ_GATEUP || proj == SD_PROJ_DOWN)) return SD_EINVAL;
+  const int dtype = ffn_q ? SD_DTYPE_BF16 : c.dtype;
   if (epi == EPI_RESID) max_split = residual_splits(ln.part_rows, rows);
-  const ProjPlan pl = plan_projection(rows, N, K, c.dtype, esize(c.dtype), epi, max_split);
+  const ProjPlan pl = plan_projection(rows, N, K, dtype, esize(dtype), epi, max_split);
   *out = sd_proj_plan{};
   out->M = rows;
   out->N = N;
@@ -1195,7 +1263,7 @@ int sd_pack_linear(const void* src, void* dst, int N, int K, int dtype, void* st
 
 size_t sd_linear_q_bytes(int N, int K) {
   if (N < 1 || N > LINEAR8_MAX_MN || K < 1 || K > LINEAR8_MAX_K) return 0;
-  return (size_t)((N + 15) / 16) * blocks8(K) * 2048 + (size_t)((N + 127) / 128) * ke8(K);
+  return codes8_bytes(N, K) + (size_t)((N + 127) / 128) * ke8(K);
 }
 
 int sd_pack_linear_q(const void* src, void* dst, int N, int K, int dtype, void* stream) {
@@ -1220,52 +1288,62 @@ int sd_add_rmsnorm_q(int M, int d, int dtype, const void* x, int n_add, const vo
   return SD_OK;
 }
 
+size_t sd_linear_q_workspace_bytes(int M, int N, int K) {
+  if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K)) return 0;
+  const size_t one = (size_t)M * part8_ld(N), any = SIZE_MAX;
+  const int ks = M == 0 ? 1 : std::max(plan_gemm8(M, N, K, true, any).ksplit, plan_gemm8(M, N, K, false, any).ksplit);
+  return std::max<size_t>(256, ks > 1 ? ks * one * sizeof(float) : 0);
+}
+
 int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add, void* out,
-               int ldo, int dtype, void* stream) {
+                int ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K) || ldo < N || (dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32))
     return SD_EINVAL;
   if (M == 0) return SD_OK;
-  if (!q || !exps || !w || !out || ((uintptr_t)q | (uintptr_t)w) % 16) return SD_EINVAL;
+  if (!q || !exps || !w || !out || !workspace || workspace_bytes < sd_linear_q_workspace_bytes(M, N, K)) return SD_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)w | (uintptr_t)workspace) % 16 || (uintptr_t)exps % 4) return SD_EINVAL;
   if ((uintptr_t)add % 4 || (uintptr_t)out % esize(dtype)) return SD_EINVAL;
   Gemm8Params gp{};
   gp.q = q;
   gp.exps = exps;
   gp.w = (const uint8_t*)w;
-  gp.wexps = gp.w + (size_t)((N + 15) / 16) * blocks8(K) * 2048;
+  gp.wexps = gp.w + codes8_bytes(N, K);
   gp.M = M;
   gp.N = N;
   gp.K = K;
   gp.add = add;
   gp.out = out;
   gp.ldo = ldo;
+  gp.part = (float*)workspace;
   gp.bf16 = dtype == SD_DTYPE_BF16;
-  HIPCHK(launch_gemm8(EPI8_STORE, gp, (hipStream_t)stream));
+  const Gemm8Plan plan = plan_gemm8(M, N, K, dtype == SD_DTYPE_F32, workspace_bytes / sizeof(float));
+  HIPCHK(launch_gemm8(EPI8_STORE, plan, gp, (hipStream_t)stream));
   return SD_OK;
 }
 
-size_t sd_gate_up_q_workspace_bytes(int M, int F) {
-  if (M < 0 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_MN / 2) return 0;
-  return std::max<size_t>(256, (size_t)M * F * sizeof(float));
+size_t sd_gate_up_q_workspace_bytes(int M, int F, int K) {
+  if (M < 0 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_K || !sd_linear_q_bytes(2 * F, K)) return 0;
+  return gate_up8_fused(M, K) ? 256 : std::max<size_t>(256, (size_t)M * F * sizeof(float));
 }
 
 int sd_gate_up_q(int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
                 uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
-  const size_t need = sd_gate_up_q_workspace_bytes(M, F);
-  if (!need || !sd_linear_q_bytes(2 * F, K) || F > LINEAR8_MAX_K) return SD_EINVAL;
+  const size_t need = sd_gate_up_q_workspace_bytes(M, F, K);
+  if (!need) return SD_EINVAL;
   if (M == 0) return SD_OK;
   if (!q || !exps || !w || !q_out || !exps_out || !workspace || workspace_bytes < need) return SD_EINVAL;
-  if (((uintptr_t)q | (uintptr_t)w | (uintptr_t)q_out | (uintptr_t)workspace) % 16) return SD_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)w | (uintptr_t)q_out | (uintptr_t)workspace) % 16 || (uintptr_t)exps % 4) return SD_EINVAL;
   Gemm8Params gp{};
   gp.q = q;
   gp.exps = exps;
   gp.w = (const uint8_t*)w;
-  gp.wexps = gp.w + (size_t)(2 * F / 16) * blocks8(K) * 2048;
+  gp.wexps = gp.w + codes8_bytes(2 * F, K);
   gp.M = M;
   gp.N = 2 * F;
   gp.K = K;
-  gp.out = workspace;
-  HIPCHK(launch_gemm8(EPI8_SWIGLU, gp, (hipStream_t)stream));
-  HIPCHK(launch_quantise_rows8((const float*)workspace, q_out, exps_out, M, F, (hipStream_t)stream));
+  gp.q_out = q_out;
+  gp.exps_out = exps_out;
+  HIPCHK(launch_gate_up8(gp, (float*)workspace, (hipStream_t)stream));
   return SD_OK;
 }
 

@@ -247,13 +247,14 @@ enum GemmEpi { EPI_STORE = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_QKV = 3, EPI_PA
 
 // ---------------------------------------------------------------- 8-bit feed-forward
 
-// Operands in 8 bits (format: rows8.hip).  Activations: codes [M, K8] with K8 =
+// Operands in 8 bits (format: codes8.h).  Activations: codes [M, K8] with K8 =
 // K rounded up to 128 (zero codes past K), exponents [M, ke8(K)].  Weights:
 // 2 KB tiles of 16 rows x 128 columns (tile of rows 16 t .., column block b at
 // (t blocks + b) 2048; inside it 16-byte unit 64 h + 16 g + r holds row r,
 // columns 64 h + 16 g .. + 16), then exponents [rows / 128, ke8(K)].
 __host__ __device__ __forceinline__ int blocks8(int K) { return (K + 127) / 128; }
 __host__ __device__ __forceinline__ int ke8(int K) { return (blocks8(K) + 3) & ~3; }
+inline size_t codes8_bytes(int N, int K) { return (size_t)((N + 15) / 16) * blocks8(K) * 2048; }
 
 constexpr int NORM8_MAX_ADD = 6;       // addends of a norm: the K ranges of a residual projection
 constexpr int NORM8_MAX_D = 16384;     // row kept in registers
@@ -281,8 +282,15 @@ struct Gemm8Params {
   void* out;             // STORE: [M, ldo] fp32 or bf16; SWIGLU: h [M, N / 2] fp32
   int ldo;
   int bf16;              // STORE: out is bf16
+  int wide;              // STORE: out and add may be accessed four entries at a time (set by the launch)
+  int ksplit;            // K ranges (set by the launch)
+  float* part;           // their products [ksplit, M, part8_ld(N)] fp32 (plans of more than one range)
+  uint8_t* q_out;        // SWIGLU_Q: codes of h and their exponents
+  uint8_t* exps_out;
 };
-enum Gemm8Epi { EPI8_STORE = 0, EPI8_SWIGLU = 1 };
+// SWIGLU writes h = silu(gate) * up in fp32; SWIGLU_Q (passes that gate_up8_fused names) its codes.
+// PART leaves the K ranges' products in part for the caller to add (plans of more than one range)
+enum Gemm8Epi { EPI8_STORE = 0, EPI8_SWIGLU = 1, EPI8_SWIGLU_Q = 2, EPI8_PART = 3 };
 
 // ---------------------------------------------------------------- launchers
 // dtype: 0 bf16, 1 fp32 (same values as SD_DTYPE_*)
@@ -331,7 +339,16 @@ hipError_t launch_fill_i32(int32_t* p, int32_t v, size_t n, hipStream_t s);
 hipError_t launch_add_rmsnorm8(int x_dtype, int gain_dtype, const Norm8Params& p, hipStream_t s);
 hipError_t launch_quantise_rows8(const float* h, uint8_t* q, uint8_t* exps, int M, int F, hipStream_t s);
 hipError_t launch_pack_linear8(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
-hipError_t launch_gemm8(int epi, const Gemm8Params& p, hipStream_t s);
+bool gate_up8_fused(int M, int K);
+// How a STORE product runs.  exact: sums as exact as fp32 ones; else row tiles
+// use the 8-bit matrix instruction.  part_cap: entries that p.part holds
+struct Gemm8Plan { bool rows; int tile, ksplit; };
+inline int part8_ld(int N) { return (N + 3) & ~3; }
+Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap);
+// gate/up product p (N = 2 F columns) with SwiGLU, its output in p.q_out / p.exps_out; h: [M, F] fp32
+// scratch, unless gate_up8_fused
+hipError_t launch_gate_up8(const Gemm8Params& p, float* h, hipStream_t s);
+hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p, hipStream_t s);
 hipError_t launch_pack_linear(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 
 // GEMM geometry (shared by host planning and the kernel)

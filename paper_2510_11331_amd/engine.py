@@ -16,6 +16,7 @@ import torch
 
 from . import _lib
 from ._lib import check, lib
+from .ffn_q import pack_linear_q
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -26,10 +27,14 @@ def _stream(s: Optional[torch.cuda.Stream]):
     return C.c_void_p(s.cuda_stream) if s is not None else C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def model_cfg(shape) -> _lib.ModelCfg:
+def model_cfg(shape, ffn_q: bool = False) -> _lib.ModelCfg:
+    """ffn_q: the feed-forward network of a bf16 model in 8-bit floating point."""
+    if ffn_q and shape.dtype != "bf16":
+        raise ValueError("an 8-bit feed-forward network belongs to a bf16 model")
+    bf16 = _lib.SD_DTYPE_BF16_FFN_Q if ffn_q else _lib.SD_DTYPE_BF16
     return _lib.ModelCfg(shape.n_layers, shape.d_model, shape.n_heads, shape.n_kv_heads,
                          shape.head_dim, shape.d_ffn, shape.vocab,
-                         _lib.SD_DTYPE_BF16 if shape.dtype == "bf16" else _lib.SD_DTYPE_F32,
+                         bf16 if shape.dtype == "bf16" else _lib.SD_DTYPE_F32,
                          float(shape.rope_theta), float(shape.rms_eps))
 
 
@@ -53,9 +58,10 @@ class GPUModel:
     (query and key heads in rotary pair order), gate/up rows interleaved in
     16-row blocks, and the five projection
     matrices (QKV, O, gate/up, down, LM head) repacked on the device by
-    sd_pack_linear into the MFMA-tile layout."""
+    sd_pack_linear into the MFMA-tile layout; with ffn_q, gate/up and down
+    quantised and packed by sd_pack_linear_q."""
 
-    def __init__(self, shape, get: Callable[[str], np.ndarray], device="cuda"):
+    def __init__(self, shape, get: Callable[[str], np.ndarray], device="cuda", ffn_q: bool = False):
         self.shape = shape
         self.bf16 = shape.dtype == "bf16"
         self.device = device
@@ -74,8 +80,9 @@ class GPUModel:
                                                 rotary_pair_order(get(p + "wk"), hd), get(p + "wv")], axis=0)))
             self.wo.append(pk(get(p + "wo")))
             self.ffn_norm.append(up(get(p + "ffn_norm")))
-            self.wgu.append(pk(interleave_gate_up(get(p + "w_gate"), get(p + "w_up"))))
-            self.wdown.append(pk(get(p + "w_down")))
+            pf = self._packed_q if ffn_q else pk
+            self.wgu.append(pf(interleave_gate_up(get(p + "w_gate"), get(p + "w_up"))))
+            self.wdown.append(pf(get(p + "w_down")))
         arr = lambda ts: (C.c_void_p * L)(*[t.data_ptr() for t in ts])
         self._arrays = [arr(self.attn_norm), arr(self.wqkv), arr(self.wo), arr(self.ffn_norm),
                         arr(self.wgu), arr(self.wdown)]
@@ -108,6 +115,13 @@ class GPUModel:
         del src
         self.keep.append(dst)
         return dst
+
+    def _packed_q(self, a: np.ndarray) -> torch.Tensor:
+        """[N, K] row-major on the host -> quantised and packed on the device."""
+        w = pack_linear_q(self._to_device(a))
+        torch.cuda.current_stream(w.data.device).synchronize()
+        self.keep.append(w.data)
+        return w.data
 
 
 class Batch:
@@ -142,9 +156,12 @@ class SDEngine:
     def __init__(self, tshape, dshape, tget, dget, *, max_slots: int, max_batch: int, gamma_max: int,
                  max_ctx: int, kv_blocks_target: Optional[int] = None, kv_blocks_draft: Optional[int] = None,
                  prefill_rows: int = 1024, temperature: float = 1.0, greedy: bool = False,
-                 device: str = "cuda", static_workspace: bool = False):
+                 device: str = "cuda", static_workspace: bool = False, ffn_q: bool = False,
+                 draft_ffn_q: bool = False):
         """static_workspace: the context uses libsd's own per-device
-        workspace (sd_init_static) instead of one allocated here."""
+        workspace (sd_init_static) instead of one allocated here.  ffn_q,
+        draft_ffn_q: the target's, the draft's feed-forward network in 8-bit
+        floating point (SD_DTYPE_BF16_FFN_Q; bf16 models)."""
         L = lib()
         self.device = device
         self.tshape, self.dshape = tshape, dshape
@@ -152,8 +169,8 @@ class SDEngine:
         self.vocab = tshape.vocab
         blocks = max_slots * ((max_ctx + 15) // 16)
         cfg = _lib.Config()
-        cfg.target = model_cfg(tshape)
-        cfg.draft = model_cfg(dshape)
+        cfg.target = model_cfg(tshape, ffn_q)
+        cfg.draft = model_cfg(dshape, draft_ffn_q)
         cfg.max_slots, cfg.max_batch, cfg.gamma_max, cfg.max_ctx = max_slots, max_batch, gamma_max, max_ctx
         cfg.kv_block = 16
         cfg.kv_blocks_target = kv_blocks_target or blocks
@@ -176,8 +193,8 @@ class SDEngine:
             cfg.workspace = self.workspace.data_ptr()
             cfg.workspace_bytes = ws
         self.cfg = cfg
-        self.target = GPUModel(tshape, tget, device)
-        self.draft = GPUModel(dshape, dget, device)
+        self.target = GPUModel(tshape, tget, device, ffn_q)
+        self.draft = GPUModel(dshape, dget, device, draft_ffn_q)
         h = C.c_void_p()
         init = L.sd_init_static if static_workspace else L.sd_init
         rc = init(C.byref(cfg), C.byref(self.target.cstruct), C.byref(self.draft.cstruct), C.byref(h))

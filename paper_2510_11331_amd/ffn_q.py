@@ -161,8 +161,11 @@ def linear_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, add: Optional[torc
     with _On(q.device, stream) as s:
         if out is None:
             out = torch.empty(M, N, dtype=dtype, device=q.device)
+        ws = lib().sd_linear_q_workspace_bytes(M, N, w.K)
+        work = torch.empty(ws, dtype=torch.uint8, device=q.device)
         rc = lib().sd_linear_q(M, N, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(),
-                               None if add is None else add.data_ptr(), out.data_ptr(), ldo, _DTYPES[dtype], s)
+                               None if add is None else add.data_ptr(), out.data_ptr(), ldo, _DTYPES[dtype],
+                               work.data_ptr(), ws, s)
     if rc != SD_OK:
         check(rc, "sd_linear_q")
     return out
@@ -173,8 +176,8 @@ def gate_up_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, stream: Optional[
     """Rows (q, exps) of silu(gate) * up, w the packed [2 F, K] with gate and up rows interleaved in blocks of 16
     (engine.interleave_gate_up)."""
     M, F = _rows(q, exps, w), w.N // 2
-    ws = lib().sd_gate_up_q_workspace_bytes(M, F) if w.N % 32 == 0 else 0
-    _need(ws > 0 and F <= 1 << 18, "gate and up rows come in blocks of 16, at most 2^18 of each")
+    ws = lib().sd_gate_up_q_workspace_bytes(M, F, w.K) if w.N % 32 == 0 else 0
+    _need(ws > 0, "gate and up rows come in blocks of 16, at most 2^18 of each")
     with _On(q.device, stream) as s:
         q_out = torch.empty(M, _k8(F), dtype=_E4M3, device=q.device)
         exps_out = torch.empty(M, _ke(F), dtype=_E8M0, device=q.device)

@@ -48,9 +48,11 @@ def test_sizes():
         assert L.sd_linear_q_bytes(N, K) == qref.up(N, 16) * qref.up(K, 128) + -(-N // 128) * qref.up(-(-K // 128), 4)
     for N, K in ((0, 1), (1, 0), (-1, 5), (1, (1 << 18) + 1), ((1 << 22) + 1, 1)):
         assert L.sd_linear_q_bytes(N, K) == 0
-    assert L.sd_gate_up_q_workspace_bytes(40, 11008) >= 1 and L.sd_gate_up_q_workspace_bytes(0, 16) >= 1
-    for M, F in ((-1, 16), (1, 0), (1, 8), (1, 24), (1 << 23, 16)):
-        assert L.sd_gate_up_q_workspace_bytes(M, F) == 0
+    assert L.sd_gate_up_q_workspace_bytes(40, 11008, 4096) >= 1 and L.sd_gate_up_q_workspace_bytes(0, 16, 1) >= 1
+    for M, F, K in ((-1, 16, 1), (1, 0, 1), (1, 8, 1), (1, 24, 1), (1 << 23, 16, 1), (1, 16, 0), (1, (1 << 18) + 16, 1)):
+        assert L.sd_gate_up_q_workspace_bytes(M, F, K) == 0
+    assert L.sd_linear_q_workspace_bytes(0, 1, 1) and L.sd_linear_q_workspace_bytes(300, 4096, 11008)
+    assert L.sd_linear_q_workspace_bytes(-1, 1, 1) == L.sd_linear_q_workspace_bytes(1, 0, 1) == 0
 
 
 @needs_lib
@@ -72,16 +74,17 @@ def test_calls_refuse():
         assert L.sd_add_rmsnorm_q(*{**nm, **bad}.values(), None) == E, bad
     assert L.sd_add_rmsnorm_q(*{**nm, "M": 0, "x": None, "q": None}.values(), None) == _lib.SD_OK
 
-    ln = dict(M=2, N=64, K=64, q=A, exps=A, w=A, add=A, out=A, ldo=64, dtype=F32)
+    ln = dict(M=2, N=64, K=64, q=A, exps=A, w=A, add=A, out=A, ldo=64, dtype=F32, ws=A, n=L.sd_linear_q_workspace_bytes(2, 64, 64))
     for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(K=(1 << 18) + 1), dict(q=None), dict(exps=None), dict(w=None), dict(out=None), dict(ldo=63),
-                dict(dtype=2), dict(q=A + 8), dict(w=A + 8), dict(add=A + 2), dict(out=A + 2), dict(M=(1 << 22) + 1)):
+                dict(dtype=2), dict(q=A + 8), dict(w=A + 8), dict(add=A + 2), dict(out=A + 2), dict(M=(1 << 22) + 1), dict(ws=None), dict(n=255),
+                dict(ws=A + 8), dict(exps=A + 2)):
         assert L.sd_linear_q(*{**ln, **bad}.values(), None) == E, bad
     assert L.sd_linear_q(*{**ln, "M": 0, "out": None}.values(), None) == _lib.SD_OK
 
-    n = L.sd_gate_up_q_workspace_bytes(2, 64)
+    n = L.sd_gate_up_q_workspace_bytes(2, 64, 64)
     gu = dict(M=2, F=64, K=64, q=A, exps=A, w=A, q_out=A, exps_out=A, ws=A, n=n)
     for bad in (dict(M=-1), dict(F=0), dict(F=65), dict(F=72), dict(K=0), dict(q=None), dict(exps=None), dict(w=None), dict(q_out=None),
-                dict(exps_out=None), dict(ws=None), dict(n=n - 1), dict(q=A + 8), dict(w=A + 8), dict(q_out=A + 8), dict(ws=A + 8)):
+                dict(exps_out=None), dict(ws=None), dict(n=n - 1), dict(q=A + 8), dict(w=A + 8), dict(q_out=A + 8), dict(ws=A + 8), dict(exps=A + 2)):
         assert L.sd_gate_up_q(*{**gu, **bad}.values(), None) == E, bad
     assert L.sd_gate_up_q(*{**gu, "M": 0, "q": None}.values(), None) == _lib.SD_OK
 
@@ -124,3 +127,29 @@ def test_python_refuses():
     refused(linear_q, q, e, w, add=torch.zeros(3, 16).bfloat16())
     refused(linear_q, q, e, w, add=torch.zeros(3, 32)[:, :16])
     refused(gate_up_q, q, e, w)                                               # 16 rows are no gate and up block
+
+
+@needs_lib
+def test_model_dtype():
+    """SD_DTYPE_BF16_FFN_Q: sizes of a configuration, its plan queries, and the binding's refusal of fp32 models."""
+    import synth
+    from paper_2510_11331_amd import _lib
+    from paper_2510_11331_amd.engine import model_cfg
+    L = _lib.lib()
+    c = _lib.Config()
+    t, d = synth.MODELS["small_target"], synth.MODELS["small_draft"]
+    c.target, c.draft = model_cfg(t), model_cfg(d)
+    c.max_slots, c.max_batch, c.gamma_max, c.max_ctx = 4, 2, 4, 128
+    c.kv_block, c.kv_blocks_target, c.kv_blocks_draft, c.prefill_rows, c.temperature = 16, 32, 32, 128, 1.0
+    plain, pool = L.sd_workspace_bytes(C.byref(c)), L.sd_kv_pool_bytes(C.byref(c), 0)
+    c.target = model_cfg(t, ffn_q=True)
+    assert c.target.dtype == _lib.SD_DTYPE_BF16_FFN_Q
+    assert L.sd_workspace_bytes(C.byref(c)) > plain and L.sd_kv_pool_bytes(C.byref(c), 0) == pool
+    p = _lib.ProjPlan()
+    plan = lambda proj: L.sd_plan_projection(C.byref(c), _lib.SD_PASS_VERIFY, proj, 10, C.byref(p))
+    assert plan(_lib.SD_PROJ_QKV) == plan(_lib.SD_PROJ_O) == plan(_lib.SD_PROJ_LM_HEAD) == _lib.SD_OK
+    assert plan(_lib.SD_PROJ_GATEUP) == plan(_lib.SD_PROJ_DOWN) == _lib.SD_EINVAL
+    c.target.dtype = 3
+    assert L.sd_workspace_bytes(C.byref(c)) == 0
+    with pytest.raises(ValueError):
+        model_cfg(synth.MODELS["tiny_target"], ffn_q=True)
