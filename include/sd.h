@@ -348,9 +348,10 @@ int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const vo
 /* out = [add +] rows W^T: rows (q, exps) [M, K], w a packed [N, K].  out
  * [M, N] of dtype with row stride ldo >= N (entries); add NULL or fp32 with
  * the same stride; with dtype fp32 it may be out itself (else no overlap).
- * The workspace (16-byte aligned, sd_linear_q_workspace_bytes(M, N, K)) is
- * scratch of this call alone until its work is done: calls that may overlap,
- * graphs among them, need one each. */
+ * The workspace (16-byte aligned, sd_linear_q_workspace_bytes(M, N, K); where
+ * that is 0, as on an invalid size, it may be NULL) is scratch of this call
+ * alone until its work is done: calls that may overlap, graphs among them, need
+ * one each. */
 size_t sd_linear_q_workspace_bytes(int M, int N, int K);
 int sd_linear_q(int M, int N, int K, const uint8_t *q, const uint8_t *exps, const void *w, const float *add,
                 void *out, int ldo, int dtype, void *workspace, size_t workspace_bytes, void *stream);

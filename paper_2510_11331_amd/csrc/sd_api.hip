@@ -1292,7 +1292,7 @@ size_t sd_linear_q_workspace_bytes(int M, int N, int K) {
   if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K)) return 0;
   const size_t one = (size_t)M * part8_ld(N), any = SIZE_MAX;
   const int ks = M == 0 ? 1 : std::max(plan_gemm8(M, N, K, true, any).ksplit, plan_gemm8(M, N, K, false, any).ksplit);
-  return std::max<size_t>(256, ks > 1 ? ks * one * sizeof(float) : 0);
+  return ks > 1 ? ks * one * sizeof(float) : 0;
 }
 
 int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add, void* out,
@@ -1300,7 +1300,8 @@ int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, cons
   if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K) || ldo < N || (dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32))
     return SD_EINVAL;
   if (M == 0) return SD_OK;
-  if (!q || !exps || !w || !out || !workspace || workspace_bytes < sd_linear_q_workspace_bytes(M, N, K)) return SD_EINVAL;
+  const size_t need = sd_linear_q_workspace_bytes(M, N, K);
+  if (!q || !exps || !w || !out || (need && (!workspace || workspace_bytes < need))) return SD_EINVAL;
   if (((uintptr_t)q | (uintptr_t)w | (uintptr_t)workspace) % 16 || (uintptr_t)exps % 4) return SD_EINVAL;
   if ((uintptr_t)add % 4 || (uintptr_t)out % esize(dtype)) return SD_EINVAL;
   Gemm8Params gp{};
@@ -1316,22 +1317,22 @@ int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, cons
   gp.ldo = ldo;
   gp.part = (float*)workspace;
   gp.bf16 = dtype == SD_DTYPE_BF16;
-  const Gemm8Plan plan = plan_gemm8(M, N, K, dtype == SD_DTYPE_F32, workspace_bytes / sizeof(float));
+  const Gemm8Plan plan = plan_gemm8(M, N, K, dtype == SD_DTYPE_F32, need / sizeof(float));
   HIPCHK(launch_gemm8(EPI8_STORE, plan, gp, (hipStream_t)stream));
   return SD_OK;
 }
 
 size_t sd_gate_up_q_workspace_bytes(int M, int F, int K) {
   if (M < 0 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_K || !sd_linear_q_bytes(2 * F, K)) return 0;
-  return gate_up8_fused(M, K) ? 256 : std::max<size_t>(256, (size_t)M * F * sizeof(float));
+  return gate_up8_fused(M, K) ? 0 : (size_t)M * F * sizeof(float);
 }
 
 int sd_gate_up_q(int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
                 uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
-  const size_t need = sd_gate_up_q_workspace_bytes(M, F, K);
-  if (!need) return SD_EINVAL;
+  if (M < 0 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_K || !sd_linear_q_bytes(2 * F, K)) return SD_EINVAL;
   if (M == 0) return SD_OK;
-  if (!q || !exps || !w || !q_out || !exps_out || !workspace || workspace_bytes < need) return SD_EINVAL;
+  const size_t need = sd_gate_up_q_workspace_bytes(M, F, K);
+  if (!q || !exps || !w || !q_out || !exps_out || (need && (!workspace || workspace_bytes < need))) return SD_EINVAL;
   if (((uintptr_t)q | (uintptr_t)w | (uintptr_t)q_out | (uintptr_t)workspace) % 16 || (uintptr_t)exps % 4) return SD_EINVAL;
   Gemm8Params gp{};
   gp.q = q;

@@ -16,7 +16,6 @@ that the kernels do not cover raise ValueError before anything is enqueued.
 """
 from __future__ import annotations
 
-from contextlib import nullcontext
 from typing import Optional, Tuple
 
 import torch
@@ -28,9 +27,8 @@ _DTYPES = {torch.bfloat16: SD_DTYPE_BF16, torch.float32: SD_DTYPE_F32}
 _E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _k8(K: int) -> int:
@@ -41,24 +39,42 @@ def _ke(K: int) -> int:
     return (K + 511) // 512 * 4
 
 
-class _On:
-    """The device and stream of a call: tensors are made and work is enqueued there."""
+class _Elsewhere:
+    """The device and stream of a call that is not for the current ones: tensors are made and work is enqueued there."""
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream]):
-        _need(device.type == "cuda", "tensors on a GPU are needed")
-        if stream is not None:
-            _need(stream.device == device, "the stream is of another device than the tensors")
-            self.ctx = torch.cuda.stream(stream)
-        else:
-            self.ctx = nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.device = device
+        if stream is not None and stream.device != device:
+            raise ValueError("the stream is of another device than the tensors")
+        self.ctx = torch.cuda.device(device) if stream is None else torch.cuda.stream(stream)
+        self.index = device.index
 
     def __enter__(self) -> int:
         self.ctx.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream
+        return _raw_stream(self.index)
 
     def __exit__(self, *a):
         return self.ctx.__exit__(*a)
+
+
+class _Here:
+    """The current device's current stream (the usual case: a few microseconds of host time matter to short calls)."""
+
+    def __enter__(self) -> int:
+        return _raw_stream(torch.cuda.current_device())
+
+    def __exit__(self, *a):
+        return False
+
+
+_HERE = _Here()
+
+
+def _on(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+    if not t.is_cuda:
+        raise ValueError("tensors on a GPU are needed")
+    if stream is None and t.get_device() == torch.cuda.current_device():
+        return _HERE
+    return _Elsewhere(t.device, stream)
 
 
 class LinearQ:
@@ -68,9 +84,10 @@ class LinearQ:
 
     def __init__(self, data: torch.Tensor, N: int, K: int):
         n = lib().sd_linear_q_bytes(N, K)
-        _need(n > 0, f"no packed matrix of {N} x {K}")
-        _need(data.dtype == torch.uint8 and data.dim() == 1 and data.numel() == n and data.is_contiguous(),
-              f"a packed {N} x {K} matrix is a contiguous uint8 tensor of {n} entries")
+        if n == 0:
+            raise ValueError(f"no packed matrix of {N} x {K}")
+        if data.dtype != torch.uint8 or data.shape != (n,) or not data.is_contiguous():
+            raise ValueError(f"a packed {N} x {K} matrix is a contiguous uint8 tensor of {n} entries")
         self.data, self.N, self.K = data, N, K
 
     @property
@@ -86,11 +103,13 @@ class LinearQ:
 
 def pack_linear_q(w: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> LinearQ:
     """Quantise and pack a weight [N, K] (bfloat16 or float32)."""
-    _need(w.dim() == 2 and w.dtype in _DTYPES and w.is_contiguous(), "w: contiguous [N, K], bfloat16 or float32")
+    if w.dim() != 2 or w.dtype not in _DTYPES or not w.is_contiguous():
+        raise ValueError("w: contiguous [N, K], bfloat16 or float32")
     N, K = w.shape
     n = lib().sd_linear_q_bytes(N, K)
-    _need(n > 0, f"no packed matrix of {N} x {K}")
-    with _On(w.device, stream) as s:
+    if n == 0:
+        raise ValueError(f"no packed matrix of {N} x {K}")
+    with _on(w, stream) as s:
         data = torch.empty(n, dtype=torch.uint8, device=w.device)
         check(lib().sd_pack_linear_q(w.data_ptr(), data.data_ptr(), N, K, _DTYPES[w.dtype], s), "sd_pack_linear_q")
     return LinearQ(data, N, K)
@@ -102,42 +121,46 @@ def add_rmsnorm_q(x: torch.Tensor, gain: torch.Tensor, eps: float, add: Optional
     """(s, q, exps) with s = x + add and q, exps the rows of s / sqrt(mean(s^2) + eps) * gain.  x [M, d] is bfloat16 or
     float32; add of its type [M, d], or [n, M, d] (n <= 6, all of them are added), or None (s is then x itself).  gain [d]
     is bfloat16 or float32.  x_out: where s goes (may be x)."""
-    _need(x.dim() == 2 and x.dtype in _DTYPES and x.is_contiguous(), "x: contiguous [M, d], bfloat16 or float32")
+    t, dev = x.dtype, x.device
+    if x.dim() != 2 or t not in _DTYPES or not x.is_contiguous():
+        raise ValueError("x: contiguous [M, d], bfloat16 or float32")
     M, d = x.shape
-    _need(1 <= d <= 16384, "rows of 1 to 16384 entries")
-    _need(gain.shape == (d,) and gain.dtype in _DTYPES and gain.is_contiguous() and gain.device == x.device,
-          "gain: [d], bfloat16 or float32, on the device of x")
+    if not 1 <= d <= 16384:
+        raise ValueError("rows of 1 to 16384 entries")
+    if gain.shape != (d,) or gain.dtype not in _DTYPES or not gain.is_contiguous() or gain.device != dev:
+        raise ValueError("gain: [d], bfloat16 or float32, on the device of x")
     n = 0
     if add is not None:
         n = 1 if add.dim() == 2 else add.shape[0]
-        _need(add.shape[-2:] == x.shape and add.dim() in (2, 3) and add.dtype == x.dtype and add.is_contiguous()
-              and add.device == x.device, "add: contiguous [M, d] or [n, M, d] of x's type and device")
-        _need(n <= 6, "at most 6 addends")
-    if n:
-        _need(x_out is None or (x_out.shape == x.shape and x_out.dtype == x.dtype and x_out.is_contiguous()
-                                and x_out.device == x.device), "x_out: as x")
-    else:
-        _need(x_out is None or x_out.data_ptr() == x.data_ptr(), "x_out is written with addends only")
-    with _On(x.device, stream) as s:
+        if (add.dim() not in (2, 3) or add.shape[-2:] != x.shape or add.dtype != t or not add.is_contiguous()
+                or add.device != dev):
+            raise ValueError("add: contiguous [M, d] or [n, M, d] of x's type and device")
+        if n > 6:
+            raise ValueError("at most 6 addends")
+    if x_out is not None:
+        if n and (x_out.shape != x.shape or x_out.dtype != t or not x_out.is_contiguous() or x_out.device != dev):
+            raise ValueError("x_out: as x")
+        if not n and x_out.data_ptr() != x.data_ptr():
+            raise ValueError("x_out is written with addends only")
+    with _on(x, stream) as s:
         out = x if not n else torch.empty_like(x) if x_out is None else x_out
-        q = torch.empty(M, _k8(d), dtype=_E4M3, device=x.device)
-        exps = torch.empty(M, _ke(d), dtype=_E8M0, device=x.device)
-        rc = lib().sd_add_rmsnorm_q(M, d, _DTYPES[x.dtype], x.data_ptr(), n, add.data_ptr() if n else None,
-                                    out.data_ptr(), gain.data_ptr(), _DTYPES[gain.dtype], eps, q.data_ptr(),
-                                    exps.data_ptr(), s)
+        q = torch.empty((M, _k8(d)), dtype=_E4M3, device=dev)
+        exps = torch.empty((M, _ke(d)), dtype=_E8M0, device=dev)
+        rc = lib().sd_add_rmsnorm_q(M, d, _DTYPES[t], x.data_ptr(), n, add.data_ptr() if n else None, out.data_ptr(),
+                                    gain.data_ptr(), _DTYPES[gain.dtype], eps, q.data_ptr(), exps.data_ptr(), s)
     if rc != SD_OK:
         check(rc, "sd_add_rmsnorm_q")
     return out, q, exps
 
 
 def _rows(q: torch.Tensor, exps: torch.Tensor, w: LinearQ) -> int:
-    K = w.K
-    _need(q.dtype == _E4M3 and q.dim() == 2 and q.shape[1] == _k8(K) and q.is_contiguous(),
-          f"q: contiguous float8_e4m3fn [M, {_k8(K)}]")
-    M = q.shape[0]
-    _need(exps.dtype == _E8M0 and exps.shape == (M, _ke(K)) and exps.is_contiguous(),
-          f"exps: contiguous float8_e8m0fnu [M, {_ke(K)}]")
-    _need(q.device == exps.device == w.data.device, "rows and weight on one device")
+    M, K = len(q), w.K
+    if q.dtype != _E4M3 or q.shape != (M, _k8(K)) or not q.is_contiguous():
+        raise ValueError(f"q: contiguous float8_e4m3fn [M, {_k8(K)}]")
+    if exps.dtype != _E8M0 or exps.shape != (M, _ke(K)) or not exps.is_contiguous():
+        raise ValueError(f"exps: contiguous float8_e8m0fnu [M, {_ke(K)}]")
+    if not q.device == exps.device == w.data.device:
+        raise ValueError("rows and weight on one device")
     return M
 
 
@@ -146,26 +169,29 @@ def linear_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, add: Optional[torc
              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """[add +] rows W^T as [M, N] of dtype (float32 or bfloat16).  out: where it goes (rows may lie apart); add: float32
     with out's strides, or out itself."""
-    M, N = _rows(q, exps, w), w.N
+    M, N, dev = _rows(q, exps, w), w.N, q.device
+    ldo = N
     if out is not None:
         dtype = out.dtype
-        _need(out.shape == (M, N) and (N == 1 or M == 0 or out.stride(1) == 1) and (M <= 1 or out.stride(0) >= N)
-              and out.device == q.device, "out: [M, N] with adjacent columns, on the device of the rows")
-    _need(dtype in _DTYPES, "outputs are float32 or bfloat16")
-    ldo = out.stride(0) if out is not None and M > 1 else N
-    _need(ldo < 1 << 31, "rows of out less than 2^31 entries apart")
-    if add is not None:
-        _need(add.dtype == torch.float32 and add.shape == (M, N) and add.device == q.device
-              and (N == 1 or M == 0 or add.stride(1) == 1) and (M <= 1 or add.stride(0) == ldo),
-              "add: float32 [M, N] with the strides of the output")
-    with _On(q.device, stream) as s:
+        if (out.shape != (M, N) or out.device != dev or not (N == 1 or M == 0 or out.stride(1) == 1)
+                or not (M <= 1 or N <= out.stride(0) < 1 << 31)):
+            raise ValueError("out: [M, N] with adjacent columns, on the device of the rows")
+        if M > 1:
+            ldo = out.stride(0)
+    if dtype not in _DTYPES:
+        raise ValueError("outputs are float32 or bfloat16")
+    if add is not None and (add.dtype != torch.float32 or add.shape != (M, N) or add.device != dev
+                            or not (N == 1 or M == 0 or add.stride(1) == 1) or not (M <= 1 or add.stride(0) == ldo)):
+        raise ValueError("add: float32 [M, N] with the strides of the output")
+    L = lib()
+    ws = L.sd_linear_q_workspace_bytes(M, N, w.K)
+    with _on(q, stream) as s:
         if out is None:
-            out = torch.empty(M, N, dtype=dtype, device=q.device)
-        ws = lib().sd_linear_q_workspace_bytes(M, N, w.K)
-        work = torch.empty(ws, dtype=torch.uint8, device=q.device)
-        rc = lib().sd_linear_q(M, N, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(),
-                               None if add is None else add.data_ptr(), out.data_ptr(), ldo, _DTYPES[dtype],
-                               work.data_ptr(), ws, s)
+            out = torch.empty((M, N), dtype=dtype, device=dev)
+        work = torch.empty(ws, dtype=torch.uint8, device=dev) if ws else None
+        rc = L.sd_linear_q(M, N, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(),
+                           None if add is None else add.data_ptr(), out.data_ptr(), ldo, _DTYPES[dtype],
+                           work.data_ptr() if ws else None, ws, s)
     if rc != SD_OK:
         check(rc, "sd_linear_q")
     return out
@@ -175,15 +201,17 @@ def gate_up_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, stream: Optional[
               ) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows (q, exps) of silu(gate) * up, w the packed [2 F, K] with gate and up rows interleaved in blocks of 16
     (engine.interleave_gate_up)."""
-    M, F = _rows(q, exps, w), w.N // 2
-    ws = lib().sd_gate_up_q_workspace_bytes(M, F, w.K) if w.N % 32 == 0 else 0
-    _need(ws > 0, "gate and up rows come in blocks of 16, at most 2^18 of each")
-    with _On(q.device, stream) as s:
-        q_out = torch.empty(M, _k8(F), dtype=_E4M3, device=q.device)
-        exps_out = torch.empty(M, _ke(F), dtype=_E8M0, device=q.device)
-        work = torch.empty(ws, dtype=torch.uint8, device=q.device)
-        rc = lib().sd_gate_up_q(M, F, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(), q_out.data_ptr(),
-                                exps_out.data_ptr(), work.data_ptr(), ws, s)
+    M, F, dev = _rows(q, exps, w), w.N // 2, q.device
+    L = lib()
+    if w.N % 32 or F > 1 << 18:
+        raise ValueError("gate and up rows come in blocks of 16, at most 2^18 of each")
+    with _on(q, stream) as s:
+        q_out = torch.empty((M, _k8(F)), dtype=_E4M3, device=dev)
+        exps_out = torch.empty((M, _ke(F)), dtype=_E8M0, device=dev)
+        ws = L.sd_gate_up_q_workspace_bytes(M, F, w.K)
+        work = torch.empty(ws, dtype=torch.uint8, device=dev) if ws else None
+        rc = L.sd_gate_up_q(M, F, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(), q_out.data_ptr(),
+                            exps_out.data_ptr(), work.data_ptr() if ws else None, ws, s)
     if rc != SD_OK:
         check(rc, "sd_gate_up_q")
     return q_out, exps_out

@@ -48,11 +48,12 @@ def test_sizes():
         assert L.sd_linear_q_bytes(N, K) == qref.up(N, 16) * qref.up(K, 128) + -(-N // 128) * qref.up(-(-K // 128), 4)
     for N, K in ((0, 1), (1, 0), (-1, 5), (1, (1 << 18) + 1), ((1 << 22) + 1, 1)):
         assert L.sd_linear_q_bytes(N, K) == 0
-    assert L.sd_gate_up_q_workspace_bytes(40, 11008, 4096) >= 1 and L.sd_gate_up_q_workspace_bytes(0, 16, 1) >= 1
+    assert L.sd_gate_up_q_workspace_bytes(40, 11008, 4096) == 40 * 11008 * 4 and L.sd_gate_up_q_workspace_bytes(0, 16, 1) == 0
     for M, F, K in ((-1, 16, 1), (1, 0, 1), (1, 8, 1), (1, 24, 1), (1 << 23, 16, 1), (1, 16, 0), (1, (1 << 18) + 16, 1)):
         assert L.sd_gate_up_q_workspace_bytes(M, F, K) == 0
-    assert L.sd_linear_q_workspace_bytes(0, 1, 1) and L.sd_linear_q_workspace_bytes(300, 4096, 11008)
-    assert L.sd_linear_q_workspace_bytes(-1, 1, 1) == L.sd_linear_q_workspace_bytes(1, 0, 1) == 0
+    # K ranges: whole sums [ranges, M, N rounded up to 4]
+    assert L.sd_linear_q_workspace_bytes(100, 1023, 11008) in (2 * 100 * 1024 * 4, 4 * 100 * 1024 * 4)
+    assert L.sd_linear_q_workspace_bytes(-1, 1, 1) == L.sd_linear_q_workspace_bytes(1, 0, 1) == L.sd_linear_q_workspace_bytes(0, 1, 1) == 0
 
 
 @needs_lib
@@ -74,9 +75,11 @@ def test_calls_refuse():
         assert L.sd_add_rmsnorm_q(*{**nm, **bad}.values(), None) == E, bad
     assert L.sd_add_rmsnorm_q(*{**nm, "M": 0, "x": None, "q": None}.values(), None) == _lib.SD_OK
 
-    ln = dict(M=2, N=64, K=64, q=A, exps=A, w=A, add=A, out=A, ldo=64, dtype=F32, ws=A, n=L.sd_linear_q_workspace_bytes(2, 64, 64))
+    n = L.sd_linear_q_workspace_bytes(100, 64, 11008)
+    assert n >= 2 * 100 * 64 * 4
+    ln = dict(M=100, N=64, K=11008, q=A, exps=A, w=A, add=A, out=A, ldo=64, dtype=F32, ws=A, n=n)
     for bad in (dict(M=-1), dict(N=0), dict(K=0), dict(K=(1 << 18) + 1), dict(q=None), dict(exps=None), dict(w=None), dict(out=None), dict(ldo=63),
-                dict(dtype=2), dict(q=A + 8), dict(w=A + 8), dict(add=A + 2), dict(out=A + 2), dict(M=(1 << 22) + 1), dict(ws=None), dict(n=255),
+                dict(dtype=2), dict(q=A + 8), dict(w=A + 8), dict(add=A + 2), dict(out=A + 2), dict(M=(1 << 22) + 1), dict(ws=None), dict(n=n - 1),
                 dict(ws=A + 8), dict(exps=A + 2)):
         assert L.sd_linear_q(*{**ln, **bad}.values(), None) == E, bad
     assert L.sd_linear_q(*{**ln, "M": 0, "out": None}.values(), None) == _lib.SD_OK
