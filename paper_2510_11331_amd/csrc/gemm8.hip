@@ -87,13 +87,18 @@ __device__ __forceinline__ void add_scaled(f32x4& acc, f32x4 s, float f) {
   for (int v = 0; v < 4; ++v) acc[v] = fmaf(s[v], f, acc[v]);
 }
 
-// Product for few rows (up to 64 a workgroup), bound by streaming the weights:
-// a workgroup takes 16 NT columns x 16 MT rows, its KW waves the 128-entry
-// blocks of K in turn, and their sums are added through LDS in wave order.  A
-// wave loads its weight tiles into registers and its rows into a part of LDS of
-// its own, D - 1 blocks ahead, and waits for nothing but its own loads.  (The rows go
-// through LDS because a load straight into the operand's layout touches 16
-// rows' lines: four times the address work of one that reads whole lines.)
+// K ranges: ksplit of them, whole groups of four blocks (which share a load of
+// scales), none empty if the launch has checked range8(kb, ksplit) (ksplit - 1) < kb
+__host__ __device__ __forceinline__ int range8(int kb, int ksplit) { return ((kb + ksplit - 1) / ksplit + 3) & ~3; }
+
+// Product for few rows (up to 64), bound by streaming the weights: a workgroup
+// takes up to NT tiles of 16 columns and all rows (MT tiles), its KW waves the
+// 128-entry blocks of its K range in turn, and their sums are added through LDS
+// in wave order.  A wave loads its weight tiles into registers and its rows
+// into a part of LDS of its own, D - 1 blocks ahead, and waits for nothing but
+// its own loads.  (The rows go through LDS because a load straight into the
+// operand's layout touches 16 rows' lines: four times the address work of one
+// that reads whole lines.)
 //
 // The products run on fp16 operands: a block's sum of exact fp32 products is
 // scaled and added in fp32.  The 8-bit matrix instruction drops low bits of
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
   constexpr int STAGE = MT * 2048;                           // bytes of a block's rows
   constexpr int PS = 2 * MT + 2 * NT;                        // loads of a block
   constexpr int RED = KW * NT * MT * 1024, BUF = KW * D * STAGE > RED ? KW * D * STAGE : RED;
-  constexpr int SCALES = (16 * MT + 1) * STREAM8_KE / 256 * 256 + 256;
+  constexpr int SCALES = (16 * MT + 2) * STREAM8_KE;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[BUF + SCALES];
   static_assert(BUF + SCALES <= 160 * 1024 && (D - 1) * PS < 64, "LDS of a CU, loads in flight");
 
@@ -114,34 +119,38 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, g = lane >> 4;
   const int kb = blocks8(p.K), ke = ke8(p.K), K8 = 128 * kb;
-  const int tiles = (p.N + 15) / 16, gx = (tiles + NT - 1) / NT;
-  const int bx = blockIdx.x % gx, bz = blockIdx.x / gx;
-  const int tile0 = bx * NT, ntile = min(NT, tiles - tile0);
-  const int m0 = bz * 16 * MT, mrows = min(16 * MT, p.M - m0);
+  // the columns' tiles (SwiGLU: pairs of a gate tile and its up tile) are dealt
+  // to the workgroups of a K range evenly, a contiguous run of at most NT tiles each
+  const int tiles = (p.N + 15) / 16, gx = gridDim.x / p.ksplit;
+  const int bx = blockIdx.x % gx, split = blockIdx.x / gx;
+  const int units = tiles / TPU, base = units / gx, extra = units % gx;
+  const int tile0 = (bx * base + min(bx, extra)) * TPU, ntile = (base + (bx < extra ? 1 : 0)) * TPU;
+  const int sps = range8(kb, p.ksplit), s_lo = split * sps, s_hi = min(s_lo + sps, kb);   // blocks of this K range
+  const int mrows = p.M;
   const uint32_t tile_bytes = (uint32_t)kb * 2048u;
   const uint8_t* Wp = p.w + (size_t)tile0 * tile_bytes;
-  const uint8_t* Ap = p.q + (size_t)m0 * K8;
+  const uint8_t* Ap = p.q;
   uint8_t* const own = smem + wave * D * STAGE;
 
-  // the scales of the rows, then of the columns (NT divides 8: one row of them),
-  // are copied to LDS once: 256 bytes a load (a load of one block's scales
-  // would touch a line per row)
+  // the scales of the rows, then of the columns (one or two rows of them) are copied to LDS:
+  // 256 bytes a load (a load of one block's scales would touch a line per row)
   uint8_t* const sc = smem + BUF;
   const uint8_t* const wsc = sc + mrows * ke;
   {
-    const __amdgpu_buffer_rsrc_t er = rsrc8(p.exps + (size_t)m0 * ke, (uint32_t)mrows * ke);
-    const __amdgpu_buffer_rsrc_t fr = rsrc8(p.wexps + (size_t)(tile0 / 8) * ke, ke);
+    const __amdgpu_buffer_rsrc_t er = rsrc8(p.exps, (uint32_t)mrows * ke);
+    const int wn = ((tile0 + ntile - 1) / 8 - tile0 / 8 + 1) * ke;
+    const __amdgpu_buffer_rsrc_t fr = rsrc8(p.wexps + (size_t)(tile0 / 8) * ke, wn);
     const int n = mrows * ke;
-    for (int o = wave * 256; o < n + ke; o += KW * 256) {
+    for (int o = wave * 256; o < n + wn; o += KW * 256) {
       const uint32_t at = o + 4 * lane;
       const bool rows = (int)at < n;
-      // (the part in which the rows' scales end goes through registers)
+      // (the part in which the rows' scales end, and the columns', go through registers)
       if (o < n && o + 256 <= n) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(er, (__attribute__((address_space(3))) void*)(sc + o), 4, at, 0, 0, 0);
       } else {
         const uint32_t x = rows ? __builtin_amdgcn_raw_buffer_load_b32(er, at, 0, 0)
                                 : __builtin_amdgcn_raw_buffer_load_b32(fr, at - n, 0, 0);
-        if ((int)at < n + ke) *(uint32_t*)(sc + at) = x;
+        if ((int)at < n + wn) *(uint32_t*)(sc + at) = x;
       }
     }
   }
@@ -166,16 +175,17 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
     for (int h = 0; h < 2; ++h) woff[j][h] = j < ntile ? j * tile_bytes + 1024u * h + 16u * lane : OOB8;
   const int aswz = r16 * 128 + ((g ^ r16) & 7) * 16;
 
+  const int step8 = tile0 % 8 + ntile > 8 ? 1 : 0;     // tiles from the next multiple of 8 on have the second row of scales
   const uint8_t* srow[MT];                             // this lane's rows' scales
 #pragma unroll
   for (int t = 0; t < MT; ++t) srow[t] = sc + min(16 * t + r16, mrows - 1) * ke;
 
-  // block number i of this wave is block KW i + wave of K; past the last the
+  // block number i of this wave is block KW i + wave of the K range; past the last the
   // buffers are empty: zeros, nothing read
   u32x4 wf[D][NT][2];
   auto load = [&]<int S>(int i) {
-    const int b = KW * i + wave;
-    const bool ok = b < kb;
+    const int b = s_lo + KW * i + wave;
+    const bool ok = b < s_hi;
     const __amdgpu_buffer_rsrc_t ar = rsrc8(Ap, ok ? (uint32_t)mrows * K8 : 0u);
     const __amdgpu_buffer_rsrc_t wr = rsrc8(Wp, ok ? ntile * tile_bytes : 0u);
 #pragma unroll
@@ -195,8 +205,8 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
     wait_loads<(D - 1) * PS>();
     asm volatile("" ::: "memory");
     const uint8_t* st = own + S * STAGE;
-    const int b = min(KW * i + wave, kb - 1);           // (past the last block: its products are zero)
-    const int we = wsc[b];
+    const int b = min(s_lo + KW * i + wave, s_hi - 1);  // (past the last block: its products are zero)
+    const int we[2] = {wsc[b], wsc[(NT > 1 ? step8 * ke : 0) + b]};
     u32x4 c[MT][2];
     int e[MT];
 #pragma unroll
@@ -206,11 +216,12 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
       e[t] = srow[t][b];
     }
     Frag16 a[MT];
-    float f[MT];
+    float f[2][MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       a[t] = widen(c[t]);
-      f[t] = scale_of(e[t], we);
+#pragma unroll
+      for (int r = 0; r < (NT > 1 ? 2 : 1); ++r) f[r][t] = scale_of(e[t], we[r]);
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
@@ -220,13 +231,13 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
         f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[u], a[t].v[u], s, 0, 0, 0);
-        add_scaled(acc[j][t], s, f[t]);
+        add_scaled(acc[j][t], s, NT > 1 && tile0 % 8 + j >= 8 ? f[1][t] : f[0][t]);
       }
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  const int n = (kb - wave + KW - 1) / KW;             // this wave's blocks (none: kb < wave)
+  const int n = (s_hi - s_lo - wave + KW - 1) / KW;    // this wave's blocks (maybe none)
   [&]<int... S>(std::integer_sequence<int, S...>) {
     (load.template operator()<S>(S), ...);
   }(std::make_integer_sequence<int, D - 1>());
@@ -260,22 +271,21 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
     for (int i = 0; i < MT; ++i) {
       const int m = 16 * i + r16;
       if ((j / TPU * MT + i) % KW != wave || j >= ntile || m >= mrows) continue;
-      const size_t row = m0 + m;
+      const size_t row = m;
       if constexpr (EPI == EPI8_SWIGLU) {
         const f32x4 gt = total(j, i), up = total(j + 1, i);
         f32x4 h;
 #pragma unroll
         for (int v = 0; v < 4; ++v) h[v] = silu8(gt[v]) * up[v];
         *(f32x4*)((float*)p.out + row * (p.N / 2) + 8 * (tile0 + j) + 4 * g) = h;
+      } else if constexpr (EPI == EPI8_PART) {
+        const int n = 16 * (tile0 + j) + 4 * g;         // ldo is N rounded up to 4
+        if (n < p.N) *(f32x4*)((float*)p.out + ((size_t)split * p.M + row) * p.ldo + n) = total(j, i);
       } else {
         store_out(p, row, 16 * (tile0 + j) + 4 * g, total(j, i));
       }
     }
 }
-
-// K ranges: ksplit of them, whole groups of four blocks (which share a load of
-// scales), none empty if the launch has checked range8(kb, ksplit) (ksplit - 1) < kb
-__host__ __device__ __forceinline__ int range8(int kb, int ksplit) { return ((kb + ksplit - 1) / ksplit + 3) & ~3; }
 
 // Row-tiled product for more rows: a workgroup of WM x WN waves owns BM rows x
 // BN columns, wave (wm, wn) 16 MF rows x 16 NF columns of them.  K advances one
@@ -540,28 +550,68 @@ template <typename C, int EPI> static hipError_t gemm8_rows_t(const Gemm8Params&
   return hipGetLastError();
 }
 
-template <int MT, int NT, int KW, int D, int EPI> static hipError_t gemm8_t(const Gemm8Params& p, hipStream_t s) {
-  const size_t gx = ((p.N + 15) / 16 + NT - 1) / NT, gz = (p.M + 16 * MT - 1) / (16 * MT);
-  if (gx * gz > 0x7fffffff) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((gemm8_kernel<MT, NT, KW, D, EPI>), dim3((uint32_t)(gx * gz)), dim3(64 * KW), 0, s, p);
+static bool ranges8_ok(int kb, int ksplit) { return range8(kb, ksplit) * (ksplit - 1) < kb; }
+
+// grid: workgroups of a K range, if the tiles are enough for them and fit them
+template <int MT, int NT, int D, int EPI> static hipError_t gemm8_t(const Gemm8Params& p, int grid, hipStream_t s) {
+  constexpr int TPU = EPI == EPI8_SWIGLU ? 2 : 1;
+  const int units = (p.N + 15) / 16 / TPU;
+  const int gx = std::min(units, std::max(grid, (units + NT / TPU - 1) / (NT / TPU)));
+  hipLaunchKernelGGL((gemm8_kernel<MT, NT, 4, D, EPI>), dim3((uint32_t)gx * p.ksplit), dim3(256), 0, s, p);
   return hipGetLastError();
 }
-// One 16-column tile a workgroup while that is one round of the 256 CUs, two
-// beyond (568 measured calls of 1 to 64 rows: on average 2.5 % slower than the
-// fastest of twelve tile, wave and depth choices; one tile for all 11 %, two for
-// all 12 %).  SwiGLU takes gate and up tiles in pairs.
-template <int MT, int EPI> static hipError_t gemm8_n(const Gemm8Params& p, hipStream_t s) {
-  if constexpr (EPI == EPI8_STORE) {
-    if ((p.N + 15) / 16 <= 256) return gemm8_t<MT, 1, 4, 3, EPI>(p, s);
+
+// Tiles of a workgroup, and K ranges, of a product of up to 64 rows.  What
+// differs is how often the rows are read from L2 (once per workgroup, which from
+// 30 rows on takes as long as the weights) against how many workgroups there are:
+//   * up to 256 tiles one a workgroup, until the rows' share grows (steps: K / 512
+//     times row tiles): from 20 steps on up to 64 tiles, whose grid leaves most
+//     CUs idle, K in four ranges; from 40 on two tiles a workgroup and K in two
+//     ranges, up to 128 tiles four (4096 x 11008: 16 rows 11.6 us with one tile
+//     and 12.8 so, 40 rows 17.1 and 16.0; 512 x 11008, 64 rows: 18.1 -> 10.5);
+//   * beyond, two tiles a workgroup, four from 1000 tiles and 17 rows on (16384
+//     x 8192, 64 rows: 34.9 -> 31.7).
+// Over 448 measured calls (1 to 64 rows) on average 2 % slower than the fastest
+// of fifteen choices; one tile up to 256, two beyond: 6 %.
+static Gemm8Plan plan_stream8(int M, int N, int K, int most) {
+  const int tiles = (N + 15) / 16, kb = blocks8(K), steps4 = kb * ((M + 15) / 16);   // four times the steps
+  Gemm8Plan r{false, tiles <= 256 ? 1 : tiles >= 1000 && M > 16 ? 4 : 2, 1};
+  if (tiles <= 64 && steps4 >= 4 * 20) {
+    r.ksplit = 4;
+  } else if (tiles <= 256 && steps4 >= 4 * 40) {
+    r.tile = 2;
+    r.ksplit = tiles <= 128 ? 4 : 2;
   }
-  return gemm8_t<MT, 2, 4, 2, EPI>(p, s);
+  r.ksplit = std::min(r.ksplit, most);
+  while (r.ksplit > 1 && !ranges8_ok(kb, r.ksplit)) r.ksplit /= 2;
+  return r;
 }
-template <int EPI> static hipError_t gemm8_m(const Gemm8Params& p, hipStream_t s) {
+
+template <int MT, int EPI> static hipError_t gemm8_n(int nt, const Gemm8Params& p, hipStream_t s) {
+  if constexpr (EPI == EPI8_SWIGLU) {
+    // one workgroup per CU and round, which holds all the tiles it is dealt (of 224
+    // measured calls 1 % slower than the fastest; two tiles throughout 3 %, 27 % at
+    // 27648 x 5120 and 64 rows)
+    const int per_cu = (p.N / 16 + 255) / 256;
+    if (per_cu <= 2) return gemm8_t<MT, 2, 2, EPI>(p, 256, s);
+    if (per_cu <= 4) return gemm8_t<MT, 4, 2, EPI>(p, 256, s);
+    if (per_cu <= 6) return gemm8_t<MT, 6, 2, EPI>(p, 256, s);
+    return gemm8_t<MT, 8, 2, EPI>(p, 256, s);
+  } else {
+    if (nt == 1) return gemm8_t<MT, 1, 3, EPI>(p, 0, s);
+    if (nt == 2) return gemm8_t<MT, 2, 2, EPI>(p, 0, s);
+    if constexpr (EPI == EPI8_STORE) {
+      if (nt == 4) return gemm8_t<MT, 4, 2, EPI>(p, 0, s);
+    }
+    return hipErrorInvalidValue;
+  }
+}
+template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipStream_t s) {
   switch ((p.M + 15) / 16) {
-    case 1: return gemm8_n<1, EPI>(p, s);
-    case 2: return gemm8_n<2, EPI>(p, s);
-    case 3: return gemm8_n<3, EPI>(p, s);
-    case 4: return gemm8_n<4, EPI>(p, s);
+    case 1: return gemm8_n<1, EPI>(nt, p, s);
+    case 2: return gemm8_n<2, EPI>(nt, p, s);
+    case 3: return gemm8_n<3, EPI>(nt, p, s);
+    case 4: return gemm8_n<4, EPI>(nt, p, s);
     default: return hipErrorInvalidValue;
   }
 }
@@ -603,8 +653,6 @@ constexpr int TILES8_FAST = 0, TILES8_EXACT = 4, TILES8_GATE_UP = 7, TILES8_END 
 template <int T>
 using Tile8At = Tile8<TILES8[T].mf, TILES8[T].nf, TILES8[T].wm, TILES8[T].wn, TILES8[T].nb, TILES8[T].exact>;
 
-static bool ranges8_ok(int kb, int ksplit) { return range8(kb, ksplit) * (ksplit - 1) < kb; }
-
 static Gemm8Plan pick_tile8(int lo, int hi, int M, int N, int K, int max_ksplit) {
   const int kb = blocks8(K);
   Gemm8Plan best{true, lo, 1};
@@ -632,9 +680,9 @@ static Gemm8Plan pick_tile8(int lo, int hi, int M, int N, int K, int max_ksplit)
 static bool streams8(int M, int K) { return M <= 64 && ke8(K) <= STREAM8_KE; }
 bool gate_up8_fused(int M, int K) { return !streams8(M, K); }
 Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap) {
-  if (streams8(M, K)) return Gemm8Plan{false, 0, 1};
   const size_t one = (size_t)M * part8_ld(N);
   const int most = part_cap >= 4 * one ? 4 : part_cap >= 2 * one ? 2 : 1;
+  if (streams8(M, K)) return plan_stream8(M, N, K, most);
   return exact ? pick_tile8(TILES8_EXACT, TILES8_GATE_UP, M, N, K, most) : pick_tile8(TILES8_FAST, TILES8_EXACT, M, N, K, most);
 }
 
@@ -662,16 +710,20 @@ hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p0, h
     return gemm8_rows_at<EPI8_SWIGLU_Q, TILES8_GATE_UP, TILES8_END>(
         pick_tile8(TILES8_GATE_UP, TILES8_END, p.M, p.N, p.K, 1).tile, p, s);
   }
-  if (epi == EPI8_SWIGLU) return p.N % 32 || !streams8(p.M, p.K) ? hipErrorInvalidValue : gemm8_m<EPI8_SWIGLU>(p, s);
+  if (epi == EPI8_SWIGLU) return p.N % 32 || !streams8(p.M, p.K) ? hipErrorInvalidValue : gemm8_m<EPI8_SWIGLU>(0, p, s);
   if (epi != EPI8_STORE && epi != EPI8_PART) return hipErrorInvalidValue;
-  if (!plan.rows) return epi == EPI8_PART || !streams8(p.M, p.K) ? hipErrorInvalidValue : gemm8_m<EPI8_STORE>(p, s);
-  if (plan.ksplit == 1) return epi == EPI8_PART ? hipErrorInvalidValue : gemm8_rows_at<EPI8_STORE, 0, TILES8_GATE_UP>(plan.tile, p, s);
+  if (!plan.rows && !streams8(p.M, p.K)) return hipErrorInvalidValue;
+  if (plan.ksplit == 1) {
+    if (epi == EPI8_PART) return hipErrorInvalidValue;
+    return plan.rows ? gemm8_rows_at<EPI8_STORE, 0, TILES8_GATE_UP>(plan.tile, p, s) : gemm8_m<EPI8_STORE>(plan.tile, p, s);
+  }
   if (!p.part || plan.ksplit < 1 || !ranges8_ok(blocks8(p.K), plan.ksplit)) return hipErrorInvalidValue;
   p.ksplit = plan.ksplit;
   Gemm8Params q = p;
   q.out = p.part;
   q.ldo = part8_ld(p.N);
-  const hipError_t r = gemm8_rows_at<EPI8_PART, 0, TILES8_GATE_UP>(plan.tile, q, s);
+  const hipError_t r = plan.rows ? gemm8_rows_at<EPI8_PART, 0, TILES8_GATE_UP>(plan.tile, q, s)
+                                 : gemm8_m<EPI8_PART>(plan.tile, q, s);
   if (r != hipSuccess || epi == EPI8_PART) return r;
   const size_t blocks = ((size_t)p.M * (q.ldo / 4) + 255) / 256;
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
