@@ -316,11 +316,13 @@ int sd_force_draft(sd_ctx *ctx, int B, const int32_t *slots, int gamma, int i,
  * block.  E is the smallest E >= 1 with amax <= 448 2^(E - 127), amax the
  * largest magnitude of the block's finite entries; a code is the value times
  * 2^(127 - E) rounded to nearest even.  NaN and infinities become the code of
- * NaN (which makes NaN of every sum it enters).
+ * NaN (which makes NaN of every sum it enters; so does E = 255, which is
+ * never written).
  *   Rows (activations)  [M, K]: codes uint8 [M, K8], K8 = K rounded up to a
  *     multiple of 128, entries past K zero; exponents uint8 [M, Ke], one per
  *     128 entries, Ke = K8 / 128 rounded up to a multiple of 4, padding 0.
- *     Codes start on 16 bytes, exponents on 4.  A buffer written here can be read as it is.
+ *     Codes start on 16 bytes, exponents on 4.  Rows behind the last are
+ *     neither read nor written.
  *   Weights [N, K] (y = x W^T), one scale per 128 x 128 block, packed by
  *     sd_pack_linear_q: 2 KB tiles of 16 rows x 128 columns, row tiles major;
  *     inside a tile 16-byte unit 64 h + 16 g + r holds row r, columns 64 h +
@@ -340,14 +342,19 @@ int sd_pack_linear_q(const void *src, void *dst, int N, int K, int dtype, void *
  * entries (q, exps).  x [M, d] and add [n_add, M, d] (0 <= n_add <= 6) are of
  * dtype; with n_add > 0, s is written to x_out [M, d] in that type and the norm
  * is of the value written; x_out may be x (else it must not overlap an
- * input).  gain [d] is of gain_dtype.  Sums and the norm are taken in 64 bits, y is rounded to fp32 and
- * then to its code.  d <= 16384, eps > 0. */
+ * input).  gain [d] is of gain_dtype.  Sums and the norm are taken in 64 bits, y
+ * is rounded to fp32 and then to its code.  d <= 16384, eps > 0. */
 int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const void *add, void *x_out,
                     const void *gain, int gain_dtype, float eps, uint8_t *q, uint8_t *exps, void *stream);
 
 /* out = [add +] rows W^T: rows (q, exps) [M, K], w a packed [N, K].  out
  * [M, N] of dtype with row stride ldo >= N (entries); add NULL or fp32 with
  * the same stride; with dtype fp32 it may be out itself (else no overlap).
+ * Sums are in fp32.  The products of up to 64 rows, and those of fp32 outputs,
+ * run on fp16 operands (the codes' values, exactly), with the product of two
+ * blocks' scales held within 2^-126 to 2^127 (below it counts as 0); bf16
+ * outputs of more rows run on the 8-bit matrix instruction, which drops low
+ * bits of the products it adds (up to 5e-5 of the outputs' root mean square).
  * The workspace (16-byte aligned, sd_linear_q_workspace_bytes(M, N, K); where
  * that is 0, as on an invalid size, it may be NULL) is scratch of this call
  * alone until its work is done: calls that may overlap, graphs among them, need
@@ -360,6 +367,7 @@ int sd_linear_q(int M, int N, int K, const uint8_t *q, const uint8_t *exps, cons
  * with gate and up rows interleaved in blocks of 16 (see wgu of sd_weights), h
  * = silu(gate) * up is written as rows of F entries (q_out, exps_out), the
  * input of a down projection with K = F.  F a multiple of 16, at most 2^18.
+ * Above 64 rows, or K = 16384, on the 8-bit matrix instruction.
  * Workspace as for sd_linear_q, of sd_gate_up_q_workspace_bytes(M, F, K). */
 size_t sd_gate_up_q_workspace_bytes(int M, int F, int K);
 int sd_gate_up_q(int M, int F, int K, const uint8_t *q, const uint8_t *exps, const void *w, uint8_t *q_out,

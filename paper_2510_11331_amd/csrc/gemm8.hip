@@ -79,9 +79,12 @@ template <int N> __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
-// acc += s 2^(E + F - 254) for two scale exponents: powers from 2^-126 to 2^127
-// (a smaller one counts as zero: the products it would scale are below 2^-101)
-__device__ __forceinline__ float scale_of(int E, int F) { return __uint_as_float((uint32_t)min(max(E + F - 127, 0), 254) << 23); }
+// 2^(E + F - 254) of two scale exponents, as a float: from 2^-126 to 2^127 (a
+// smaller one counts as zero: the sums that it would scale are below 2^-101; a
+// larger one as 2^127); 255, which no kernel here writes, is NaN
+__device__ __forceinline__ float scale_of(int E, int F) {
+  return __uint_as_float(max(E, F) == 255 ? 0x7fc00000u : (uint32_t)min(max(E + F - 127, 0), 254) << 23);
+}
 __device__ __forceinline__ void add_scaled(f32x4& acc, f32x4 s, float f) {
 #pragma unroll
   for (int v = 0; v < 4; ++v) acc[v] = fmaf(s[v], f, acc[v]);
@@ -501,9 +504,9 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
       const int E = block_exp(m);
       const float inv = inv_scale(E);
 #pragma unroll
-      for (int j = 0; j < NF; j += 2)
+      for (int j = 0; j < NF; j += 2)                  // (padding is zero in rows of NaN too)
         *(uint32_t*)(p.q_out + row * 128 * fb + 128 * bx + (wn * NF + j) * 8 + 4 * g) =
-            codes4(acc[i][j].x, acc[i][j].y, acc[i][j].z, acc[i][j].w, inv);
+            wn * NF + j < ntile ? codes4(acc[i][j].x, acc[i][j].y, acc[i][j].z, acc[i][j].w, inv) : 0u;
       if (wn == 0 && g == 0) p.exps_out[row * fe + bx] = (uint8_t)E;
       if (bx == fb - 1 && wn == 1 && g < fe - fb) p.exps_out[row * fe + fb + g] = 0;   // padding (at most 3)
     }

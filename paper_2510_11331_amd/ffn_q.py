@@ -12,7 +12,9 @@ feed-forward pass on a residual stream x is
 
 Every call enqueues on `stream` (default: the current stream of the tensors'
 device) and returns new tensors unless it is given some to write to.  Arguments
-that the kernels do not cover raise ValueError before anything is enqueued.
+that the kernels do not cover raise ValueError, or SDError where only the
+library sees it (sizes past its limits, addresses off their alignment, eps <= 0),
+before anything is enqueued.
 """
 from __future__ import annotations
 
@@ -120,7 +122,7 @@ def add_rmsnorm_q(x: torch.Tensor, gain: torch.Tensor, eps: float, add: Optional
                   ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(s, q, exps) with s = x + add and q, exps the rows of s / sqrt(mean(s^2) + eps) * gain.  x [M, d] is bfloat16 or
     float32; add of its type [M, d], or [n, M, d] (n <= 6, all of them are added), or None (s is then x itself).  gain [d]
-    is bfloat16 or float32.  x_out: where s goes (may be x)."""
+    is bfloat16 or float32.  x_out: where s goes (x itself, or memory that overlaps no input)."""
     t, dev = x.dtype, x.device
     if x.dim() != 2 or t not in _DTYPES or not x.is_contiguous():
         raise ValueError("x: contiguous [M, d], bfloat16 or float32")
@@ -154,7 +156,7 @@ def add_rmsnorm_q(x: torch.Tensor, gain: torch.Tensor, eps: float, add: Optional
 
 
 def _rows(q: torch.Tensor, exps: torch.Tensor, w: LinearQ) -> int:
-    M, K = len(q), w.K
+    M, K = q.shape[0] if q.dim() else 0, w.K
     if q.dtype != _E4M3 or q.shape != (M, _k8(K)) or not q.is_contiguous():
         raise ValueError(f"q: contiguous float8_e4m3fn [M, {_k8(K)}]")
     if exps.dtype != _E8M0 or exps.shape != (M, _ke(K)) or not exps.is_contiguous():

@@ -439,3 +439,184 @@ def test_streams_and_graphs():
         eager = [layer(*a) for a in sets]
         torch.cuda.synchronize()
         assert all(torch.equal(x, w) for x, w in zip(outs + eager, want + want))
+
+
+# ------------------------------------------------------------------ ranges, tiles, borders
+
+
+# few rows: K in 4 ranges with one tile a workgroup, 2 ranges, 4 and 2 ranges with two tiles, four tiles a workgroup whose
+# runs cross a block of 128 rows; more rows: each tile with 1, 2 and 4 ranges, for both types; K past the streamed scales
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(3, 500, 10300), (64, 1000, 2560), (64, 1500, 5200), (50, 3000, 5130), (20, 16130, 140), (64, 4200, 300),
+                                   (70, 300, 10000), (65, 300, 4200), (200, 2100, 8400), (200, 8200, 140), (769, 5000, 140), (65, 4100, 8400),
+                                   (769, 2100, 1500), (65, 8200, 8400), (3, 40, 16500), (64, 33, 40000)])
+def test_linear_ranges_and_tiles(M, N, K, dtype):
+    import torch
+    from paper_2510_11331_amd import linear_q
+    say("linear ranges", M, N, K, dtype)
+    r = np.random.default_rng([M, N, K])
+    c, E, q, e = rows8(r, M, K)
+    wc, wE, w = weight8(r, N, K)
+    a, b = torch.from_numpy(qref.row_values(c, E, K)), torch.from_numpy(qref.weight_values(wc, wE))
+    add = r.normal(size=(M, N)).astype(np.float32)
+    want, mag = (a @ b.T).numpy() + add, (a.abs() @ b.abs().T).numpy() + np.abs(add)
+    check_product(host(linear_q(q, e, w, add=t(add), dtype=dt(dtype))), want, mag, K, dtype)
+
+
+@pytest.mark.parametrize("M,F,K", [(3, 6000, 140), (20, 10000, 260), (33, 14000, 130), (64, 18000, 130), (64, 16400, 20), (3, 48, 16500), (65, 288, 140),
+                                   (2050, 992, 140), (769, 4992, 140), (769, 8192, 140)])
+def test_gate_up_tiles(M, F, K):
+    """Few rows: 4, 6 and 8 tiles a workgroup, more than one round of them; K past the streamed scales; every row tile."""
+    import torch
+    from paper_2510_11331_amd import gate_up_q
+    say("gate_up tiles", M, F, K)
+    r = np.random.default_rng([M, F, K])
+    c, E, q, e = rows8(r, M, K, 0.5)
+    wc, wE, w = weight8(r, 2 * F, K)
+    a, b = torch.from_numpy(qref.row_values(c, E, K)), torch.from_numpy(qref.weight_values(wc, wE))
+    mag = (a.abs() @ b.abs().T).numpy()
+    tol = sum_error(K, mag) + (CUT8 * mag if M > 64 or K > 16384 else 0)
+    p = (a @ b.T).numpy()
+    check_codes_of(*gate_up_q(q, e, w), qref.swiglu(p), swiglu_error(p, tol))
+
+
+@pytest.mark.parametrize("M", [5, 40, 300])
+def test_only_its_own_memory(M):
+    """Every buffer ends in bytes that no call may touch: codes, exponents, outputs, workspaces, x_out; rows of the input
+    behind the last are not read (NaN codes)."""
+    import torch
+    from paper_2510_11331_amd import _lib
+    say("own memory", M)
+    L, F32 = _lib.lib(), _lib.SD_DTYPE_F32
+    r = np.random.default_rng(M)
+    d, F = 700, 10320
+    s = torch.cuda.current_stream().cuda_stream
+    made = []
+
+    def buf(n, fill=0x7f):
+        b = torch.full((n + 512,), fill, dtype=torch.uint8, device="cuda")
+        made.append((b, n, fill))
+        return b
+
+    x, add, gain = (t(r.normal(size=k).astype(np.float32)) for k in ((M, d), (2, M, d), (d,)))
+    w1, w2 = (t((0.02 * r.normal(size=k)).astype(np.float32)) for k in ((2 * F, d), (d, F)))
+    p1, p2 = buf(L.sd_linear_q_bytes(2 * F, d)), buf(L.sd_linear_q_bytes(d, F))
+    xo, q, e, h, eh, out = buf(M * d * 4), buf(M * 768), buf(M * 8), buf(M * 10368), buf(M * 84), buf(M * d * 4)
+    n1, n2 = L.sd_gate_up_q_workspace_bytes(M, F, d), L.sd_linear_q_workspace_bytes(M, d, F)
+    assert n2 or M == 300
+    ws1, ws2 = buf(n1), buf(n2)
+    P = lambda b: b.data_ptr()
+    assert L.sd_pack_linear_q(P(w1), P(p1), 2 * F, d, F32, s) == L.sd_pack_linear_q(P(w2), P(p2), d, F, F32, s) == 0
+    assert L.sd_add_rmsnorm_q(M, d, F32, P(x), 2, P(add), P(xo), P(gain), F32, 1e-5, P(q), P(e), s) == 0
+    assert L.sd_gate_up_q(M, F, d, P(q), P(e), P(p1), P(h), P(eh), P(ws1), n1, s) == 0
+    assert L.sd_linear_q(M, d, F, P(h), P(eh), P(p2), P(xo), P(out), d, F32, P(ws2), n2, s) == 0
+    torch.cuda.synchronize()
+    assert all(bool((b[n:] == fill).all()) for b, n, fill in made)
+    y = out[:M * d * 4].view(torch.float32)
+    assert bool(torch.isfinite(y).all())
+
+
+@pytest.mark.parametrize("M", [3, 100])
+def test_scale_of_nan(M):
+    """E = 255 of a row's block or of a weight's block makes NaN of the sums that it enters and of no others."""
+    import torch
+    from paper_2510_11331_amd import LinearQ, linear_q
+    say("nan scale", M)
+    r = np.random.default_rng(13)
+    N, K = 300, 700
+    c, E, q, _ = rows8(r, M, K)
+    wc, wE, w = weight8(r, N, K)
+    E, wE2 = E.copy(), wE.copy()
+    E[1, 2] = 255
+    wE2[1, 3] = 255
+    e, w2 = t(qref.exps_bytes(E)).view(torch.float8_e8m0fnu), LinearQ(t(qref.pack(wc, wE2)), N, K)
+    for dtype in ("fp32", "bf16"):
+        nan = np.isnan(host(linear_q(q, e, w, dtype=dt(dtype))))
+        assert nan[1].all() and nan.sum() == N
+        nan = np.isnan(host(linear_q(q, e, w2, dtype=dt(dtype))))
+        assert nan[1].all() and nan[:, 128:256].all() and nan.sum() == N + 128 * (M - 1)
+
+
+@pytest.mark.parametrize("M", [3, 100])
+def test_gate_up_nan_row(M):
+    """A row of NaN: F codes of NaN, padding zero; the other rows as without it."""
+    import torch
+    from paper_2510_11331_amd import gate_up_q
+    say("gate_up nan row", M)
+    r = np.random.default_rng(14)
+    F, K = 272, 300
+    c, E, q, e = rows8(r, M, K, 0.5)
+    _, _, w = weight8(r, 2 * F, K)
+    want = [host(a) for a in gate_up_q(q, e, w)]
+    c = c.copy()
+    c[1, 299] = 0x7f
+    got = [host(a) for a in gate_up_q(t(c).view(torch.float8_e4m3fn), e, w)]
+    assert (got[0][1, :F] & 127 == 127).all() and not got[0][1, F:].any()
+    rest = [i for i in range(M) if i != 1]
+    assert all(np.array_equal(g[rest], v[rest]) for g, v in zip(got, want))
+
+
+def test_packed_past_32_bits():
+    """A packed matrix of more than 2^32 bytes: tiles of its start, middle and end, and a product with it."""
+    import torch
+    from paper_2510_11331_amd import linear_q, pack_linear_q
+    say("pack large")
+    N, K, n = 65600, 66000, 1312                              # rows and columns repeat: N = 50 n, K = 500 x 132
+    r = np.random.default_rng(15)
+    small = t((0.02 * r.normal(size=(n, 132))).astype(np.float32), torch.bfloat16)
+    w = pack_linear_q(small.repeat(50, 500))
+    assert w.codes.numel() > 1 << 32
+    kb = 516
+    tiles = w.codes.view(torch.uint8).view(N // 16, kb, 2048)
+    full = small.double().cpu().numpy()
+    for row0 in (0, 32768, 65536 - 128):
+        block = np.take(np.tile(full, (1, 10)), np.arange(row0, row0 + 128) % n, axis=0)
+        for b in (0, 258, 514):
+            cols = np.take(block, np.arange(128 * b, 128 * b + 128) % 132, axis=1)
+            data = qref.pack(*qref.quantise_weight(cols))
+            assert np.array_equal(tiles[row0 // 16:row0 // 16 + 8, b].reshape(-1).cpu().numpy(), data[:128 * 128])
+            assert int(host(w.exps)[row0 // 128, b]) == data[128 * 128]
+    K2 = 66000                                                # rows that pick one column each, of every eighth part of K
+    pick = np.zeros((8, K2))
+    at = [8250 * i + 7 * i for i in range(8)]
+    pick[np.arange(8), at] = 1.0
+    c, E = qref.quantise_rows(pick)
+    got = host(linear_q(t(c).view(torch.float8_e4m3fn), t(qref.exps_bytes(E)).view(torch.float8_e8m0fnu), w))
+    for i, k in enumerate(at):
+        for row0 in (0, 32768, 65536 - 128):
+            rows, cols = np.arange(row0, row0 + 128) % n, np.arange(k // 128 * 128, k // 128 * 128 + 128) % 132
+            block = full[np.ix_(rows, cols)]
+            v = qref.weight_values(*qref.quantise_weight(block))[:, k % 128]
+            assert np.allclose(got[i, row0:row0 + 128], v, rtol=4 * U32, atol=0)
+
+
+def test_ranges_in_graphs():
+    """Products with K ranges, captured twice (each with the workspace of its capture), replayed at once on two streams
+    between eager ones: bit for bit the eager results."""
+    import torch
+    from paper_2510_11331_amd import linear_q
+    say("ranges in graphs")
+    r = np.random.default_rng(16)
+    sets = []
+    for M, N, K in ((40, 700, 10300), (70, 300, 10000)):
+        _, _, q, e = rows8(r, M, K)
+        sets.append((q, e, weight8(r, N, K)[2]))
+    want = [linear_q(*a) for a in sets]
+    torch.cuda.synchronize()
+    st, graphs, outs = [torch.cuda.Stream(), torch.cuda.Stream()], [], []
+    for a in sets:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(linear_q(*a))
+        graphs.append(g)
+    for _ in range(4):
+        for o in outs:
+            o.zero_()
+        for s in st:
+            s.wait_stream(torch.cuda.current_stream())
+        for g, s in zip(graphs, st):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = [linear_q(*a) for a in sets]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs + eager, want + want))
