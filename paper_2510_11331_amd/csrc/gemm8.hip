@@ -414,6 +414,8 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
     if (st == 0) load_scales(s_lo / 4);
     gload(s_lo + st, 0, 1);
   }
+  f32x4 last[C::EXACT ? NF : 1] = {};                  // sums not added yet, and their scale
+  float flast = 0.f;
   for (int st = s_lo; st < s_hi; ++st) {
     wait_loads<(NB - 2) * (LA + LW)>();
     asm volatile("s_barrier" ::: "memory");
@@ -436,37 +438,67 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
         wf[j][h] = *(const u32x4*)(base + (FA / 2 + wn * NF + j) * 2048 + 1024 * h + lane * 16);
     read_a(0);
     __builtin_amdgcn_sched_barrier(0);
-    Frag16 w16[C::EXACT ? NF : 1];
-    if constexpr (C::EXACT) {
-#pragma unroll
-      for (int j = 0; j < NF; ++j) w16[j] = widen(wf[j]);
-    }
     // the loads of stage st + NB - 1 go out between the rows' products: issued
     // together they would hold up every wave behind the address unit
+    if constexpr (!C::EXACT) {
 #pragma unroll
-    for (int i = 0; i < MF; ++i) {
-      if (i + 1 < MF) read_a(i + 1);
-      gload(st + NB - 1, i, MF);
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (!C::EXACT) {
+      for (int i = 0; i < MF; ++i) {
+        if (i + 1 < MF) read_a(i + 1);
+        gload(st + NB - 1, i, MF);
+        __builtin_amdgcn_sched_barrier(0);
         const i32x8 a = __builtin_bit_cast(i32x8, Pair16{af[i & 1][0], af[i & 1][1]});
 #pragma unroll
         for (int j = 0; j < NF; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
               __builtin_bit_cast(i32x8, Pair16{wf[j][0], wf[j][1]}), a, acc[i][j], 0, 0, 0, we, 0, ae[i & 1]);
-      } else {
-        const Frag16 a = widen(af[i & 1]);
-        const float f = scale_of(ae[i & 1] & 255, we & 255);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      // while a row tile's products run, the next is widened and the sums of the
+      // one before (the last stage's last, first) are scaled and added (2048 x
+      // 4096 x 4096: 71.5 -> 67.6 us against doing the three in turn)
+      Frag16 w16[NF], a[2];
+      float f[2];
+      a[0] = widen(af[0]);
+      f[0] = scale_of(ae[0] & 255, we & 255);
+      if (MF > 1) read_a(1);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        if (i + 2 < MF) read_a(i + 2);
+        gload(st + NB - 1, i, MF);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sum[NF];
 #pragma unroll
         for (int j = 0; j < NF; ++j) {
-          f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (i == 0) w16[j] = widen(wf[j]);
+          sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_16x16x32_f16(w16[j].v[u], a.v[u], s, 0, 0, 0);
-          add_scaled(acc[i][j], s, f);
+          for (int u = 0; u < 4; ++u) sum[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w16[j].v[u], a[i & 1].v[u], sum[j], 0, 0, 0);
         }
+        if (i + 1 < MF) {
+          a[(i + 1) & 1] = widen(af[(i + 1) & 1]);
+          f[(i + 1) & 1] = scale_of(ae[(i + 1) & 1] & 255, we & 255);
+        }
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+          add_scaled(acc[(i + MF - 1) % MF][j], last[j], flast);
+          last[j] = sum[j];
+        }
+        flast = f[i & 1];
+        if (i > 0) {
+#pragma unroll
+          for (int k = 0; k < 4 * NF; ++k) {
+            __builtin_amdgcn_sched_group_barrier(8, 1, 0);                       // a product, then
+            __builtin_amdgcn_sched_group_barrier(2, (20 + 4 * NF) / (4 * NF), 0);  // vector instructions
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
+  }
+  if constexpr (C::EXACT) {
+#pragma unroll
+    for (int j = 0; j < NF; ++j) add_scaled(acc[MF - 1][j], last[j], flast);
   }
   wait_loads<0>();                                    // the trailing empty loads
 
@@ -626,7 +658,7 @@ template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipSt
 // sums them.  Fitted to 65 to 2048 rows, N of 512 to 11008 and K of 1024 to 11008
 // (weights from HBM); against the fastest of nine to twelve tiles and of 1, 2
 // and 4 K ranges the choice is on average 2.4 % slower for bf16 outputs (304
-// shapes, the worst 31 %), 3.7 % for fp32 ones (the worst 27 %) and 0.1 % for
+// shapes, the worst 31 %), 2.9 % for fp32 ones (the worst 28 %) and 0.1 % for
 // gate/up (225 shapes, the worst 6 %).  One K range for all would cost 6 % and 14 %.
 struct Tile8Model {
   int mf, nf, wm, wn, nb;   // Tile8
@@ -643,8 +675,8 @@ static constexpr Tile8Model TILES8[] = {
     {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.084f},    // 128 x 64
     {2, 2, 2, 2, 4, false, 2, 3.0f, 0.230f, 0.135f},    // 64 x 64
     // fp32 outputs, on fp16 operands
-    {4, 4, 2, 4, 3, true, 1, 7.5f, 1.563f, 0.358f},     // 128 x 256
-    {2, 2, 2, 4, 3, true, 2, 4.4f, 0.587f, 0.300f},     // 64 x 128
+    {4, 4, 2, 4, 3, true, 1, 7.5f, 1.454f, 0.322f},     // 128 x 256
+    {2, 2, 2, 4, 3, true, 2, 4.4f, 0.610f, 0.312f},     // 64 x 128
     {2, 2, 2, 2, 4, true, 2, 3.4f, 0.469f, 0.140f},     // 64 x 64
     // gate/up: 256 columns, the block of 128 outputs
     {4, 4, 4, 4, 2, false, 1, 12.7f, 1.391f, 0.532f},   // 256 x 256
