@@ -98,7 +98,8 @@ enum { SD_DTYPE_BF16 = 0, SD_DTYPE_F32 = 1, SD_DTYPE_BF16_FFN_Q = 2 };
  * point (sd_add_rmsnorm_q, sd_gate_up_q, sd_linear_q below): wgu and wdown are
  * packed by sd_pack_linear_q, and the inputs of both products are rounded to
  * 8-bit rows.  Half the weight bytes of two thirds of the layer; each code is
- * within 2^-4 of its value. */
+ * within 2^-4 of its value.  d_model <= 16384; passes of more than 64 rows run
+ * both products on the 8-bit matrix instruction. */
 typedef struct {
     int n_layers, d_model, n_heads, n_kv_heads, head_dim, d_ffn, vocab;
     int dtype;              /* SD_DTYPE_*                                   */

@@ -67,8 +67,9 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* row, i
 // us at 2048).  Bound by memory: 2048 x 8192 fp32 with two addends 59 us, 4.8
 // TB/s of the 5.2 that a copy reaches; 2048 x 5120 bf16 with one 20.0 us; 40 x
 // 4096 fp32 with four 5.2 us and one row 3.3 us, a launch and three memory round
-// trips.  Sixteen bytes a load (eight before: 24.2 us at 2048 x 5120).  All addends are loaded before the first is added (NS of them,
-// those past n_add as zeros).
+// trips.  Sixteen bytes a load (eight before: 24.2 us at 2048 x 5120).  All
+// addends are loaded before the first is added (NS of them, those past n_add as
+// zeros).
 template <typename TX, typename TG, int R, int NS, bool VEC>
 __global__ __launch_bounds__(R == 1 ? 256 : 512, 4) void add_rmsnorm8_kernel(Norm8Params p) {
   __shared__ double red[8];

@@ -24,6 +24,7 @@ namespace {
 
 constexpr int KV_BLOCK = 16;
 constexpr int MAX_KSPLIT = 6;   // K splits of a residual projection (partial sums in the workspace)
+static_assert(MAX_KSPLIT <= NORM8_MAX_ADD, "the 8-bit norm adds them");
 constexpr int SKINNY_MAX_KSPLIT = 4;   // of those on the skinny GEMM
 
 struct ModelRT {
@@ -131,6 +132,7 @@ bool model_ok(const sd_model_cfg& m) {
   if ((m.d_model * e) % GEMM_CHUNK || (m.d_ffn * e) % GEMM_CHUNK) return false;
   if (m.vocab % 16 || m.d_ffn % 16 || m.vocab > 32768) return false;   // row kernels hold <= 32768 entries
   if (!(m.rope_theta > 0.f) || !(m.rms_eps > 0.f)) return false;
+  if (m.dtype == SD_DTYPE_BF16_FFN_Q && (m.d_model > NORM8_MAX_D || m.d_ffn > LINEAR8_MAX_K)) return false;
   return true;
 }
 

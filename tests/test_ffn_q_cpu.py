@@ -154,5 +154,9 @@ def test_model_dtype():
     assert plan(_lib.SD_PROJ_GATEUP) == plan(_lib.SD_PROJ_DOWN) == _lib.SD_EINVAL
     c.target.dtype = 3
     assert L.sd_workspace_bytes(C.byref(c)) == 0
+    c.target = model_cfg(synth.ModelShape(1, 16384, 128, 128, 16384, t.vocab, "bf16"), ffn_q=True)
+    assert L.sd_workspace_bytes(C.byref(c)) > 0
+    c.target = model_cfg(synth.ModelShape(1, 16512, 129, 129, 16384, t.vocab, "bf16"), ffn_q=True)    # rows past what the norm holds
+    assert L.sd_workspace_bytes(C.byref(c)) == 0
     with pytest.raises(ValueError):
         model_cfg(synth.MODELS["tiny_target"], ffn_q=True)

@@ -49,6 +49,7 @@ def engine(shape, draft, tw, dw, B, gamma, ctx, **kw):
 
 
 SHAPES = {"mha": synth.ModelShape(2, 256, 4, 4, 512, 1008, "bf16"), "odd": synth.ModelShape(2, 320, 5, 1, 448, 1008, "bf16")}
+LONG = synth.ModelShape(2, 256, 4, 4, 10304, 1008, "bf16")
 DRAFT = synth.ModelShape(1, 192, 3, 1, 320, 1008, "bf16")
 
 
@@ -60,7 +61,18 @@ def test_verify_logits(name, lens, gamma):
     their last place (2^-11): a share of 2^-11 / 2^-4 = 2^-7 of the codes, 2^-3 sqrt(2^-7) = 1.1 % of a feed-forward
     output, whose part of a logit is at most all of it; two layers, three sets of codes each: 3 % is under sqrt(6) times that."""
     say("ffn_q verify", name, lens)
-    shape = SHAPES[name]
+    check_verify(SHAPES[name], lens, gamma)
+
+
+@pytest.mark.parametrize("lens,gamma", [((37, 5), 3), ((130, 71, 9, 66, 20, 33, 8, 90, 3, 50, 64, 17, 25, 40), 4)])
+def test_verify_logits_ranges(lens, gamma):
+    """A feed-forward width whose down projection takes K in ranges (with 8 and 70 rows, and in prefill), which the next norm
+    adds: as above."""
+    say("ffn_q verify ranges", lens)
+    check_verify(LONG, lens, gamma)
+
+
+def check_verify(shape, lens, gamma):
     tw, dw = synth.model_weights(shape, 5), synth.model_weights(DRAFT, 6)
     prompts = synth.prompts(len(lens), list(lens), shape.vocab)
     model = FFNQ(shape, tw)
