@@ -328,15 +328,30 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
   const int kb = blocks8(p.K), ke = ke8(p.K), K8 = 128 * kb;
   const int tiles = (p.N + 15) / 16;
   const int gz = (p.M + BM - 1) / BM;
-  // workgroup w runs on XCD w % 8, which takes one contiguous run of tiles, the
-  // row tiles of a column tile first: its weights then come from HBM once
+  // Workgroup w runs on XCD w % 8, which takes one contiguous run of tiles in this
+  // order: groups of up to 8 row tiles (of even size); in a group its column tiles;
+  // of a column tile the row tiles of each K range.  The 32 workgroups that an XCD
+  // runs at a time then share about as many bytes of rows as of weights (8192 x
+  // 4096 x 11008, bf16 out: 333 us, 355 with all row tiles of a column tile first).
   int bx, bz, split;
   {
     const int w = blockIdx.x, T8 = gridDim.x >> 3, rem = gridDim.x & 7, x = w & 7;
-    const int tile = x * T8 + min(x, rem) + (w >> 3), r = tile % (gz * p.ksplit);
-    bx = tile / (gz * p.ksplit);
-    bz = r % gz;
-    split = r / gz;
+    const int gx = (tiles + BN / 16 - 1) / (BN / 16), col = gx * p.ksplit;
+    const int groups = (gz + 7) / 8, lo = gz / groups, more = gz % groups;   // the first `more` groups have lo + 1 rows
+    int tile = x * T8 + min(x, rem) + (w >> 3), rows = lo + 1, z0;
+    if (tile < more * rows * col) {
+      z0 = tile / (rows * col) * rows;
+      tile %= rows * col;
+    } else {
+      tile -= more * rows * col;
+      rows = lo;
+      z0 = more + tile / (rows * col) * rows + more * lo;
+      tile %= rows * col;
+    }
+    const int r = tile % (rows * p.ksplit);
+    bx = tile / (rows * p.ksplit);
+    bz = z0 + r % rows;
+    split = r / rows;
   }
   const int sps = range8(kb, p.ksplit), s_lo = split * sps, s_hi = min(s_lo + sps, kb);   // blocks of this K range
   const uint32_t tile_bytes = (uint32_t)kb * 2048u;
