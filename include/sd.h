@@ -311,6 +311,7 @@ int sd_force_draft(sd_ctx *ctx, int B, const int32_t *slots, int gamma, int i,
  * operands).  Context-free like sd_accept_resample: every call only enqueues
  * on the stream of the current device, keeps no state, and is safe to capture
  * and to call from several streams at once (with buffers of their own).
+ * Outputs and workspaces overlap nothing else, but where a call says so.
  *
  * Format.  Numbers are e4m3 codes (one sign, four exponent, three fraction
  * bits; largest 448) with a power-of-two scale 2^(E - 127), E a byte, per

@@ -307,10 +307,10 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
 // stage; those past the operands have an empty buffer range or an offset outside
 // it: zeros, nothing read.
 //
-// 2048 x 4096 x 11008, bf16 out: 82 us, 2.25 PFLOP/s of the 2.64 of a large
+// 2048 x 4096 x 11008, bf16 out: 81 us, 2.29 PFLOP/s of the 2.64 of a large
 // library product (in a graph of such calls 91, of which its loads alone would
 // take 78 and its LDS reads and products alone 80); gate/up 2048 x 22016 x 4096:
-// 202 us, 1.83 PFLOP/s.
+// 198 us, 1.87 PFLOP/s.
 template <int MF_, int NF_, int WM_, int WN_, int NB_, bool EXACT_> struct Tile8 {
   static constexpr int MF = MF_, NF = NF_, WM = WM_, WN = WN_, NB = NB_;
   static constexpr bool EXACT = EXACT_;
@@ -660,8 +660,10 @@ template <int MT, int EPI> static hipError_t gemm8_n(int nt, const Gemm8Params& 
     return gemm8_t<MT, 8, 2, EPI>(p, 256, s);
   } else {
     if (nt == 1) return gemm8_t<MT, 1, 3, EPI>(p, 0, s);
-    if (nt == 2) return gemm8_t<MT, 2, 2, EPI>(p, 0, s);
-    if constexpr (EPI == EPI8_STORE) {
+    if constexpr (EPI == EPI8_STORE || MT > 1) {         // (two tiles in K ranges: 17 rows and more, at K up to 16384)
+      if (nt == 2) return gemm8_t<MT, 2, 2, EPI>(p, 0, s);
+    }
+    if constexpr (EPI == EPI8_STORE && MT > 1) {
       if (nt == 4) return gemm8_t<MT, 4, 2, EPI>(p, 0, s);
     }
     return hipErrorInvalidValue;

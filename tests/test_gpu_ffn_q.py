@@ -449,7 +449,8 @@ def test_streams_and_graphs():
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("M,N,K", [(3, 500, 10300), (64, 1000, 2560), (64, 1500, 5200), (50, 3000, 5130), (20, 16130, 140), (64, 4200, 300),
                                    (70, 300, 10000), (65, 300, 4200), (200, 2100, 8400), (200, 8200, 140), (769, 5000, 140), (65, 4100, 8400),
-                                   (769, 2100, 1500), (65, 8200, 8400), (3, 40, 16500), (64, 33, 40000), (1200, 300, 700), (4000, 130, 2200)])
+                                   (769, 2100, 1500), (65, 8200, 8400), (3, 40, 16500), (64, 33, 40000), (1200, 300, 700), (4000, 130, 2200),
+                                   (65, 8200, 11000), (65, 12000, 6000), (4200, 130, 6000), (2100, 130, 8400), (2100, 520, 11000)])
 def test_linear_ranges_and_tiles(M, N, K, dtype):
     import torch
     from paper_2510_11331_amd import linear_q

@@ -1,5 +1,7 @@
 """Models whose feed-forward network runs in 8 bits (SD_DTYPE_BF16_FFN_Q), through the engine's prefill, draft and verify
 passes, against a float64 model with codes at the same places."""
+import functools
+
 import numpy as np
 import pytest
 
@@ -17,6 +19,7 @@ class FFNQ(om.Model):
     def codes(self, x):
         return qref.row_values(*qref.quantise_rows(x.astype(np.float32).astype(np.float64)), x.shape[1])
 
+    @functools.cached_property
     def quantised(self):
         s, w = self.s, dict(self.w)
         for l in range(s.n_layers):
@@ -28,7 +31,7 @@ class FFNQ(om.Model):
         return w
 
     def logits(self, toks, n):
-        s, w, q = self.s, self.ops, self.quantised()
+        s, w, q = self.s, self.ops, self.quantised
         pos = np.arange(len(toks))
         x = w["embed"][np.asarray(toks)]
         for l in range(s.n_layers):
