@@ -307,6 +307,13 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
 // stage; those past the operands have an empty buffer range or an offset outside
 // it: zeros, nothing read.
 //
+// With two buffers (tiles of 192 and 256 rows) the rows' loads of the next stage
+// go out in the first half of a stage; a second barrier in its middle, when every
+// wave has the stage's weights in registers, frees their part of the buffer for
+// the weights' loads of the stage after next.  All of them then have at least
+// half a stage to arrive (gate/up of 8192 rows, 256 x 256: 755 -> 695 us; 1024
+// rows 138 -> 121).
+//
 // 2048 x 4096 x 11008, bf16 out: 81 us, 2.29 PFLOP/s of the 2.64 of a large
 // library product (in a graph of such calls 91, of which its loads alone would
 // take 78 and its LDS reads and products alone 80); gate/up 2048 x 22016 x 4096:
@@ -328,7 +335,7 @@ template <int MF_, int NF_, int WM_, int WN_, int NB_, bool EXACT_> struct Tile8
 template <typename C, int EPI>
 __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel(Gemm8Params p) {
   constexpr int MF = C::MF, NF = C::NF, NB = C::NB, WAVES = C::WAVES, BM = C::BM, BN = C::BN;
-  constexpr int FA = C::FA, FW = C::FW, LA = C::LA, LW = C::LW, LE = C::LE;
+  constexpr int FA = C::FA, FW = C::FW, LA = C::LA, LW = C::LW, LE = C::LE, L = LA + LW;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[C::LDS];
   uint8_t* const lds = smem;
 
@@ -391,16 +398,15 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
     if (e < BM / 64) eoff[k] = m < mrows ? (uint32_t)m * ke : OOB8;
     else eoff[k] = e == BM / 64 && lane < nblk ? (uint32_t)lane * ke : OOB8;
   }
-  // part i of n of the loads of stage st
-  auto gload = [&](int st, int i, int n) {
+  // loads from .. to - 1 of stage st (the rows', then the weights')
+  auto gload = [&](int st, int from, int to) {
     const bool ok = st < s_hi;
     const __amdgpu_buffer_rsrc_t ar = rsrc8(Ap, ok ? (uint32_t)mrows * K8 : 0u);
     const __amdgpu_buffer_rsrc_t wr = rsrc8(Wp, ok ? (uint32_t)ntile * tile_bytes : 0u);
     uint8_t* base = lds + (st % NB) * C::STAGE;
-    constexpr int L = LA + LW;
 #pragma unroll
     for (int q = 0; q < L; ++q) {
-      if (q < L * i / n || q >= L * (i + 1) / n) continue;
+      if (q < from || q >= to) continue;
       if (q < LA) {
         const uint32_t off = aoff[q];
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -438,12 +444,13 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
 #pragma unroll
   for (int st = 0; st < NB - 1; ++st) {
     if (st == 0) load_scales(s_lo / 4);
-    gload(s_lo + st, 0, 1);
+    gload(s_lo + st, 0, L);
   }
+  if constexpr (NB == 2) gload(s_lo + 1, LA, L);
   f32x4 last[C::EXACT ? NF : 1] = {};                  // sums not added yet, and their scale
   float flast = 0.f;
   for (int st = s_lo; st < s_hi; ++st) {
-    wait_loads<(NB - 2) * (LA + LW)>();
+    wait_loads<NB == 2 ? LW : (NB - 2) * L>();
     asm volatile("s_barrier" ::: "memory");
     if ((st & 3) == 0) load_scales(st / 4 + 1);
     const uint8_t* base = lds + (st % NB) * C::STAGE;
@@ -470,7 +477,14 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
 #pragma unroll
       for (int i = 0; i < MF; ++i) {
         if (i + 1 < MF) read_a(i + 1);
-        gload(st + NB - 1, i, MF);
+        if constexpr (NB > 2) {
+          gload(st + NB - 1, L * i / MF, L * (i + 1) / MF);
+        } else if (i < MF / 2) {                        // two buffers
+          gload(st + 1, LA * i / (MF / 2), LA * (i + 1) / (MF / 2));
+        } else {
+          if (i == MF / 2) asm volatile("s_barrier" ::: "memory");
+          gload(st + 2, LA + LW * (i - MF / 2) / (MF - MF / 2), LA + LW * (i - MF / 2 + 1) / (MF - MF / 2));
+        }
         __builtin_amdgcn_sched_barrier(0);
         const i32x8 a = __builtin_bit_cast(i32x8, Pair16{af[i & 1][0], af[i & 1][1]});
 #pragma unroll
@@ -491,7 +505,7 @@ __global__ __launch_bounds__(64 * C::WAVES, C::WAVES / 4) void gemm8_rows_kernel
 #pragma unroll
       for (int i = 0; i < MF; ++i) {
         if (i + 2 < MF) read_a(i + 2);
-        gload(st + NB - 1, i, MF);
+        gload(st + NB - 1, L * i / MF, L * (i + 1) / MF);
         __builtin_amdgcn_sched_barrier(0);
         f32x4 sum[NF];
 #pragma unroll
@@ -683,11 +697,11 @@ template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipSt
 // ranges: a round of workgroups takes e microseconds for its start and epilogue,
 // and a + c w for every stage, w the workgroups per CU (up to per_cu; less than
 // one in a last round that does not fill the card).  K ranges add the pass that
-// sums them.  Fitted to 65 to 2048 rows, N of 512 to 11008 and K of 1024 to 11008
-// (weights from HBM); against the fastest of nine to twelve tiles and of 1, 2
-// and 4 K ranges the choice is on average 2.4 % slower for bf16 outputs (304
-// shapes, the worst 31 %), 2.9 % for fp32 ones (the worst 28 %) and 0.1 % for
-// gate/up (225 shapes, the worst 6 %).  One K range for all would cost 6 % and 14 %.
+// sums them.  Fitted to 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008
+// (weights from HBM); against the fastest of all tiles and of 1, 2 and 4 K ranges
+// the choice is on average 0.4 % slower for bf16 outputs (360 shapes, the worst
+// 32 %), 0.8 % for fp32 ones (304, the worst 14 %) and 0.1 % for gate/up (405,
+// the worst 7 %).  One K range for all would cost 5 % and 17 %.
 struct Tile8Model {
   int mf, nf, wm, wn, nb;   // Tile8
   bool exact;
@@ -698,26 +712,27 @@ struct Tile8Model {
 };
 static constexpr Tile8Model TILES8[] = {
     // bf16 outputs, on the 8-bit matrix instruction
-    {4, 4, 2, 4, 3, false, 1, 6.8f, 0.725f, 0.258f},    // 128 x 256
-    {4, 2, 2, 4, 3, false, 1, 4.6f, 0.467f, 0.175f},    // 128 x 128
-    {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.084f},    // 128 x 64
-    {2, 2, 2, 2, 4, false, 2, 3.0f, 0.230f, 0.135f},    // 64 x 64
+    {4, 4, 2, 4, 3, false, 1, 6.8f, 0.756f, 0.228f},    // 128 x 256
+    {4, 2, 2, 4, 3, false, 1, 5.3f, 0.399f, 0.166f},    // 128 x 128
+    {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.050f},    // 128 x 64
+    {2, 2, 2, 2, 4, false, 2, 3.1f, 0.227f, 0.138f},    // 64 x 64
+    {4, 4, 4, 4, 2, false, 1, 10.3f, 1.111f, 0.611f},   // 256 x 256
     // fp32 outputs, on fp16 operands
-    {4, 4, 2, 4, 3, true, 1, 7.5f, 1.454f, 0.322f},     // 128 x 256
-    {2, 2, 2, 4, 3, true, 2, 4.4f, 0.610f, 0.312f},     // 64 x 128
-    {2, 2, 2, 2, 4, true, 2, 3.4f, 0.469f, 0.140f},     // 64 x 64
+    {4, 4, 2, 4, 3, true, 1, 4.5f, 0.968f, 0.223f},     // 128 x 256
+    {2, 2, 2, 4, 3, true, 2, 4.3f, 0.554f, 0.174f},     // 64 x 128
+    {2, 2, 2, 2, 4, true, 2, 3.8f, 0.513f, 0.145f},     // 64 x 64
     // gate/up: 256 columns, the block of 128 outputs.  On the 8-bit matrix
     // instruction: its outputs are rounded to four significant bits, and the
     // 5e-5 that it is off by moves under one code in a thousand across a border
     // (2^-3 of its value; 2.4e-3 of all outputs' norm, of which the rounding to
     // codes takes 2.5e-2).  fp16 operands: 1.9 times the time (178 us against 94
     // at 2048 x 4096 x 11008).
-    {4, 4, 4, 4, 2, false, 1, 12.7f, 1.391f, 0.532f},   // 256 x 256
-    {6, 4, 2, 4, 2, false, 1, 10.5f, 1.253f, 0.356f},   // 192 x 256
-    {4, 4, 2, 4, 3, false, 1, 8.8f, 0.731f, 0.135f},    // 128 x 256
+    {4, 4, 4, 4, 2, false, 1, 13.0f, 1.029f, 0.419f},   // 256 x 256
+    {6, 4, 2, 4, 2, false, 1, 7.1f, 1.072f, 0.356f},   // 192 x 256
+    {4, 4, 2, 4, 3, false, 1, 8.8f, 0.693f, 0.176f},    // 128 x 256
     {2, 4, 2, 4, 3, false, 1, 6.1f, 0.550f, 0.054f},    // 64 x 256
 };
-constexpr int TILES8_FAST = 0, TILES8_EXACT = 4, TILES8_GATE_UP = 7, TILES8_END = 11;
+constexpr int TILES8_FAST = 0, TILES8_EXACT = 5, TILES8_GATE_UP = 8, TILES8_END = 12;
 template <int T>
 using Tile8At = Tile8<TILES8[T].mf, TILES8[T].nf, TILES8[T].wm, TILES8[T].wn, TILES8[T].nb, TILES8[T].exact>;
 
@@ -734,7 +749,7 @@ static Gemm8Plan pick_tile8(int lo, int hi, int M, int N, int K, int max_ksplit)
       const double slots = 256.0 * m.per_cu, full = std::floor(grid / slots), part = grid - full * slots;
       double us = full * (m.e + stages * (m.a + m.c * m.per_cu));
       if (part > 0) us += m.e + stages * (m.a + m.c * part / 256);
-      if (ks > 1) us += 3.2 + 0.2e-6 * ks * M * N * 4;
+      if (ks > 1) us += 4.0 + 0.29e-6 * ks * M * N * 4;
       if (us < best_t) {
         best_t = us;
         best = Gemm8Plan{true, t, ks};

@@ -450,7 +450,8 @@ def test_streams_and_graphs():
 @pytest.mark.parametrize("M,N,K", [(3, 500, 10300), (64, 1000, 2560), (64, 1500, 5200), (50, 3000, 5130), (20, 16130, 140), (64, 4200, 300),
                                    (70, 300, 10000), (65, 300, 4200), (200, 2100, 8400), (200, 8200, 140), (769, 5000, 140), (65, 4100, 8400),
                                    (769, 2100, 1500), (65, 8200, 8400), (3, 40, 16500), (64, 33, 40000), (1200, 300, 700), (4000, 130, 2200),
-                                   (65, 8200, 11000), (65, 12000, 6000), (4200, 130, 6000), (2100, 130, 8400), (2100, 520, 11000)])
+                                   (65, 8200, 11000), (65, 12000, 6000), (4200, 130, 6000), (2100, 130, 8400), (2100, 520, 11000),
+                                   (1000, 8200, 140), (100, 5000, 6000), (400, 8200, 14000)])
 def test_linear_ranges_and_tiles(M, N, K, dtype):
     import torch
     from paper_2510_11331_amd import linear_q
@@ -465,7 +466,8 @@ def test_linear_ranges_and_tiles(M, N, K, dtype):
 
 
 @pytest.mark.parametrize("M,F,K", [(3, 6000, 140), (20, 10000, 260), (33, 14000, 130), (64, 18000, 130), (64, 16400, 20), (3, 48, 16500), (65, 288, 140),
-                                   (2050, 992, 140), (769, 4992, 140), (769, 8192, 140)])
+                                   (2050, 992, 140), (769, 4992, 140), (769, 8192, 140),
+                                   (130, 12016, 1000), (400, 12016, 270)])
 def test_gate_up_tiles(M, F, K):
     """Few rows: 4, 6 and 8 tiles a workgroup, more than one round of them; K past the streamed scales; every row tile."""
     import torch
