@@ -314,10 +314,10 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
 // half a stage to arrive (gate/up of 8192 rows, 256 x 256: 755 -> 695 us; 1024
 // rows 138 -> 121).
 //
-// 2048 x 4096 x 11008, bf16 out: 81 us, 2.29 PFLOP/s of the 2.64 of a large
+// 2048 x 4096 x 11008, bf16 out: 83 us, 2.22 PFLOP/s of the 2.64 of a large
 // library product (in a graph of such calls 91, of which its loads alone would
 // take 78 and its LDS reads and products alone 80); gate/up 2048 x 22016 x 4096:
-// 198 us, 1.87 PFLOP/s.
+// 184 us, 2.01 PFLOP/s.
 template <int MF_, int NF_, int WM_, int WN_, int NB_, bool EXACT_> struct Tile8 {
   static constexpr int MF = MF_, NF = NF_, WM = WM_, WN = WN_, NB = NB_;
   static constexpr bool EXACT = EXACT_;
