@@ -311,8 +311,10 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
 // go out in the first half of a stage; a second barrier in its middle, when every
 // wave has the stage's weights in registers, frees their part of the buffer for
 // the weights' loads of the stage after next.  All of them then have at least
-// half a stage to arrive (gate/up of 8192 rows, 256 x 256: 755 -> 695 us; 1024
-// rows 138 -> 121).
+// half a stage to arrive (gate/up of 8192 rows on sixteen waves: 755 -> 695 us).
+// Eight waves of 128 x 64 read three quarters of what sixteen of 64 x 64 read
+// from LDS, whose reads take as long as the products (8192 rows 645 us, 2048 rows
+// 220 -> 184 in the same graph).
 //
 // 2048 x 4096 x 11008, bf16 out: 83 us, 2.22 PFLOP/s of the 2.64 of a large
 // library product (in a graph of such calls 91, of which its loads alone would
@@ -700,8 +702,8 @@ template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipSt
 // sums them.  Fitted to 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008
 // (weights from HBM); against the fastest of all tiles and of 1, 2 and 4 K ranges
 // the choice is on average 0.4 % slower for bf16 outputs (360 shapes, the worst
-// 32 %), 0.8 % for fp32 ones (304, the worst 14 %) and 0.1 % for gate/up (405,
-// the worst 7 %).  One K range for all would cost 5 % and 17 %.
+// 31 %), 0.8 % for fp32 ones (304, the worst 14 %) and 0.03 % for gate/up (405,
+// the worst 5 %).  One K range for all would cost 5 % and 17 %.
 struct Tile8Model {
   int mf, nf, wm, wn, nb;   // Tile8
   bool exact;
@@ -712,11 +714,11 @@ struct Tile8Model {
 };
 static constexpr Tile8Model TILES8[] = {
     // bf16 outputs, on the 8-bit matrix instruction
-    {4, 4, 2, 4, 3, false, 1, 6.8f, 0.756f, 0.228f},    // 128 x 256
-    {4, 2, 2, 4, 3, false, 1, 5.3f, 0.399f, 0.166f},    // 128 x 128
+    {4, 4, 2, 4, 3, false, 1, 6.8f, 0.756f, 0.207f},    // 128 x 256
+    {4, 2, 2, 4, 3, false, 1, 5.3f, 0.399f, 0.156f},    // 128 x 128
     {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.050f},    // 128 x 64
     {2, 2, 2, 2, 4, false, 2, 3.1f, 0.227f, 0.138f},    // 64 x 64
-    {4, 4, 4, 4, 2, false, 1, 10.3f, 1.111f, 0.611f},   // 256 x 256
+    {8, 4, 2, 4, 2, false, 1, 10.3f, 1.111f, 0.446f},   // 256 x 256
     // fp32 outputs, on fp16 operands
     {4, 4, 2, 4, 3, true, 1, 4.5f, 0.968f, 0.223f},     // 128 x 256
     {2, 2, 2, 4, 3, true, 2, 4.3f, 0.554f, 0.174f},     // 64 x 128
@@ -727,9 +729,9 @@ static constexpr Tile8Model TILES8[] = {
     // (2^-3 of its value; 2.4e-3 of all outputs' norm, of which the rounding to
     // codes takes 2.5e-2).  fp16 operands: 1.9 times the time (178 us against 94
     // at 2048 x 4096 x 11008).
-    {4, 4, 4, 4, 2, false, 1, 13.0f, 1.029f, 0.419f},   // 256 x 256
-    {6, 4, 2, 4, 2, false, 1, 7.1f, 1.072f, 0.356f},   // 192 x 256
-    {4, 4, 2, 4, 3, false, 1, 8.8f, 0.693f, 0.176f},    // 128 x 256
+    {8, 4, 2, 4, 2, false, 1, 11.6f, 1.264f, 0.378f},   // 256 x 256
+    {6, 4, 2, 4, 2, false, 1, 7.2f, 1.072f, 0.356f},   // 192 x 256
+    {4, 4, 2, 4, 3, false, 1, 8.8f, 0.731f, 0.161f},    // 128 x 256
     {2, 4, 2, 4, 3, false, 1, 6.1f, 0.550f, 0.054f},    // 64 x 256
 };
 constexpr int TILES8_FAST = 0, TILES8_EXACT = 5, TILES8_GATE_UP = 8, TILES8_END = 12;
