@@ -316,10 +316,10 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
 // from LDS, whose reads take as long as the products (8192 rows 645 us, 2048 rows
 // 220 -> 184 in the same graph).
 //
-// 2048 x 4096 x 11008, bf16 out: 83 us, 2.22 PFLOP/s of the 2.64 of a large
-// library product (in a graph of such calls 91, of which its loads alone would
+// 2048 x 4096 x 11008, bf16 out: 79 us, 2.35 PFLOP/s of the 2.64 of a large
+// library product (in a graph of such calls 90, of which its loads alone would
 // take 78 and its LDS reads and products alone 80); gate/up 2048 x 22016 x 4096:
-// 184 us, 2.01 PFLOP/s.
+// 169 us, 2.19 PFLOP/s.
 template <int MF_, int NF_, int WM_, int WN_, int NB_, bool EXACT_> struct Tile8 {
   static constexpr int MF = MF_, NF = NF_, WM = WM_, WN = WN_, NB = NB_;
   static constexpr bool EXACT = EXACT_;
