@@ -352,11 +352,11 @@ int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const vo
 /* out = [add +] rows W^T: rows (q, exps) [M, K], w a packed [N, K].  out
  * [M, N] of dtype with row stride ldo >= N (entries); add NULL or fp32 with
  * the same stride; with dtype fp32 it may be out itself (else no overlap).
- * Sums are in fp32.  The products of up to 64 rows, and those of fp32 outputs,
- * run on fp16 operands (the codes' values, exactly), with the product of two
- * blocks' scales held within 2^-126 to 2^127 (below it counts as 0); bf16
- * outputs of more rows run on the 8-bit matrix instruction, which drops low
- * bits of the products it adds (up to 5e-5 of the outputs' root mean square).
+ * Sums are in fp32, on fp16 operands (the codes' values, exactly), with the
+ * product of two blocks' scales held within 2^-126 to 2^127 (below it counts as
+ * 0).  sd_linear_q_fast: the same, but products of more than 64 rows run on
+ * the 8-bit matrix instruction, which drops low bits of the products it adds (up
+ * to 5e-5 of the outputs' root mean square).
  * The workspace (16-byte aligned, sd_linear_q_workspace_bytes(M, N, K); where
  * that is 0, as on an invalid size, it may be NULL) is scratch of this call
  * alone until its work is done: calls that may overlap, graphs among them, need
@@ -364,16 +364,20 @@ int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const vo
 size_t sd_linear_q_workspace_bytes(int M, int N, int K);
 int sd_linear_q(int M, int N, int K, const uint8_t *q, const uint8_t *exps, const void *w, const float *add,
                 void *out, int ldo, int dtype, void *workspace, size_t workspace_bytes, void *stream);
+int sd_linear_q_fast(int M, int N, int K, const uint8_t *q, const uint8_t *exps, const void *w, const float *add,
+                     void *out, int ldo, int dtype, void *workspace, size_t workspace_bytes, void *stream);
 
 /* SwiGLU of the gate/up product with an 8-bit output: w is the packed [2 F, K]
  * with gate and up rows interleaved in blocks of 16 (see wgu of sd_weights), h
  * = silu(gate) * up is written as rows of F entries (q_out, exps_out), the
  * input of a down projection with K = F.  F a multiple of 16, at most 2^18.
- * Above 64 rows, or K = 16384, on the 8-bit matrix instruction.
- * Workspace as for sd_linear_q, of sd_gate_up_q_workspace_bytes(M, F, K). */
+ * Sums, and sd_gate_up_q_fast, as for sd_linear_q.  Workspace as for sd_linear_q,
+ * of sd_gate_up_q_workspace_bytes(M, F, K). */
 size_t sd_gate_up_q_workspace_bytes(int M, int F, int K);
 int sd_gate_up_q(int M, int F, int K, const uint8_t *q, const uint8_t *exps, const void *w, uint8_t *q_out,
                 uint8_t *exps_out, void *workspace, size_t workspace_bytes, void *stream);
+int sd_gate_up_q_fast(int M, int F, int K, const uint8_t *q, const uint8_t *exps, const void *w, uint8_t *q_out,
+                     uint8_t *exps_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Copy slot state to out [B, 4] int32 (device): committed target length
  * P, next input token x0, pending draft input (-1 if none), KV capacity. */

@@ -666,14 +666,13 @@ static Gemm8Plan plan_stream8(int M, int N, int K, int most) {
 
 template <int MT, int EPI> static hipError_t gemm8_n(int nt, const Gemm8Params& p, hipStream_t s) {
   if constexpr (EPI == EPI8_SWIGLU) {
-    // one workgroup per CU and round, which holds all the tiles it is dealt (of 224
-    // measured calls 1 % slower than the fastest; two tiles throughout 3 %, 27 % at
-    // 27648 x 5120 and 64 rows)
-    const int per_cu = (p.N / 16 + 255) / 256;
-    if (per_cu <= 2) return gemm8_t<MT, 2, 2, EPI>(p, 256, s);
-    if (per_cu <= 4) return gemm8_t<MT, 4, 2, EPI>(p, 256, s);
-    if (per_cu <= 6) return gemm8_t<MT, 6, 2, EPI>(p, 256, s);
-    return gemm8_t<MT, 8, 2, EPI>(p, 256, s);
+    switch (nt) {
+      case 2: return gemm8_t<MT, 2, 2, EPI>(p, 256, s);
+      case 4: return gemm8_t<MT, 4, 2, EPI>(p, 256, s);
+      case 6: return gemm8_t<MT, 6, 2, EPI>(p, 256, s);
+      case 8: return gemm8_t<MT, 8, 2, EPI>(p, 256, s);
+      default: return hipErrorInvalidValue;
+    }
   } else {
     if (nt == 1) return gemm8_t<MT, 1, 3, EPI>(p, 0, s);
     if constexpr (EPI == EPI8_STORE || MT > 1) {         // (two tiles in K ranges: 17 rows and more, at K up to 16384)
@@ -701,9 +700,10 @@ template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipSt
 // one in a last round that does not fill the card).  K ranges add the pass that
 // sums them.  Fitted to 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008
 // (weights from HBM); against the fastest of all tiles and of 1, 2 and 4 K ranges
-// the choice is on average 0.4 % slower for bf16 outputs (360 shapes, the worst
-// 31 %), 0.8 % for fp32 ones (304, the worst 14 %) and 0.03 % for gate/up (405,
-// the worst 5 %).  One K range for all would cost 5 % and 17 %.
+// the choice is on average 0.4 % slower for the 8-bit instruction (360 shapes with
+// bf16 outputs, the worst 31 %), 0.8 % for fp16 operands (304 with fp32 ones, the
+// worst 14 %) and 0.03 % for gate/up on the 8-bit instruction (405, the worst 5 %).
+// One K range for all would cost 5 % and 17 %.
 struct Tile8Model {
   int mf, nf, wm, wn, nb;   // Tile8
   bool exact;
@@ -713,28 +713,32 @@ struct Tile8Model {
   constexpr int bn() const { return 16 * nf * wn; }
 };
 static constexpr Tile8Model TILES8[] = {
-    // bf16 outputs, on the 8-bit matrix instruction
+    // on the 8-bit matrix instruction, for callers that chose it
     {4, 4, 2, 4, 3, false, 1, 6.8f, 0.756f, 0.207f},    // 128 x 256
     {4, 2, 2, 4, 3, false, 1, 5.3f, 0.399f, 0.156f},    // 128 x 128
     {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.050f},    // 128 x 64
     {2, 2, 2, 2, 4, false, 2, 3.1f, 0.227f, 0.138f},    // 64 x 64
     {8, 4, 2, 4, 2, false, 1, 10.3f, 1.111f, 0.446f},   // 256 x 256
-    // fp32 outputs, on fp16 operands
+    // on fp16 operands (2048 x 4096 x 11008, bf16 out: 158 us against 82)
     {4, 4, 2, 4, 3, true, 1, 4.5f, 0.968f, 0.223f},     // 128 x 256
     {2, 2, 2, 4, 3, true, 2, 4.3f, 0.554f, 0.174f},     // 64 x 128
     {2, 2, 2, 2, 4, true, 2, 3.8f, 0.513f, 0.145f},     // 64 x 64
     // gate/up: 256 columns, the block of 128 outputs.  On the 8-bit matrix
-    // instruction: its outputs are rounded to four significant bits, and the
-    // 5e-5 that it is off by moves under one code in a thousand across a border
-    // (2^-3 of its value; 2.4e-3 of all outputs' norm, of which the rounding to
-    // codes takes 2.5e-2).  fp16 operands: 1.9 times the time (178 us against 94
-    // at 2048 x 4096 x 11008).
+    // instruction, for callers that chose it: its outputs are rounded to four
+    // significant bits, and the 5e-5 that it is off by moves under one code in a
+    // thousand across a border (2^-3 of its value; 2.4e-3 of all outputs' norm, of
+    // which the rounding to codes takes 2.5e-2)
     {8, 4, 2, 4, 2, false, 1, 11.6f, 1.264f, 0.378f},   // 256 x 256
     {6, 4, 2, 4, 2, false, 1, 7.2f, 1.072f, 0.356f},   // 192 x 256
     {4, 4, 2, 4, 3, false, 1, 8.8f, 0.731f, 0.161f},    // 128 x 256
     {2, 4, 2, 4, 3, false, 1, 6.1f, 0.550f, 0.054f},    // 64 x 256
+    // gate/up on fp16 operands (of 2048 x 22016 x 4096 361 us against 178; 446 measured
+    // calls of 65 to 4096 rows: the choice is on average 0.06 % slower than the
+    // faster of the two, the worst 4 %)
+    {4, 4, 2, 4, 3, true, 1, 9.2f, 1.530f, 0.242f},     // 128 x 256
+    {2, 4, 2, 4, 3, true, 1, 6.4f, 1.061f, 0.015f},     // 64 x 256
 };
-constexpr int TILES8_FAST = 0, TILES8_EXACT = 5, TILES8_GATE_UP = 8, TILES8_END = 12;
+constexpr int TILES8_FAST = 0, TILES8_EXACT = 5, TILES8_GATE_UP = 8, TILES8_GATE_UP_EXACT = 12, TILES8_END = 14;
 template <int T>
 using Tile8At = Tile8<TILES8[T].mf, TILES8[T].nf, TILES8[T].wm, TILES8[T].wn, TILES8[T].nb, TILES8[T].exact>;
 
@@ -764,6 +768,15 @@ static Gemm8Plan pick_tile8(int lo, int hi, int M, int N, int K, int max_ksplit)
 // Up to 64 rows the streaming kernel, above (and past the scales it holds in LDS) row tiles
 static bool streams8(int M, int K) { return M <= 64 && ke8(K) <= STREAM8_KE; }
 bool gate_up8_fused(int M, int K) { return !streams8(M, K); }
+Gemm8Plan plan_gate_up8(int M, int N, int K, bool exact) {
+  if (streams8(M, K)) {
+    // one workgroup per CU and round, which holds all the tiles it is dealt (of 224
+    // measured calls 1 % slower than the fastest; two tiles throughout 3 %, 27 % at
+    // 27648 x 5120 and 64 rows)
+    return Gemm8Plan{false, std::min(8, (N / 16 + 511) / 512 * 2), 1};
+  }
+  return exact ? pick_tile8(TILES8_GATE_UP_EXACT, TILES8_END, M, N, K, 1) : pick_tile8(TILES8_GATE_UP, TILES8_GATE_UP_EXACT, M, N, K, 1);
+}
 Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap) {
   const size_t one = (size_t)M * part8_ld(N);
   const int most = part_cap >= 4 * one ? 4 : part_cap >= 2 * one ? 2 : 1;
@@ -791,11 +804,9 @@ hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p0, h
   p.wide = p.ldo % 4 == 0 && (uintptr_t)p.out % (p.bf16 ? 8 : 16) == 0 && (uintptr_t)p.add % 16 == 0;
   p.ksplit = 1;
   if (epi == EPI8_SWIGLU_Q) {
-    if (p.N % 32) return hipErrorInvalidValue;
-    return gemm8_rows_at<EPI8_SWIGLU_Q, TILES8_GATE_UP, TILES8_END>(
-        pick_tile8(TILES8_GATE_UP, TILES8_END, p.M, p.N, p.K, 1).tile, p, s);
+    return p.N % 32 || !plan.rows ? hipErrorInvalidValue : gemm8_rows_at<EPI8_SWIGLU_Q, TILES8_GATE_UP, TILES8_END>(plan.tile, p, s);
   }
-  if (epi == EPI8_SWIGLU) return p.N % 32 || !streams8(p.M, p.K) ? hipErrorInvalidValue : gemm8_m<EPI8_SWIGLU>(0, p, s);
+  if (epi == EPI8_SWIGLU) return p.N % 32 || plan.rows || !streams8(p.M, p.K) ? hipErrorInvalidValue : gemm8_m<EPI8_SWIGLU>(plan.tile, p, s);
   if (epi != EPI8_STORE && epi != EPI8_PART) return hipErrorInvalidValue;
   if (!plan.rows && !streams8(p.M, p.K)) return hipErrorInvalidValue;
   if (plan.ksplit == 1) {
@@ -816,11 +827,12 @@ hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p0, h
   return hipGetLastError();
 }
 
-hipError_t launch_gate_up8(const Gemm8Params& p, float* h, hipStream_t s) {
-  if (gate_up8_fused(p.M, p.K)) return launch_gemm8(EPI8_SWIGLU_Q, Gemm8Plan{}, p, s);
+hipError_t launch_gate_up8(const Gemm8Params& p, float* h, bool exact, hipStream_t s) {
+  const Gemm8Plan plan = plan_gate_up8(p.M, p.N, p.K, exact);
+  if (plan.rows) return launch_gemm8(EPI8_SWIGLU_Q, plan, p, s);
   Gemm8Params q = p;
   q.out = h;
-  const hipError_t r = launch_gemm8(EPI8_SWIGLU, Gemm8Plan{}, q, s);
+  const hipError_t r = launch_gemm8(EPI8_SWIGLU, plan, q, s);
   return r != hipSuccess ? r : launch_quantise_rows8(h, p.q_out, p.exps_out, p.M, p.N / 2, s);
 }
 

@@ -528,7 +528,7 @@ int ffn_q(sd_ctx* ctx, const ModelRT& m, Lane& ln, int l, int M, int ns, bool ve
   ProfRec r;
   prof_begin(ctx, s, r, verify ? SD_PROF_GEMM_VERIFY_ALL : -1, verify ? SD_PROF_GEMM_VERIFY_GATEUP : -1,
              (double)sd_linear_q_bytes(2 * F, d) + (double)M * (d + F), false);
-  HIPCHK(launch_gate_up8(g, ln.h8, s));
+  HIPCHK(launch_gate_up8(g, ln.h8, false, s));
   prof_end(ctx, s, r);
   g = Gemm8Params{};
   g.q = ln.qh8;
@@ -1297,8 +1297,8 @@ size_t sd_linear_q_workspace_bytes(int M, int N, int K) {
   return ks > 1 ? ks * one * sizeof(float) : 0;
 }
 
-int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add, void* out,
-                int ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+static int linear_q(bool exact, int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add,
+                    void* out, int ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K) || ldo < N || (dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32))
     return SD_EINVAL;
   if (M == 0) return SD_OK;
@@ -1319,9 +1319,19 @@ int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, cons
   gp.ldo = ldo;
   gp.part = (float*)workspace;
   gp.bf16 = dtype == SD_DTYPE_BF16;
-  const Gemm8Plan plan = plan_gemm8(M, N, K, dtype == SD_DTYPE_F32, need / sizeof(float));
+  const Gemm8Plan plan = plan_gemm8(M, N, K, exact, need / sizeof(float));
   HIPCHK(launch_gemm8(EPI8_STORE, plan, gp, (hipStream_t)stream));
   return SD_OK;
+}
+
+int sd_linear_q(int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add, void* out,
+                int ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  return linear_q(true, M, N, K, q, exps, w, add, out, ldo, dtype, workspace, workspace_bytes, stream);
+}
+
+int sd_linear_q_fast(int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add, void* out,
+                     int ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  return linear_q(false, M, N, K, q, exps, w, add, out, ldo, dtype, workspace, workspace_bytes, stream);
 }
 
 size_t sd_gate_up_q_workspace_bytes(int M, int F, int K) {
@@ -1329,8 +1339,8 @@ size_t sd_gate_up_q_workspace_bytes(int M, int F, int K) {
   return gate_up8_fused(M, K) ? 0 : (size_t)M * F * sizeof(float);
 }
 
-int sd_gate_up_q(int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
-                uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
+static int gate_up_q(bool exact, int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
+                     uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
   if (M < 0 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_K || !sd_linear_q_bytes(2 * F, K)) return SD_EINVAL;
   if (M == 0) return SD_OK;
   const size_t need = sd_gate_up_q_workspace_bytes(M, F, K);
@@ -1346,8 +1356,18 @@ int sd_gate_up_q(int M, int F, int K, const uint8_t* q, const uint8_t* exps, con
   gp.K = K;
   gp.q_out = q_out;
   gp.exps_out = exps_out;
-  HIPCHK(launch_gate_up8(gp, (float*)workspace, (hipStream_t)stream));
+  HIPCHK(launch_gate_up8(gp, (float*)workspace, exact, (hipStream_t)stream));
   return SD_OK;
+}
+
+int sd_gate_up_q(int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
+                uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
+  return gate_up_q(true, M, F, K, q, exps, w, q_out, exps_out, workspace, workspace_bytes, stream);
+}
+
+int sd_gate_up_q_fast(int M, int F, int K, const uint8_t* q, const uint8_t* exps, const void* w, uint8_t* q_out,
+                      uint8_t* exps_out, void* workspace, size_t workspace_bytes, void* stream) {
+  return gate_up_q(false, M, F, K, q, exps, w, q_out, exps_out, workspace, workspace_bytes, stream);
 }
 
 const char* sd_last_error(void) { return g_last_error; }

@@ -340,15 +340,16 @@ hipError_t launch_add_rmsnorm8(int x_dtype, int gain_dtype, const Norm8Params& p
 hipError_t launch_quantise_rows8(const float* h, uint8_t* q, uint8_t* exps, int M, int F, hipStream_t s);
 hipError_t launch_pack_linear8(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 bool gate_up8_fused(int M, int K);
-// How a STORE product runs.  exact: sums as exact as fp32 ones; else row tiles
+// How a product runs.  exact: sums as exact as fp32 ones; else row tiles
 // use the 8-bit matrix instruction.  part_cap: entries that p.part holds.
 // rows: on row tiles (tile: its number), else streamed (tile: 16-column tiles of a workgroup)
 struct Gemm8Plan { bool rows; int tile, ksplit; };
 inline int part8_ld(int N) { return (N + 3) & ~3; }
 Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap);
+Gemm8Plan plan_gate_up8(int M, int N, int K, bool exact);
 // gate/up product p (N = 2 F columns) with SwiGLU, its output in p.q_out / p.exps_out; h: [M, F] fp32
 // scratch, unless gate_up8_fused
-hipError_t launch_gate_up8(const Gemm8Params& p, float* h, hipStream_t s);
+hipError_t launch_gate_up8(const Gemm8Params& p, float* h, bool exact, hipStream_t s);
 hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p, hipStream_t s);
 hipError_t launch_pack_linear(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 

@@ -10,6 +10,10 @@ feed-forward pass on a residual stream x is
     q, e = gate_up_q(q, e, w_gate_up)
     x = linear_q(q, e, w_down, add=x)
 
+Sums are as exact as fp32 ones.  fast=True: of more than 64 rows they run on the 8-bit
+matrix instruction, which takes about half the time and drops low bits of the products
+that it adds (sd_linear_q_fast).
+
 Every call enqueues on `stream` (default: the current stream of the tensors'
 device) and returns new tensors unless it is given some to write to.  Arguments
 that the kernels do not cover raise ValueError, or SDError where only the
@@ -153,13 +157,13 @@ def _rows(q: torch.Tensor, exps: torch.Tensor, w: LinearQ) -> int:
 
 def linear_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, add: Optional[torch.Tensor] = None,
              out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.float32,
-             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+             stream: Optional[torch.cuda.Stream] = None, fast: bool = False) -> torch.Tensor:
     """[add +] rows W^T as [M, N] of dtype (float32 or bfloat16).  out: where it goes (rows may lie apart); add: float32
     with out's strides, or out itself."""
     there = _elsewhere(q, stream) if q.is_cuda else None
     if there is not None:
         with there:
-            return linear_q(q, exps, w, add, out, dtype)
+            return linear_q(q, exps, w, add, out, dtype, None, fast)
     M, N, index = _rows(q, exps, w), w.N, q.get_device()
     ldo = N
     if out is not None:
@@ -181,22 +185,23 @@ def linear_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, add: Optional[torc
     if out is None:
         out = torch.empty((M, N), dtype=dtype, device=q.device)
     work = torch.empty(ws, dtype=torch.uint8, device=q.device) if ws else None
-    rc = L.sd_linear_q(M, N, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(),
-                       None if add is None else add.data_ptr(), out.data_ptr(), ldo, _DTYPES[dtype],
-                       work.data_ptr() if ws else None, ws, _raw_stream(index))
+    call = L.sd_linear_q_fast if fast else L.sd_linear_q
+    rc = call(M, N, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(),
+              None if add is None else add.data_ptr(), out.data_ptr(), ldo, _DTYPES[dtype],
+              work.data_ptr() if ws else None, ws, _raw_stream(index))
     if rc != SD_OK:
         check(rc, "sd_linear_q")
     return out
 
 
-def gate_up_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, stream: Optional[torch.cuda.Stream] = None
-              ) -> Tuple[torch.Tensor, torch.Tensor]:
+def gate_up_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, stream: Optional[torch.cuda.Stream] = None,
+              fast: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows (q, exps) of silu(gate) * up, w the packed [2 F, K] with gate and up rows interleaved in blocks of 16
     (engine.interleave_gate_up)."""
     there = _elsewhere(q, stream) if q.is_cuda else None
     if there is not None:
         with there:
-            return gate_up_q(q, exps, w)
+            return gate_up_q(q, exps, w, None, fast)
     M, F, dev = _rows(q, exps, w), w.N // 2, q.device
     L = lib()
     if w.N % 32 or F > 1 << 18:
@@ -207,8 +212,9 @@ def gate_up_q(q: torch.Tensor, exps: torch.Tensor, w: LinearQ, stream: Optional[
     exps_out = torch.empty((M, _ke(F)), dtype=_E8M0, device=dev)
     ws = L.sd_gate_up_q_workspace_bytes(M, F, w.K)
     work = torch.empty(ws, dtype=torch.uint8, device=dev) if ws else None
-    rc = L.sd_gate_up_q(M, F, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(), q_out.data_ptr(),
-                        exps_out.data_ptr(), work.data_ptr() if ws else None, ws, _raw_stream(q.get_device()))
+    call = L.sd_gate_up_q_fast if fast else L.sd_gate_up_q
+    rc = call(M, F, w.K, q.data_ptr(), exps.data_ptr(), w.data.data_ptr(), q_out.data_ptr(),
+              exps_out.data_ptr(), work.data_ptr() if ws else None, ws, _raw_stream(q.get_device()))
     if rc != SD_OK:
         check(rc, "sd_gate_up_q")
     return q_out, exps_out
