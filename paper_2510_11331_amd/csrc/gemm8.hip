@@ -765,8 +765,10 @@ static Gemm8Plan pick_tile8(int lo, int hi, int M, int N, int K, int max_ksplit)
   return best;
 }
 
-// Up to 64 rows the streaming kernel, above (and past the scales it holds in LDS) row tiles
-static bool streams8(int M, int K) { return M <= 64 && ke8(K) <= STREAM8_KE; }
+// Up to 64 rows the streaming kernel, above (and past the scales it holds in LDS) row tiles.
+// Up to 64 rows sums are exact on both
+constexpr int FEW8 = 64;
+static bool streams8(int M, int K) { return M <= FEW8 && ke8(K) <= STREAM8_KE; }
 bool gate_up8_fused(int M, int K) { return !streams8(M, K); }
 Gemm8Plan plan_gate_up8(int M, int N, int K, bool exact) {
   if (streams8(M, K)) {
@@ -775,13 +777,15 @@ Gemm8Plan plan_gate_up8(int M, int N, int K, bool exact) {
     // 27648 x 5120 and 64 rows)
     return Gemm8Plan{false, std::min(8, (N / 16 + 511) / 512 * 2), 1};
   }
-  return exact ? pick_tile8(TILES8_GATE_UP_EXACT, TILES8_END, M, N, K, 1) : pick_tile8(TILES8_GATE_UP, TILES8_GATE_UP_EXACT, M, N, K, 1);
+  return exact || M <= FEW8 ? pick_tile8(TILES8_GATE_UP_EXACT, TILES8_END, M, N, K, 1)
+                            : pick_tile8(TILES8_GATE_UP, TILES8_GATE_UP_EXACT, M, N, K, 1);
 }
 Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap) {
   const size_t one = (size_t)M * part8_ld(N);
   const int most = part_cap >= 4 * one ? 4 : part_cap >= 2 * one ? 2 : 1;
   if (streams8(M, K)) return plan_stream8(M, N, K, most);
-  return exact ? pick_tile8(TILES8_EXACT, TILES8_GATE_UP, M, N, K, most) : pick_tile8(TILES8_FAST, TILES8_EXACT, M, N, K, most);
+  return exact || M <= FEW8 ? pick_tile8(TILES8_EXACT, TILES8_GATE_UP, M, N, K, most)
+                            : pick_tile8(TILES8_FAST, TILES8_EXACT, M, N, K, most);
 }
 
 template <int EPI, int LO, int HI> static hipError_t gemm8_rows_at(int tile, const Gemm8Params& p, hipStream_t s) {

@@ -340,8 +340,8 @@ hipError_t launch_add_rmsnorm8(int x_dtype, int gain_dtype, const Norm8Params& p
 hipError_t launch_quantise_rows8(const float* h, uint8_t* q, uint8_t* exps, int M, int F, hipStream_t s);
 hipError_t launch_pack_linear8(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 bool gate_up8_fused(int M, int K);
-// How a product runs.  exact: sums as exact as fp32 ones; else row tiles
-// use the 8-bit matrix instruction.  part_cap: entries that p.part holds.
+// How a product runs.  exact: sums as exact as fp32 ones; else row tiles of
+// more than 64 rows use the 8-bit matrix instruction.  part_cap: entries that p.part holds.
 // rows: on row tiles (tile: its number), else streamed (tile: 16-column tiles of a workgroup)
 struct Gemm8Plan { bool rows; int tile, ksplit; };
 inline int part8_ld(int N) { return (N + 3) & ~3; }

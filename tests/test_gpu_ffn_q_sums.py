@@ -38,19 +38,19 @@ def operands(M, N, K, spread=1.0):
     return a, w, t(c).view(torch.float8_e4m3fn), t(qref.exps_bytes(E)).view(torch.float8_e8m0fnu), LinearQ(t(qref.pack(wc, wE)), N, K)
 
 
-def check_linear(M, N, K, dtype):
+def check_linear(M, N, K, dtype, fast=False):
     from paper_2510_11331_amd import linear_q
     a, w, q, e, wq = operands(M, N, K)
     want, s = qsums.terms(a, w)
-    assert qsums.product_ok(host(linear_q(q, e, wq, dtype=dt(dtype))), want, qsums.sum_error(K, s), dtype)
+    assert qsums.product_ok(host(linear_q(q, e, wq, dtype=dt(dtype), fast=fast)), want, qsums.sum_error(K, s), dtype)
 
 
-def check_gate_up(M, F, K):
+def check_gate_up(M, F, K, fast=False):
     from paper_2510_11331_amd import gate_up_q
     a, w, q, e, wq = operands(M, 2 * F, K, 0.5)
     p, s = qsums.terms(a, w)
     h, err = qref.swiglu(p), qsums.swiglu_error(p, qsums.sum_error(K, s))
-    got = [host(x) for x in gate_up_q(q, e, wq)]
+    got = [host(x) for x in gate_up_q(q, e, wq, fast=fast)]
     blocks = -(-F // 128)
     E = got[1][:, :blocks].astype(np.int64)
     assert not got[0][:, F:].any() and not got[1][:, blocks:].any()
@@ -71,3 +71,13 @@ def test_sums_of_any_rows(M, N, K, dtype):
 def test_gate_up_sums_of_any_rows(M, F, K):
     say("gate_up sums", M, F, K)
     check_gate_up(M, F, K)
+
+
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M,K", [(1, 16384), (1, 16512), (3, 28672), (64, 16500), (64, 40000)])
+def test_sums_of_few_rows_long_k(M, K, fast):
+    """Up to 64 rows every sum is exact, also where K is past what the streaming kernel holds scales of."""
+    say("few rows, long K", M, K, fast)
+    for dtype in ("fp32", "bf16"):
+        check_linear(M, 200, K, dtype, fast)
+    check_gate_up(M, 144, K, fast)
