@@ -379,6 +379,19 @@ int sd_gate_up_q(int M, int F, int K, const uint8_t *q, const uint8_t *exps, con
 int sd_gate_up_q_fast(int M, int F, int K, const uint8_t *q, const uint8_t *exps, const void *w, uint8_t *q_out,
                      uint8_t *exps_out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* How these products run (host only): the choice the launch itself makes, with
+ * fast those of the _fast calls.  A model's projections run as the _fast ones;
+ * its down projection in no more K ranges than its workspace holds sums of.
+ * SD_EINVAL: a size that the call refuses, or no rows. */
+typedef struct sd_linear_q_plan {
+    int streamed;                   /* 1: the weights pass by all rows, else row tiles */
+    int matrix8;                    /* 1: 8-bit matrix instruction, else fp16 operands */
+    int rows, cols;                 /* outputs of a workgroup (streamed: at most) */
+    int k_ranges;                   /* whose sums a second kernel adds (1: none) */
+} sd_linear_q_plan;
+int sd_plan_linear_q(int M, int N, int K, int fast, sd_linear_q_plan *out);
+int sd_plan_gate_up_q(int M, int F, int K, int fast, sd_linear_q_plan *out);
+
 /* Copy slot state to out [B, 4] int32 (device): committed target length
  * P, next input token x0, pending draft input (-1 if none), KV capacity. */
 int sd_slot_state(sd_ctx *ctx, int B, const int32_t *slots, int32_t *out,

@@ -21,7 +21,8 @@ EXPORTS = ("sd_kv_pool_bytes", "sd_workspace_bytes", "sd_plan_projection", "sd_i
            "sd_draft_step", "sd_verify", "sd_accept_resample", "sd_kv_commit", "sd_force_draft", "sd_slot_state",
            "sd_check", "sd_profile", "sd_profile_read", "sd_destroy", "sd_strerror", "sd_last_error",
            "sd_pack_linear", "sd_linear_q_bytes", "sd_linear_q_workspace_bytes", "sd_pack_linear_q", "sd_add_rmsnorm_q", "sd_linear_q",
-           "sd_linear_q_fast", "sd_gate_up_q_workspace_bytes", "sd_gate_up_q", "sd_gate_up_q_fast", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
+           "sd_linear_q_fast", "sd_gate_up_q_workspace_bytes", "sd_gate_up_q", "sd_gate_up_q_fast",
+           "sd_plan_linear_q", "sd_plan_gate_up_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
 
 
 class ModelCfg(C.Structure):
@@ -54,6 +55,10 @@ class Config(C.Structure):
 class ProjPlan(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("M", "N", "K", "ksplit", "grid", "tile", "mf", "nf", "wm", "wn", "ks", "nb", "mt",
                                        "nt", "kw", "tile_unit")]
+
+
+class LinearQPlan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("streamed", "matrix8", "rows", "cols", "k_ranges")]
 
 
 class SchedModel(C.Structure):
@@ -124,6 +129,8 @@ def lib():
         "sd_gate_up_q": (I, [I, I, I, P, P, P, P, P, P, C.c_size_t, P]),
         "sd_linear_q_fast": (I, [I, I, I, P, P, P, P, P, I, I, P, C.c_size_t, P]),
         "sd_gate_up_q_fast": (I, [I, I, I, P, P, P, P, P, P, C.c_size_t, P]),
+        "sd_plan_linear_q": (I, [I, I, I, I, C.POINTER(LinearQPlan)]),
+        "sd_plan_gate_up_q": (I, [I, I, I, I, C.POINTER(LinearQPlan)]),
         "sd_sched_latency": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32), I,
                                  C.POINTER(C.c_double)]),
         "sd_sched_batching": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32),

@@ -788,6 +788,12 @@ Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap) {
                             : pick_tile8(TILES8_FAST, TILES8_EXACT, M, N, K, most);
 }
 
+Gemm8Tile tile_of(const Gemm8Plan& plan, int M) {
+  if (!plan.rows) return Gemm8Tile{true, (M + 15) / 16 * 16, 16 * plan.tile};
+  const Tile8Model& t = TILES8[plan.tile];
+  return Gemm8Tile{t.exact, t.bm(), t.bn()};
+}
+
 template <int EPI, int LO, int HI> static hipError_t gemm8_rows_at(int tile, const Gemm8Params& p, hipStream_t s) {
   hipError_t r = hipErrorInvalidValue;
   auto at = [&]<int T>() {

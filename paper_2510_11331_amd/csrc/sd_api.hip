@@ -1297,6 +1297,23 @@ size_t sd_linear_q_workspace_bytes(int M, int N, int K) {
   return ks > 1 ? ks * one * sizeof(float) : 0;
 }
 
+static sd_linear_q_plan plan_of(const Gemm8Plan& plan, int M) {
+  const Gemm8Tile t = tile_of(plan, M);
+  return sd_linear_q_plan{!plan.rows, !t.exact, t.rows, t.cols, plan.ksplit};
+}
+
+int sd_plan_linear_q(int M, int N, int K, int fast, sd_linear_q_plan* out) {
+  if (!out || M < 1 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K)) return SD_EINVAL;
+  *out = plan_of(plan_gemm8(M, N, K, !fast, sd_linear_q_workspace_bytes(M, N, K) / sizeof(float)), M);
+  return SD_OK;
+}
+
+int sd_plan_gate_up_q(int M, int F, int K, int fast, sd_linear_q_plan* out) {
+  if (!out || M < 1 || M > LINEAR8_MAX_MN || F < 16 || F % 16 || F > LINEAR8_MAX_K || !sd_linear_q_bytes(2 * F, K)) return SD_EINVAL;
+  *out = plan_of(plan_gate_up8(M, 2 * F, K, !fast), M);
+  return SD_OK;
+}
+
 static int linear_q(bool exact, int M, int N, int K, const uint8_t* q, const uint8_t* exps, const void* w, const float* add,
                     void* out, int ldo, int dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (M < 0 || M > LINEAR8_MAX_MN || !sd_linear_q_bytes(N, K) || ldo < N || (dtype != SD_DTYPE_BF16 && dtype != SD_DTYPE_F32))

@@ -347,6 +347,8 @@ struct Gemm8Plan { bool rows; int tile, ksplit; };
 inline int part8_ld(int N) { return (N + 3) & ~3; }
 Gemm8Plan plan_gemm8(int M, int N, int K, bool exact, size_t part_cap);
 Gemm8Plan plan_gate_up8(int M, int N, int K, bool exact);
+struct Gemm8Tile { bool exact; int rows, cols; };   // outputs of a workgroup of a plan for M rows
+Gemm8Tile tile_of(const Gemm8Plan& plan, int M);
 // gate/up product p (N = 2 F columns) with SwiGLU, its output in p.q_out / p.exps_out; h: [M, F] fp32
 // scratch, unless gate_up8_fused
 hipError_t launch_gate_up8(const Gemm8Params& p, float* h, bool exact, hipStream_t s);

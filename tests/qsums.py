@@ -21,6 +21,12 @@ def sum_error(K, s):
     return (np.sqrt(128) + np.sqrt(K / 128 + 16)) * STEP32 * s
 
 
+def cut_error(s):
+    """What sums on the 8-bit matrix instruction are off by: measured at 1.4e-5 to 5.1e-5 of s in the 2-norm, over K of 128 to
+    11008 and rows with and without large entries; this is 2.4 times the largest."""
+    return 2.0 ** -13 * s
+
+
 def to_bf16(v):
     """float64 -> the nearest bf16 (ties to even), as float64; for magnitudes that are normal numbers or zero."""
     m, e = np.frexp(v)

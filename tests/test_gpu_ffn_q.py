@@ -445,7 +445,8 @@ def test_streams_and_graphs():
 
 
 # few rows: K in 4 ranges with one tile a workgroup, 2 ranges, 4 and 2 ranges with two tiles, four tiles a workgroup whose
-# runs cross a block of 128 rows; more rows: each tile with 1, 2 and 4 ranges, for both types; K past the streamed scales
+# runs cross a block of 128 rows; more rows: row tiles with and without ranges, as the planner picks them (every one of them, by
+# name: test_gpu_ffn_q_sums.py); K past the streamed scales
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("M,N,K", [(3, 500, 10300), (64, 1000, 2560), (64, 1500, 5200), (50, 3000, 5130), (20, 16130, 140), (64, 4200, 300),
                                    (70, 300, 10000), (65, 300, 4200), (200, 2100, 8400), (200, 8200, 140), (769, 5000, 140), (65, 4100, 8400),

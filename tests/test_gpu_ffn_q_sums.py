@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import qplans
 import qref
 import qsums
 from sdcase import say
@@ -45,18 +46,23 @@ def check_linear(M, N, K, dtype, fast=False):
     assert qsums.product_ok(host(linear_q(q, e, wq, dtype=dt(dtype), fast=fast)), want, qsums.sum_error(K, s), dtype)
 
 
+def check_codes(got, product, err):
+    """The rows that gate_up_q returned for a product known to err."""
+    h, err = qref.swiglu(product), qsums.swiglu_error(product, err)
+    q, exps = (host(x) for x in got)
+    F, blocks = h.shape[1], -(-h.shape[1] // 128)
+    E = exps[:, :blocks].astype(np.int64)
+    assert not q[:, F:].any() and not exps[:, blocks:].any()
+    hc, hE = qref.quantise_rows(h)
+    scale = np.repeat(2.0 ** (np.maximum(E, hE) - 127.0), 128, 1)[:, :F]
+    assert qsums.codes_ok(qref.row_values(q, E, F), h, err, qref.row_values(hc, hE, F), scale)
+
+
 def check_gate_up(M, F, K, fast=False):
     from paper_2510_11331_amd import gate_up_q
     a, w, q, e, wq = operands(M, 2 * F, K, 0.5)
     p, s = qsums.terms(a, w)
-    h, err = qref.swiglu(p), qsums.swiglu_error(p, qsums.sum_error(K, s))
-    got = [host(x) for x in gate_up_q(q, e, wq, fast=fast)]
-    blocks = -(-F // 128)
-    E = got[1][:, :blocks].astype(np.int64)
-    assert not got[0][:, F:].any() and not got[1][:, blocks:].any()
-    hc, hE = qref.quantise_rows(h)
-    scale = np.repeat(2.0 ** (np.maximum(E, hE) - 127.0), 128, 1)[:, :F]
-    assert qsums.codes_ok(qref.row_values(got[0], E, F), h, err, qref.row_values(hc, hE, F), scale)
+    check_codes(gate_up_q(q, e, wq, fast=fast), p, qsums.sum_error(K, s))
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -81,3 +87,65 @@ def test_sums_of_few_rows_long_k(M, K, fast):
     for dtype in ("fp32", "bf16"):
         check_linear(M, 200, K, dtype, fast)
     check_gate_up(M, 144, K, fast)
+
+
+# ------------------------------------------------------------------ every plan
+
+
+def codes8(M, N, K, n_exp, w_exp):
+    """Random codes and a scale of its own for every block: values [M, K] and [N, K] in float64, and what the calls take, made
+    on the GPU.  n_exp, w_exp: ranges of the scales' exponents."""
+    import torch
+    from paper_2510_11331_amd import LinearQ
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M * 1000003 + N * 1009 + K)
+
+    def operand(R, R16, lo_hi, E_rows):
+        v = torch.zeros(R16, qref.up(K, 128), device="cuda")
+        v[:R, :K] = (60 * torch.randn(R, K, generator=g, device="cuda")).clamp(-448, 448)
+        v = v.to(torch.float8_e4m3fn)
+        E = torch.randint(*lo_hi, (E_rows, v.shape[1] // 128), generator=g, device="cuda")
+        exps = torch.zeros(E_rows, qref.up(E.shape[1], 4), dtype=torch.uint8, device="cuda")
+        exps[:, :E.shape[1]] = E
+        return v, E, exps
+
+    q, E, e = operand(M, M, n_exp, M)
+    v, F, f = operand(N, qref.up(N, 16), w_exp, -(-N // 128))
+    tiles = v.view(torch.uint8).view(v.shape[0] // 16, 16, -1, 2, 4, 16).permute(0, 2, 3, 4, 1, 5)
+    w = LinearQ(torch.cat([tiles.reshape(-1), f.reshape(-1)]), N, K)
+    scale = lambda E, n: torch.ldexp(torch.ones_like(E, dtype=torch.float64), E - 127).repeat_interleave(n, 0)
+    a = q.double().view(M, -1, 128) * scale(E, 1)[..., None]
+    b = v.double().view(v.shape[0], -1, 128) * scale(F, 128)[:v.shape[0], :, None]
+    return a.view(M, -1)[:, :K], b.view(v.shape[0], -1)[:N, :K], q, e.view(torch.float8_e8m0fnu), w
+
+
+def terms_gpu(a, b):
+    return host(a @ b.t().contiguous()), host(((a * a) @ (b * b).t().contiguous()).sqrt())
+
+
+@pytest.mark.parametrize("fast,rows,cols,ranges,M,N,K", qplans.LINEAR)
+def test_linear_plan(fast, rows, cols, ranges, M, N, K):
+    """Every kernel and number of K ranges, past the start of its loop, for both types, with an addend of the sum's size."""
+    import torch
+    from paper_2510_11331_amd import linear_q
+    say("linear plan", fast, rows, cols, ranges, M, N, K)
+    assert qplans.plan("linear", M, N, K, fast) == qplans.expected(fast, rows, cols, ranges, M)
+    a, b, q, e, w = codes8(M, N, K, (117, 121), (115, 120))
+    want, s = terms_gpu(a, b)
+    err = qsums.cut_error(s) if fast else qsums.sum_error(K, s)
+    for dtype in ("fp32", "bf16"):
+        assert qsums.product_ok(host(linear_q(q, e, w, dtype=dt(dtype), fast=bool(fast))), want, err, dtype)
+    add = torch.randn(M, N, device="cuda")
+    got = host(linear_q(q, e, w, add=add, fast=bool(fast)))
+    assert qsums.product_ok(got, want + host(add), err + 2 * qsums.STEP32 * np.abs(host(add)), "fp32")
+
+
+@pytest.mark.parametrize("fast,rows,cols,ranges,M,F,K", qplans.GATE_UP)
+def test_gate_up_plan(fast, rows, cols, ranges, M, F, K):
+    from paper_2510_11331_amd import gate_up_q
+    say("gate_up plan", fast, rows, cols, M, F, K)
+    assert qplans.plan("gate_up", M, F, K, fast) == qplans.expected(fast, rows, cols, ranges, M)
+    a, b, q, e, w = codes8(M, 2 * F, K, (117, 121), (115, 120))
+    p, s = terms_gpu(a, b)
+    err = qsums.cut_error(s) if fast else qsums.sum_error(K, s)
+    check_codes(gate_up_q(q, e, w, fast=bool(fast)), p, err)
