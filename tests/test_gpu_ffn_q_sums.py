@@ -149,3 +149,50 @@ def test_gate_up_plan(fast, rows, cols, ranges, M, F, K):
     p, s = terms_gpu(a, b)
     err = qsums.cut_error(s) if fast else qsums.sum_error(K, s)
     check_codes(gate_up_q(q, e, w, fast=bool(fast)), p, err)
+
+
+# ------------------------------------------------------------------ extreme scales
+
+
+@pytest.mark.parametrize("fast", [False, True])
+@pytest.mark.parametrize("M", [6, 100])
+def test_extreme_scales(M, fast):
+    """Rows whose blocks have scales of 2^-126 to 2^127, with nonzero codes in every block, and a weight with a large and
+    a small block of its own: the product of two blocks' scales is held within 2^-126 (a smaller one counts as zero) and 2^127."""
+    import torch
+    from paper_2510_11331_amd import LinearQ, linear_q
+    say("extreme scales", M, fast)
+    r = np.random.default_rng(M)
+    N, K = 300, 500
+    c, E = qref.quantise_rows(r.normal(size=(M, K)))
+    wc, wF = qref.quantise_weight(r.normal(size=(N, K)))
+    tiny = lambda shape: np.where(r.integers(0, 2, size=shape) == 1, 0x81, 0x01).astype(np.uint8)     # +- 2^-9
+    E, wF = E.copy(), wF.copy()
+    wF[:] = 118
+    wF[1], wF[2] = 140, 1                                      # rows 128 to 255 and 256 to 299 of the weight
+    wc[128:256] = tiny((128, K))
+    E[:] = 127
+    E[0] = 1                                                   # far below 2^-126
+    E[1] = 10                                                  # 10 + 118 - 254 = -126: the smallest that counts
+    E[2] = 9                                                   # the largest that does not
+    E[3] = 254                                                 # 254 + 140 - 254 = 140: held at 2^127
+    E[4] = [1, 10, 100, 120]                                   # beside each other
+    c[3] = np.where(np.arange(c.shape[1]) < K, tiny(c.shape[1]), 0)
+    e = E[:, :, None].astype(np.int64) + np.repeat(wF, 128, 0)[:N].T[None] - 254                      # [M, blocks, N]
+    if not fast or M <= 64:
+        e = np.where(e < -126, -5000, np.minimum(e, 127))
+    pad = lambda v: np.pad(v, ((0, 0), (0, 512 - K))).reshape(len(v), 4, 128)
+    a, b = pad(qref.value(c)[:, :K]), pad(qref.value(wc))
+    s = np.stack([a[:, k] @ b[:, k].T for k in range(4)], 1)                                          # [M, blocks, N]
+    root = np.stack([np.sqrt((a[:, k] ** 2) @ (b[:, k] ** 2).T) for k in range(4)], 1)
+    want, root = np.ldexp(s, e).sum(1), np.sqrt((np.ldexp(root, e) ** 2).sum(1))
+    # the 8-bit instruction takes the scales as they are: with 2^140 partial sums pass fp32's largest number, and may be infinite
+    over = 8 * root > 2.0 ** 128
+    assert not over[:3].any() and (fast and M > 64 or not over.any())
+    q, ex = t(c).view(torch.float8_e4m3fn), t(qref.exps_bytes(E)).view(torch.float8_e8m0fnu)
+    got = host(linear_q(q, ex, LinearQ(t(qref.pack(wc, wF)), N, K), fast=fast))
+    err = (qsums.cut_error(root) if fast and M > 64 else qsums.sum_error(K, root)) + 2.0 ** -149
+    got, want = np.where(over, 0, got), np.where(over, 0, want)
+    for i in range(M):                                         # each row is of a size of its own
+        for part in (slice(0, 128), slice(128, 256), slice(256, N)):
+            assert np.linalg.norm(got[i, part] - want[i, part]) <= np.linalg.norm(err[i, part]), (i, part)
