@@ -97,9 +97,10 @@ enum { SD_DTYPE_BF16 = 0, SD_DTYPE_F32 = 1, SD_DTYPE_BF16_FFN_Q = 2 };
  * only): as SD_DTYPE_BF16, but the feed-forward network runs in 8-bit floating
  * point (sd_add_rmsnorm_q, sd_gate_up_q, sd_linear_q below): wgu and wdown are
  * packed by sd_pack_linear_q, and the inputs of both products are rounded to
- * 8-bit rows.  Half the weight bytes of two thirds of the layer; each code is
- * within 2^-4 of its value.  d_model <= 16384; passes of more than 64 rows run
- * both products on the 8-bit matrix instruction. */
+ * 8-bit rows.  Half the weight bytes of two thirds of the layer; a code is within
+ * 2^-4 of its value, or within 2^-10 of its block's scale where that is more.
+ * d_model <= 16384; passes of more than 64 rows run both products on the 8-bit
+ * matrix instruction (sd_gate_up_q_fast, sd_linear_q_fast). */
 typedef struct {
     int n_layers, d_model, n_heads, n_kv_heads, head_dim, d_ffn, vocab;
     int dtype;              /* SD_DTYPE_*                                   */
@@ -344,8 +345,9 @@ int sd_pack_linear_q(const void *src, void *dst, int N, int K, int dtype, void *
  * entries (q, exps).  x [M, d] and add [n_add, M, d] (0 <= n_add <= 6) are of
  * dtype; with n_add > 0, s is written to x_out [M, d] in that type and the norm
  * is of the value written; x_out may be x (else it must not overlap an
- * input).  gain [d] is of gain_dtype.  Sums and the norm are taken in 64 bits, y
- * is rounded to fp32 and then to its code.  d <= 16384, eps > 0. */
+ * input).  gain [d] is of gain_dtype.  Sums and the norm are taken in 64 bits; s
+ * is rounded to fp32 and then to its type, y to fp32 and then to its code.  d <=
+ * 16384, eps > 0. */
 int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const void *add, void *x_out,
                     const void *gain, int gain_dtype, float eps, uint8_t *q, uint8_t *exps, void *stream);
 
@@ -355,8 +357,11 @@ int sd_add_rmsnorm_q(int M, int d, int dtype, const void *x, int n_add, const vo
  * Sums are in fp32, on fp16 operands (the codes' values, exactly), with the
  * product of two blocks' scales held within 2^-126 to 2^127 (below it counts as
  * 0).  sd_linear_q_fast: the same, but products of more than 64 rows run on
- * the 8-bit matrix instruction, which drops low bits of the products it adds (up
- * to 5e-5 of the outputs' root mean square).
+ * the 8-bit matrix instruction, with the scales as they are.  It takes about
+ * half the time and drops low bits of the products it adds: measured at 1.4e-5
+ * to 5.1e-5 of the outputs' 2-norm (256 x 256 outputs, K of 128 to 11008;
+ * normal rows 1.5e-5, the most with one entry of 30 times the others' size), single
+ * outputs at up to 1.1e-3 of their root mean square.
  * The workspace (16-byte aligned, sd_linear_q_workspace_bytes(M, N, K); where
  * that is 0, as on an invalid size, it may be NULL) is scratch of this call
  * alone until its work is done: calls that may overlap, graphs among them, need

@@ -105,9 +105,9 @@ __host__ __device__ __forceinline__ int range8(int kb, int ksplit) { return ((kb
 //
 // The products run on fp16 operands: a block's sum of exact fp32 products is
 // scaled and added in fp32.  The 8-bit matrix instruction drops low bits of
-// the products it adds (1.3e-5 of the sums for normal data, at any K, against
-// 1e-7 here; with 32 entries of K or 128 an instruction alike), which fp32
-// outputs would show.
+// the products it adds (1.5e-5 of the sums for normal data, at any K, up to 5.1e-5
+// for rows with a few large entries, against 1e-7 here; with 32 entries of K
+// or 128 an instruction alike), which fp32 outputs would show.
 //
 // 4096 x 11008: 8 rows 10.5 us (4.3 TB/s), 40 rows 15.7, 64 rows 18.8; gate/up
 // 22016 x 4096 without the codes' pass (3.5 us): 8 rows 17.5 us (5.2 TB/s), 40
@@ -713,7 +713,8 @@ struct Tile8Model {
   constexpr int bn() const { return 16 * nf * wn; }
 };
 static constexpr Tile8Model TILES8[] = {
-    // on the 8-bit matrix instruction, for callers that chose it
+    // on the 8-bit matrix instruction, for callers that chose it (2048 x 4096 x
+    // 11008, bf16 out: 82 us)
     {4, 4, 2, 4, 3, false, 1, 6.8f, 0.756f, 0.207f},    // 128 x 256
     {4, 2, 2, 4, 3, false, 1, 5.3f, 0.399f, 0.156f},    // 128 x 128
     {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.050f},    // 128 x 64
@@ -725,9 +726,9 @@ static constexpr Tile8Model TILES8[] = {
     {2, 2, 2, 2, 4, true, 2, 3.8f, 0.513f, 0.145f},     // 64 x 64
     // gate/up: 256 columns, the block of 128 outputs.  On the 8-bit matrix
     // instruction, for callers that chose it: its outputs are rounded to four
-    // significant bits, and the 5e-5 that it is off by moves under one code in a
-    // thousand across a border (2^-3 of its value; 2.4e-3 of all outputs' norm, of
-    // which the rounding to codes takes 2.5e-2)
+    // significant bits, and what it is off by moves under one code in a
+    // thousand across a border (2^-3 of its value; 1.8e-3 of all outputs' norm at
+    // 2048 x 22016 x 4096, of which the rounding to codes takes 2.5e-2)
     {8, 4, 2, 4, 2, false, 1, 11.6f, 1.264f, 0.378f},   // 256 x 256
     {6, 4, 2, 4, 2, false, 1, 7.2f, 1.072f, 0.356f},   // 192 x 256
     {4, 4, 2, 4, 3, false, 1, 8.8f, 0.731f, 0.161f},    // 128 x 256

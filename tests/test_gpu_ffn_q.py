@@ -217,7 +217,7 @@ def test_linear(M, N, K, dtype):
     check_product(got, want, mag, K, dtype)
 
 
-# The 8-bit matrix instruction, which bf16 outputs of many rows may run on, drops low bits of the products it adds: probed
+# The 8-bit matrix instruction, which products of many rows run on where the caller chose it, drops low bits of the products it adds: probed
 # at 2^-14 to 2^-16 of a sum's root mean square for any K; as a bound, 2^-12 of the terms' magnitudes
 CUT8 = 2.0 ** -12
 
