@@ -60,3 +60,21 @@ def test_plan_queries():
         assert L.sd_plan_linear_q(M, N, K, 0, C.byref(p)) == L.sd_plan_gate_up_q(M, N, K, 0, C.byref(p)) == _lib.SD_EINVAL
     assert L.sd_plan_gate_up_q(1, 24, 1, 0, C.byref(p)) == _lib.SD_EINVAL
     assert L.sd_plan_linear_q(1, 16, 1, 0, None) == L.sd_plan_gate_up_q(1, 16, 1, 0, None) == _lib.SD_EINVAL
+
+
+@needs_lib
+def test_fast_calls_refuse():
+    """What the plain calls refuse.  The pointers are never dereferenced."""
+    from paper_2510_11331_amd import _lib
+    L, E, A = _lib.lib(), _lib.SD_EINVAL, 1 << 20
+    n = L.sd_linear_q_workspace_bytes(100, 64, 11008)
+    ln = dict(M=100, N=64, K=11008, q=A, exps=A, w=A, add=A, out=A, ldo=64, dtype=_lib.SD_DTYPE_F32, ws=A, n=n)
+    for bad in (dict(M=-1), dict(N=0), dict(K=(1 << 18) + 1), dict(q=None), dict(out=None), dict(ldo=63), dict(dtype=2), dict(w=A + 8),
+                dict(add=A + 2), dict(ws=None), dict(n=n - 1), dict(exps=A + 2)):
+        assert L.sd_linear_q_fast(*{**ln, **bad}.values(), None) == E, bad
+    assert L.sd_linear_q_fast(*{**ln, "M": 0, "out": None}.values(), None) == _lib.SD_OK
+    n = L.sd_gate_up_q_workspace_bytes(2, 64, 64)
+    gu = dict(M=2, F=64, K=64, q=A, exps=A, w=A, q_out=A, exps_out=A, ws=A, n=n)
+    for bad in (dict(M=-1), dict(F=72), dict(K=0), dict(w=None), dict(exps_out=None), dict(ws=None), dict(n=n - 1), dict(q_out=A + 8)):
+        assert L.sd_gate_up_q_fast(*{**gu, **bad}.values(), None) == E, bad
+    assert L.sd_gate_up_q_fast(*{**gu, "M": 0, "q": None}.values(), None) == _lib.SD_OK

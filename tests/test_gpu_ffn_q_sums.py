@@ -196,3 +196,41 @@ def test_extreme_scales(M, fast):
     for i in range(M):                                         # each row is of a size of its own
         for part in (slice(0, 128), slice(128, 256), slice(256, N)):
             assert np.linalg.norm(got[i, part] - want[i, part]) <= np.linalg.norm(err[i, part]), (i, part)
+
+
+# ------------------------------------------------------------------ the caller's choice
+
+
+@pytest.mark.parametrize("M", [64, 300])
+def test_fast_on_streams_and_in_graphs(M):
+    """fast goes along to another stream and into a graph, with K in ranges and without; up to 64 rows it changes nothing, above
+    it is another result; each replay is the eager call's, bit for bit."""
+    import torch
+    from paper_2510_11331_amd import gate_up_q, linear_q
+    say("fast on streams", M)
+    gu, down = codes8(M, 2 * 528, 1110, (117, 121), (115, 120))[2:], codes8(M, 520, 6000, (117, 121), (115, 120))[2:]
+    assert M == 64 or qplans.plan("linear", M, 520, 6000, 1)[4] > 1
+
+    def both(fast, stream=None):
+        return [x.view(torch.uint8) if x.element_size() == 1 else x
+                for x in (*gate_up_q(*gu, stream=stream, fast=fast), linear_q(*down, stream=stream, fast=fast),
+                          linear_q(*down, dtype=torch.bfloat16, stream=stream, fast=fast))]
+
+    same = lambda a, b: all(torch.equal(x, y) for x, y in zip(a, b))
+    exact, want = both(False), both(True)
+    assert same(exact, want) == (M <= 64)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    got = both(True, other)
+    torch.cuda.synchronize()
+    assert same(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = both(True)
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        eager = both(True), both(False)
+        torch.cuda.synchronize()
+        assert same(outs, want) and same(eager[0], want) and same(eager[1], exact)
