@@ -110,7 +110,7 @@ __host__ __device__ __forceinline__ int range8(int kb, int ksplit) { return ((kb
 // or 128 an instruction alike), which fp32 outputs would show.
 //
 // 4096 x 11008: 8 rows 10.5 us (4.3 TB/s), 40 rows 15.7, 64 rows 18.8; gate/up
-// 22016 x 4096 without the codes' pass (3.5 us): 8 rows 17.5 us (5.2 TB/s), 40
+// 22016 x 4096 without the codes' pass (3 to 5 us): 8 rows 17.5 us (5.2 TB/s), 40
 // rows 19.3.  A plain read of the bytes reaches 6.3 to 6.8 TB/s; what grows with
 // the rows is their reads from L2, once per workgroup.
 constexpr int STREAM8_KE = 128;          // bytes of a row's scales: K up to 16384
@@ -316,10 +316,15 @@ __global__ __launch_bounds__(64 * KW) void gemm8_kernel(Gemm8Params p) {
 // from LDS, whose reads take as long as the products (8192 rows 645 us, 2048 rows
 // 220 -> 184 in the same graph).
 //
-// 2048 x 4096 x 11008, bf16 out: 79 us, 2.35 PFLOP/s of the 2.64 of a large
-// library product (in a graph of such calls 90, of which its loads alone would
-// take 78 and its LDS reads and products alone 80); gate/up 2048 x 22016 x 4096:
-// 169 us, 2.19 PFLOP/s.
+// On the 8-bit instruction 2048 x 4096 x 11008, bf16 out: 82 us, 2.26 PFLOP/s of the
+// 2.64 of a large library product (in a graph of such calls 91, of which its loads
+// alone would take 78 and its LDS reads and products alone 80); gate/up 2048 x
+// 22016 x 4096: 178 us, 2.08 PFLOP/s.
+//
+// On fp16 operands 155 us and 359 us, 1.2 and 1.03 PFLOP/s of the 1.56 of a large
+// library product: the matrix units are busy 0.48 of the cycles (of the first), the
+// other vector instructions (3.7 for each matrix instruction: widening, scaling,
+// addresses) issue in 0.44, and the waves wait a quarter of theirs for loads.
 template <int MF_, int NF_, int WM_, int WN_, int NB_, bool EXACT_> struct Tile8 {
   static constexpr int MF = MF_, NF = NF_, WM = WM_, WN = WN_, NB = NB_;
   static constexpr bool EXACT = EXACT_;
@@ -694,11 +699,13 @@ template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipSt
   }
 }
 
-// The row tiles and the time model that picks one of a list, and a number of K
-// ranges: a round of workgroups takes e microseconds for its start and epilogue,
-// and a + c w for every stage, w the workgroups per CU (up to per_cu; less than
-// one in a last round that does not fill the card).  K ranges add the pass that
-// sums them.  Fitted to 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008
+// The row tiles and the model that picks one of a list, and a number of K
+// ranges: a round of workgroups takes e for its start and epilogue, and a + c w for
+// every stage, w the workgroups per CU (up to per_cu; less than one in a last
+// round that does not fill the card).  K ranges add the pass that sums them.  The
+// coefficients are about microseconds, but set for the right choice, not the right
+// time: with fp16 operands a measured time is up to 1.9 times the model's (2048 x
+// 4096 x 2816), and one of them changed alone ranks its tile wrongly.  Fitted to 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008
 // (weights from HBM); against the fastest of all tiles and of 1, 2 and 4 K ranges
 // the choice is on average 0.4 % slower for the 8-bit instruction (360 shapes with
 // bf16 outputs, the worst 31 %), 0.8 % for fp16 operands (304 with fp32 ones, the
@@ -720,7 +727,7 @@ static constexpr Tile8Model TILES8[] = {
     {2, 2, 4, 2, 4, false, 1, 3.4f, 0.346f, 0.050f},    // 128 x 64
     {2, 2, 2, 2, 4, false, 2, 3.1f, 0.227f, 0.138f},    // 64 x 64
     {8, 4, 2, 4, 2, false, 1, 10.3f, 1.111f, 0.446f},   // 256 x 256
-    // on fp16 operands (2048 x 4096 x 11008, bf16 out: 158 us against 82)
+    // on fp16 operands (2048 x 4096 x 11008, bf16 out: 155 us)
     {4, 4, 2, 4, 3, true, 1, 4.5f, 0.968f, 0.223f},     // 128 x 256
     {2, 2, 2, 4, 3, true, 2, 4.3f, 0.554f, 0.174f},     // 64 x 128
     {2, 2, 2, 2, 4, true, 2, 3.8f, 0.513f, 0.145f},     // 64 x 64
@@ -733,7 +740,7 @@ static constexpr Tile8Model TILES8[] = {
     {6, 4, 2, 4, 2, false, 1, 7.2f, 1.072f, 0.356f},   // 192 x 256
     {4, 4, 2, 4, 3, false, 1, 8.8f, 0.731f, 0.161f},    // 128 x 256
     {2, 4, 2, 4, 3, false, 1, 6.1f, 0.550f, 0.054f},    // 64 x 256
-    // gate/up on fp16 operands (of 2048 x 22016 x 4096 361 us against 178; 446 measured
+    // gate/up on fp16 operands (2048 x 22016 x 4096 359 us against 178; 446 measured
     // calls of 65 to 4096 rows: the choice is on average 0.06 % slower than the
     // faster of the two, the worst 4 %)
     {4, 4, 2, 4, 3, true, 1, 9.2f, 1.530f, 0.242f},     // 128 x 256
@@ -767,7 +774,8 @@ static Gemm8Plan pick_tile8(int lo, int hi, int M, int N, int K, int max_ksplit)
 }
 
 // Up to 64 rows the streaming kernel, above (and past the scales it holds in LDS) row tiles.
-// Up to 64 rows sums are exact on both
+// Up to 64 rows sums are exact on both.  (Past K = 16384 the row tiles compute 64 rows
+// for one: 4096 columns, 8 rows, K = 16384 14.1 us, 28672 49.3)
 constexpr int FEW8 = 64;
 static bool streams8(int M, int K) { return M <= FEW8 && ke8(K) <= STREAM8_KE; }
 bool gate_up8_fused(int M, int K) { return !streams8(M, K); }

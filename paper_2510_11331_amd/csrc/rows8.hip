@@ -59,7 +59,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* row, i
 
 // Residual addition, RMSNorm and 8-bit output of one row per workgroup (R units
 // of eight entries a thread, a block's 128 entries in 16 neighbouring lanes):
-//   s = x + add_0 + ... + add_{n-1}         summed in 64 bits, stored in x's type
+//   s = x + add_0 + ... + add_{n-1}         summed in 64 bits, stored in x's type (by way of fp32)
 //   y = s / sqrt(mean(s^2) + eps) * gain    in 64 bits, rounded to fp32
 //   q, E = codes and exponents of y
 // 64-bit sums and norm: codes are a function of the input alone, not of the
@@ -70,6 +70,12 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* row, i
 // trips.  Sixteen bytes a load (eight before: 24.2 us at 2048 x 5120).  All
 // addends are loaded before the first is added (NS of them, those past n_add as
 // zeros).
+// Two addends take the code of six, and no time by it: 2048 x 8192 fp32 with six
+// 112 us, 5.0 TB/s.  What 128 registers do not hold goes to scratch: six addends of
+// four units (d past 8192, two or more addends) 70 to 300 registers, 2048 x
+// 16384 fp32 with two 379 us, 1.5 TB/s; and rows that are read entry by entry (d no
+// multiple of 8, or off 16 bytes) with two or more addends 270 to 800 of them from
+// d = 2049 on, 2048 x 4096 fp32 with two 214 us against 32.
 template <typename TX, typename TG, int R, int NS, bool VEC>
 __global__ __launch_bounds__(R == 1 ? 256 : 512, 4) void add_rmsnorm8_kernel(Norm8Params p) {
   __shared__ double red[8];
@@ -155,7 +161,7 @@ __global__ __launch_bounds__(256) void quantise_rows8_kernel(const float* h, uin
 // One 128 x 128 block per workgroup: 16 lanes read the 128 entries of a row
 // (lanes across rows, as the packed order has them, would touch a line each),
 // the codes are put in order in LDS and leave as the block's eight 2 KB tiles.
-// 22016 x 4096 bf16: 55.7 us, 4.9 TB/s (78 us with lanes across rows).
+// 22016 x 4096 bf16: 54.3 us, 5.0 TB/s (78 us with lanes across rows); fp32 84 us, 5.35.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void pack_linear8_kernel(const T* src, uint8_t* dst, int N, int K) {
   __shared__ __attribute__((aligned(16))) uint8_t out[8 * 2048];
