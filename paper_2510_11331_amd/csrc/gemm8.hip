@@ -705,12 +705,13 @@ template <int EPI> static hipError_t gemm8_m(int nt, const Gemm8Params& p, hipSt
 // round that does not fill the card).  K ranges add the pass that sums them.  The
 // coefficients are about microseconds, but set for the right choice, not the right
 // time: with fp16 operands a measured time is up to 1.9 times the model's (2048 x
-// 4096 x 2816), and one of them changed alone ranks its tile wrongly.  Fitted to 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008
-// (weights from HBM); against the fastest of all tiles and of 1, 2 and 4 K ranges
-// the choice is on average 0.4 % slower for the 8-bit instruction (360 shapes with
-// bf16 outputs, the worst 31 %), 0.8 % for fp16 operands (304 with fp32 ones, the
-// worst 14 %) and 0.03 % for gate/up on the 8-bit instruction (405, the worst 5 %).
-// One K range for all would cost 5 % and 17 %.
+// 4096 x 2816), and one of them changed alone ranks its tile wrongly.  Fitted to
+// 65 to 8192 rows, N of 512 to 11008 and K of 1024 to 11008 (weights from HBM);
+// against the fastest of all tiles and of 1, 2 and 4 K ranges the choice is on
+// average 0.4 % slower for the 8-bit instruction (360 shapes with bf16 outputs, the
+// worst 31 %), 0.8 % for fp16 operands (304 with fp32 ones, the worst 14 %) and
+// 0.03 % for gate/up on the 8-bit instruction (405, the worst 5 %).  One K range
+// for all would cost 5 % and 17 %.
 struct Tile8Model {
   int mf, nf, wm, wn, nb;   // Tile8
   bool exact;
@@ -823,9 +824,13 @@ hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p0, h
   p.wide = p.ldo % 4 == 0 && (uintptr_t)p.out % (p.bf16 ? 8 : 16) == 0 && (uintptr_t)p.add % 16 == 0;
   p.ksplit = 1;
   if (epi == EPI8_SWIGLU_Q) {
-    return p.N % 32 || !plan.rows ? hipErrorInvalidValue : gemm8_rows_at<EPI8_SWIGLU_Q, TILES8_GATE_UP, TILES8_END>(plan.tile, p, s);
+    if (p.N % 32 || !plan.rows) return hipErrorInvalidValue;
+    return gemm8_rows_at<EPI8_SWIGLU_Q, TILES8_GATE_UP, TILES8_END>(plan.tile, p, s);
   }
-  if (epi == EPI8_SWIGLU) return p.N % 32 || plan.rows || !streams8(p.M, p.K) ? hipErrorInvalidValue : gemm8_m<EPI8_SWIGLU>(plan.tile, p, s);
+  if (epi == EPI8_SWIGLU) {
+    if (p.N % 32 || plan.rows || !streams8(p.M, p.K)) return hipErrorInvalidValue;
+    return gemm8_m<EPI8_SWIGLU>(plan.tile, p, s);
+  }
   if (epi != EPI8_STORE && epi != EPI8_PART) return hipErrorInvalidValue;
   if (!plan.rows && !streams8(p.M, p.K)) return hipErrorInvalidValue;
   if (plan.ksplit == 1) {

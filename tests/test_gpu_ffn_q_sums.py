@@ -5,6 +5,7 @@ import pytest
 import qplans
 import qref
 import qsums
+import test_gpu_ffn_q as plain
 from sdcase import say
 
 pytestmark = pytest.mark.gpu
@@ -234,3 +235,39 @@ def test_fast_on_streams_and_in_graphs(M):
         eager = both(True), both(False)
         torch.cuda.synchronize()
         assert same(outs, want) and same(eager[0], want) and same(eager[1], exact)
+
+
+@pytest.fixture
+def all_fast(monkeypatch):
+    """The public calls with fast=True, and the library's fast calls in the place of the others."""
+    import functools
+    import paper_2510_11331_amd as P
+    monkeypatch.setattr(P, "linear_q", functools.partial(P.linear_q, fast=True))
+    monkeypatch.setattr(P, "gate_up_q", functools.partial(P.gate_up_q, fast=True))
+    from paper_2510_11331_amd import _lib
+    L = _lib.lib()
+    for name in ("sd_linear_q", "sd_gate_up_q"):
+        monkeypatch.setattr(L, name, getattr(L, name + "_fast"))
+
+
+@pytest.mark.parametrize("name,args", [
+    ("test_linear", (65, 144, 384, "bf16")), ("test_linear", (257, 129, 1100, "bf16")), ("test_linear_add_and_strides", (200, "bf16")),
+    ("test_linear_offsets_past_32_bits", ()), ("test_gate_up", (130, 272, 700)), ("test_gate_up", (300, 1040, 260)), ("test_layer", (130, 512, 1408)),
+    ("test_streams_and_graphs", ()), ("test_only_its_own_memory", (300,)), ("test_scale_of_nan", (100,)), ("test_gate_up_nan_row", (100,)),
+    ("test_ranges_in_graphs", ())])
+def test_fast_borders(all_fast, name, args):
+    """The plain calls' tests of strides, untouched memory, NaN, offsets past 32 bits and graphs, of the fast ones (fp32 outputs are
+    bounded in test_linear_plan)."""
+    getattr(plain, name)(*args)
+
+
+def test_fast_nan_code(all_fast):
+    """A NaN code makes NaN of its row's outputs and no others."""
+    import torch
+    from paper_2510_11331_amd import linear_q
+    say("fast, a NaN code")
+    _, _, q, e, w = codes8(100, 300, 700, (117, 121), (115, 120))
+    q.view(torch.uint8)[7, 650] = 0xff
+    for dtype in (torch.float32, torch.bfloat16):
+        nan = np.isnan(host(linear_q(q, e, w, dtype=dtype)))
+        assert nan[7].all() and nan.sum() == 300
