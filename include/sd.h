@@ -397,6 +397,105 @@ typedef struct sd_linear_q_plan {
 int sd_plan_linear_q(int M, int N, int K, int fast, sd_linear_q_plan *out);
 int sd_plan_gate_up_q(int M, int F, int K, int fast, sd_linear_q_plan *out);
 
+/* ---- Attention over a KV cache held in 4 bits (eqs. d_kv, d_atte with 4-bit
+ * keys and values), and what writes that cache.  Context-free like the 8-bit
+ * calls above, and as safe to capture and to call from several streams at once;
+ * calls on one pool or workspace are ordered by the caller.
+ *
+ * Format.  Numbers are e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives, code + 8) with a power-of-two scale 2^(E - 127), E a byte, per
+ * 32 dimensions of one token and head.  E is the smallest E >= 1 with amax <= 6
+ * 2^(E - 127), amax the block's largest magnitude; a code is the value times
+ * 2^(127 - E) rounded to nearest even (fp32 values past 1.75 2^127 become
+ * infinities).  A block with a NaN or an infinity gets E = 255 and reads as NaN.
+ *   Pool  uint8 [n_blocks, n_kv_heads, 17 head_dim], 16-byte aligned; head_dim
+ *     64 or 128.  A page holds 16 tokens; of one head: key codes [16 tokens]
+ *     [head_dim / 2], value codes [token / 4][16][token % 4][head_dim / 32],
+ *     key scales [16 tokens][head_dim / 32], value scales [head_dim / 32][16
+ *     tokens].  Two dimensions share a byte, the even one its low half.
+ *   Rows  Sequence b of a pass has the rows cu_rows[b] .. cu_rows[b + 1] - 1
+ *     (cu_rows [n_seqs + 1] ascending from 0, at most M) and, with them,
+ *     lengths[b] tokens: row r is at position lengths[b] - cu_rows[b + 1] + r,
+ *     token position % 16 of page table[b, position / 16].  Rows at or behind
+ *     cu_rows[n_seqs] are of no sequence: they are not read, and what belongs
+ *     to them is left as it was.  The three arrays are int32 on the device, so
+ *     that a captured call follows what they hold.
+ *     A position before the first, behind the table's width or whose table
+ *     entry is no page of the pool has no token: it is not written, and reads
+ *     as NaN.
+ * In every call q, k, v and the outputs are rows of heads of head_dim adjacent
+ * entries, of dtype (SD_DTYPE_BF16 or SD_DTYPE_F32); ld* are row strides in
+ * entries (at least heads head_dim).  Addresses are 16-byte aligned, strides a
+ * multiple of 16 bytes.  1 <= n_kv_heads <= 1024, n_heads a multiple of it, at
+ * most 1024 (0 where queries are left out), n_blocks <= 2^24, table_width <=
+ * 2^20, 0 <= n_seqs <= 2^20, 0 <= M <= 2^20 (M = 0 and n_seqs = 0 enqueue
+ * nothing and read no pointer). */
+typedef struct sd_kv_q_pool {
+    void *data;
+    int n_blocks, n_kv_heads, head_dim;
+} sd_kv_q_pool;
+typedef struct sd_kv_rows {
+    const int32_t *cu_rows, *lengths, *table;
+    int n_seqs, table_width;
+} sd_kv_rows;
+/* Norms and rotation of heads: y = x / sqrt(mean(x^2) + eps) * gain over the
+ * head_dim entries of a head (gain [head_dim] of gain_dtype, or NULL: no norm),
+ * then entries i and i + head_dim / 2 are rotated by the angle whose (cos, sin)
+ * is rope[position, i] (rope fp32 [n_pos, head_dim / 2, 2], 16-byte aligned; or
+ * NULL: no rotation).  Computed in 64 bits, rounded to fp32 and from there to
+ * its type or its code.  Positions outside the table make NaN. */
+typedef struct sd_head_norm {
+    const void *q_gain, *k_gain;
+    const float *rope;
+    int gain_dtype, n_pos;
+    float eps;              /* > 0 with a gain                              */
+} sd_head_norm;
+
+/* Bytes of a pool (0 on an invalid size). */
+size_t sd_kv_q_bytes(int n_blocks, int n_kv_heads, int head_dim);
+
+/* rope [n_pos, head_dim / 2, 2] = (cos, sin) of position theta^(-2 i /
+ * head_dim), the angle in 64 bits.  theta > 0, n_pos <= 2^24. */
+int sd_rope_table(int n_pos, int head_dim, double theta, float *rope, void *stream);
+
+/* Norms and rotation of queries and keys: row r at positions[r] (NULL without
+ * rotation).  The outputs may be the inputs (with their strides), else they do
+ * not overlap. */
+int sd_norm_rope(int M, int n_heads, int n_kv_heads, int head_dim, int dtype, const void *q, int ldq, const void *k,
+                 int ldk, const int32_t *positions, const sd_head_norm *norm, void *q_out, int ldq_out, void *k_out,
+                 int ldk_out, void *stream);
+
+/* Keys and values of a pass's rows into the pool.  No two rows may share a
+ * page and token. */
+int sd_kv_append_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int dtype, const void *k, int ldk,
+                   const void *v, int ldv, void *stream);
+
+/* sd_norm_rope of queries and keys at the rows' positions, the keys (their
+ * fp32 values) and v going into the pool: what a layer does between its QKV
+ * product and its attention. */
+int sd_norm_rope_append_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int n_heads, int dtype, const void *q,
+                          int ldq, const void *k, int ldk, const void *v, int ldv, const sd_head_norm *norm, void *q_out,
+                          int ldq_out, void *stream);
+
+/* Keys and values at the rows' positions out of the pool (exact in fp32, and
+ * in bf16 but for scales at its range's ends). */
+int sd_kv_read_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int dtype, void *k, int ldk, void *v, int ldv,
+                 void *stream);
+
+/* out = softmax(scale q K^T) V of every row and head; query head h uses kv
+ * head h n_kv_heads / n_heads.  causal: a row sees the positions up to its
+ * own, else all lengths[b] of its sequence (whose rows then need no position).
+ * A row that sees nothing is zero.  NaN and infinities in positions that a row
+ * does not see do not reach it; a NaN that it sees is in its output as
+ * the formula has it (a key's in all of a head, a value block's in its 32
+ * dimensions).  Sums and the softmax are in fp32.  out may not overlap q.  A length may
+ * be anything up to 16 table_width: max_len (0: the table's width) only says
+ * for which lengths the work is split. */
+size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len);
+int sd_attention_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int n_heads, int dtype, const void *q, int ldq,
+                   void *out, int ldo, int causal, float scale, int max_len, void *workspace, size_t workspace_bytes,
+                   void *stream);
+
 /* Copy slot state to out [B, 4] int32 (device): committed target length
  * P, next input token x0, pending draft input (-1 if none), KV capacity. */
 int sd_slot_state(sd_ctx *ctx, int B, const int32_t *slots, int32_t *out,

@@ -22,7 +22,8 @@ EXPORTS = ("sd_kv_pool_bytes", "sd_workspace_bytes", "sd_plan_projection", "sd_i
            "sd_check", "sd_profile", "sd_profile_read", "sd_destroy", "sd_strerror", "sd_last_error",
            "sd_pack_linear", "sd_linear_q_bytes", "sd_linear_q_workspace_bytes", "sd_pack_linear_q", "sd_add_rmsnorm_q", "sd_linear_q",
            "sd_linear_q_fast", "sd_gate_up_q_workspace_bytes", "sd_gate_up_q", "sd_gate_up_q_fast",
-           "sd_plan_linear_q", "sd_plan_gate_up_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
+           "sd_plan_linear_q", "sd_plan_gate_up_q", "sd_kv_q_bytes", "sd_rope_table", "sd_norm_rope", "sd_kv_append_q",
+           "sd_norm_rope_append_q", "sd_kv_read_q", "sd_attention_q_workspace_bytes", "sd_attention_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
 
 
 class ModelCfg(C.Structure):
@@ -59,6 +60,19 @@ class ProjPlan(C.Structure):
 
 class LinearQPlan(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("streamed", "matrix8", "rows", "cols", "k_ranges")]
+
+
+class KvQPool(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int) for n in ("n_blocks", "n_kv_heads", "head_dim")]
+
+
+class KvRows(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("cu_rows", "lengths", "table")] + [("n_seqs", C.c_int), ("table_width", C.c_int)]
+
+
+class HeadNorm(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q_gain", "k_gain", "rope")] + [("gain_dtype", C.c_int), ("n_pos", C.c_int),
+                                                                          ("eps", C.c_float)]
 
 
 class SchedModel(C.Structure):
@@ -131,6 +145,14 @@ def lib():
         "sd_gate_up_q_fast": (I, [I, I, I, P, P, P, P, P, P, C.c_size_t, P]),
         "sd_plan_linear_q": (I, [I, I, I, I, C.POINTER(LinearQPlan)]),
         "sd_plan_gate_up_q": (I, [I, I, I, I, C.POINTER(LinearQPlan)]),
+        "sd_kv_q_bytes": (C.c_size_t, [I, I, I]),
+        "sd_rope_table": (I, [I, I, C.c_double, P, P]),
+        "sd_norm_rope": (I, [I, I, I, I, I, P, I, P, I, P, P, P, I, P, I, P]),
+        "sd_kv_append_q": (I, [P, P, I, I, P, I, P, I, P]),
+        "sd_norm_rope_append_q": (I, [P, P, I, I, I, P, I, P, I, P, I, P, P, I, P]),
+        "sd_kv_read_q": (I, [P, P, I, I, P, I, P, I, P]),
+        "sd_attention_q_workspace_bytes": (C.c_size_t, [I, I, I, I, I, I]),
+        "sd_attention_q": (I, [P, P, I, I, I, P, I, P, I, I, F, I, P, C.c_size_t, P]),
         "sd_sched_latency": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32), I,
                                  C.POINTER(C.c_double)]),
         "sd_sched_batching": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32),

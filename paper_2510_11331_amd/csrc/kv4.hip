@@ -1,0 +1,206 @@
+// What lies between a layer's QKV product and its attention over a 4-bit cache
+// (format: codes4.h): the RMS norm of every query and key head and the rotary
+// embedding, the quantisation of keys and values into their pages, and the
+// reverse.
+//
+//   y = x / sqrt(mean(x^2) + eps) gain      over the hd entries of a head
+//   (y_i, y_{i + hd/2}) -> (y_i c - y_{i + hd/2} s, y_{i + hd/2} c + y_i s)
+//
+// Everything is bound by memory (a value is read once and written once; about
+// seven operations on it).  hd / 16 lanes take a head, a lane the 8 entries
+// from 8 i and the 8 from hd / 2 + 8 i: the two entries that a rotation mixes
+// are in one lane, a scale's block of 32 in four neighbouring ones, and every
+// access to a row is of 16 bytes.  The norm and the rotation are in 64 bits,
+// which the vector unit does at the rate of 32: a code is then a function of
+// the input alone, not of an order of sums.  What is stored is rounded to fp32
+// and from there to its type or its code; the first step is off by 2^-24.
+#include "codes4.h"
+
+namespace sd {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    const u32x4 u = *(const u32x4*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
+  } else {
+    const u32x4 u = ((const u32x4*)p)[0], w = ((const u32x4*)p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[e] = __uint_as_float(u[e]);
+      x[4 + e] = __uint_as_float(w[e]);
+    }
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    u32x4 u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * e], (__bf16)x[2 * e + 1]});
+    *(u32x4*)p = u;
+  } else {
+    ((u32x4*)p)[0] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+    ((u32x4*)p)[1] = u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
+  }
+}
+
+// 8 entries of a gain (aligned to its entries only)
+__device__ __forceinline__ void gain8(const void* g, int bf16, int i, double (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = bf16 ? bf2f(((const bf16_t*)g)[i + e]) : ((const float*)g)[i + e];
+}
+
+template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) void kv4_kernel(Kv4Params p) {
+  using P = Page4<HD>;
+  constexpr int LANES = HD / 16;
+  const int per_row = (MODE == KV4_HEADS || MODE == KV4_BOTH ? p.H : 0) + (MODE == KV4_HEADS ? 1 : 2) * p.KV;
+  const int64_t item = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int i = threadIdx.x % LANES;
+  if (item >= (int64_t)p.M * per_row) return;    // whole heads: the shuffles below stay within one
+  const int row = (int)(item / per_row), h0 = (int)(item % per_row);
+  const int nq = MODE == KV4_HEADS || MODE == KV4_BOTH ? p.H : 0;
+  const int what = h0 < nq ? 0 : h0 < nq + p.KV ? 1 : 2;      // query, key, value
+  const int h = what == 0 ? h0 : what == 1 ? h0 - nq : h0 - nq - p.KV;
+
+  int b = 0, pos = 0, page = -1;
+  if constexpr (MODE == KV4_HEADS) {
+    if (p.positions) pos = p.positions[row];
+  } else {
+    if (!row_place(p.rows, row, b, pos)) return;
+    page = what ? row_page(p.rows, b, pos, p.n_blocks) : -1;
+  }
+  const int t = pos & 15;
+  uint8_t* const pg = p.pool + ((size_t)max(page, 0) * p.KV + h) * P::BYTES;
+
+  float x[2][8];
+  if constexpr (MODE == KV4_READ) {
+    T* const out = (T*)(what == 1 ? p.k_out : p.v_out) + (size_t)row * (what == 1 ? p.ldko : p.ldvo) + h * HD;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int d = half * (HD / 2) + 8 * i;
+      uint32_t c = 0, E = 255;
+      if (page >= 0) {
+        if (what == 1) {
+          c = *(const uint32_t*)(pg + P::key(t, d));
+          E = pg[P::key_scale(t, d / 32)];
+        } else {
+          if constexpr (HD == 128) {
+            c = *(const uint32_t*)(pg + P::value(t, d / 8));
+          } else {
+            c = *(const uint16_t*)(pg + P::value(t, d / 4)) | (uint32_t)*(const uint16_t*)(pg + P::value(t, d / 4 + 1)) << 16;
+          }
+          E = pg[P::value_scale(t, d / 32)];
+        }
+      }
+      decode4(c, scale4(E), x[half]);
+      store8(out + d, x[half]);
+    }
+    return;
+  }
+
+  const T* const src = what == 0   ? (const T*)p.q + (size_t)row * p.ldq
+                       : what == 1 ? (const T*)p.k + (size_t)row * p.ldk
+                                   : (const T*)p.v + (size_t)row * p.ldv;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) load8(src + h * HD + half * (HD / 2) + 8 * i, x[half]);
+
+  if (MODE != KV4_APPEND && what != 2) {
+    double y[2][8];
+    double r = 1.0;
+    const void* const gain = what == 0 ? p.q_gain : p.k_gain;
+    if (gain) {
+      double sum = 0.0;
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += (double)x[half][e] * x[half][e];
+#pragma unroll
+      for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+      r = 1.0 / sqrt(sum / HD + p.eps);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      double g[8];
+      if (gain) gain8(gain, p.gain_bf16, half * (HD / 2) + 8 * i, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[half][e] = gain ? x[half][e] * r * g[e] : x[half][e];
+    }
+    if (p.rope) {
+      const bool in = (unsigned)pos < (unsigned)p.n_pos;
+      const float4* const cs = (const float4*)(p.rope + ((size_t)(in ? pos : 0) * (HD / 2) + 8 * i) * 2);
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        float4 w = cs[e / 2];
+        if (!in) w = make_float4(NAN, NAN, NAN, NAN);
+        const double a0 = y[0][e], b0 = y[1][e], a1 = y[0][e + 1], b1 = y[1][e + 1];
+        y[0][e] = a0 * w.x - b0 * w.y;
+        y[1][e] = b0 * w.x + a0 * w.y;
+        y[0][e + 1] = a1 * w.z - b1 * w.w;
+        y[1][e + 1] = b1 * w.z + a1 * w.w;
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[half][e] = (float)y[half][e];
+    if (MODE == KV4_HEADS || what == 0) {
+      T* const out = what == 0 ? (T*)p.q_out + (size_t)row * p.ldqo : (T*)p.k_out + (size_t)row * p.ldko;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) store8(out + h * HD + half * (HD / 2) + 8 * i, x[half]);
+    }
+  }
+  if (MODE == KV4_HEADS || what == 0) return;
+
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int d = half * (HD / 2) + 8 * i;
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[half][e]) & 0x7fffffffu);   // NaN is past infinity
+    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+    amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+    const uint32_t E = block_exp4(amax), c = encode4(x[half], E);
+    if (page < 0) continue;
+    if (what == 1) {
+      *(uint32_t*)(pg + P::key(t, d)) = c;
+      if (i % 4 == 0) pg[P::key_scale(t, d / 32)] = (uint8_t)E;
+    } else {
+      if constexpr (HD == 128) {
+        *(uint32_t*)(pg + P::value(t, d / 8)) = c;
+      } else {
+        *(uint16_t*)(pg + P::value(t, d / 4)) = (uint16_t)c;
+        *(uint16_t*)(pg + P::value(t, d / 4 + 1)) = (uint16_t)(c >> 16);
+      }
+      if (i % 4 == 0) pg[P::value_scale(t, d / 32)] = (uint8_t)E;
+    }
+  }
+}
+
+template <typename T, int HD> static void launch_mode(Kv4Mode mode, const Kv4Params& p, hipStream_t s) {
+  const int per_row = (mode == KV4_HEADS || mode == KV4_BOTH ? p.H : 0) + (mode == KV4_HEADS ? 1 : 2) * p.KV;
+  const int64_t items = (int64_t)p.M * per_row;
+  constexpr int each = 256 / (HD / 16);
+  const dim3 grid((unsigned)((items + each - 1) / each));
+  switch (mode) {
+    case KV4_HEADS: kv4_kernel<T, HD, KV4_HEADS><<<grid, 256, 0, s>>>(p); break;
+    case KV4_APPEND: kv4_kernel<T, HD, KV4_APPEND><<<grid, 256, 0, s>>>(p); break;
+    case KV4_BOTH: kv4_kernel<T, HD, KV4_BOTH><<<grid, 256, 0, s>>>(p); break;
+    case KV4_READ: kv4_kernel<T, HD, KV4_READ><<<grid, 256, 0, s>>>(p); break;
+  }
+}
+
+hipError_t launch_kv4(Kv4Mode mode, int dtype, int hd, const Kv4Params& p, hipStream_t s) {
+  if (dtype == 1) {
+    if (hd == 128) launch_mode<float, 128>(mode, p, s);
+    else launch_mode<float, 64>(mode, p, s);
+  } else {
+    if (hd == 128) launch_mode<bf16_t, 128>(mode, p, s);
+    else launch_mode<bf16_t, 64>(mode, p, s);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace sd

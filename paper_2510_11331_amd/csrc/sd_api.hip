@@ -1390,6 +1390,184 @@ int sd_gate_up_q_fast(int M, int F, int K, const uint8_t* q, const uint8_t* exps
   return gate_up_q(false, M, F, K, q, exps, w, q_out, exps_out, workspace, workspace_bytes, stream);
 }
 
+// ---- 4-bit KV cache
+
+static bool kv_q_heads_ok(int n_heads, int n_kv_heads, int head_dim) {
+  return n_kv_heads >= 1 && n_kv_heads <= KV4_MAX_HEADS && n_heads >= 0 && n_heads <= KV4_MAX_HEADS &&
+         n_heads % n_kv_heads == 0 && (head_dim == 64 || head_dim == 128);
+}
+static bool kv_q_pool_ok(const sd_kv_q_pool* pool) {
+  return pool && sd_kv_q_bytes(pool->n_blocks, pool->n_kv_heads, pool->head_dim);
+}
+static bool kv_q_rows_ok(const sd_kv_rows* r) {
+  return r && r->n_seqs >= 0 && r->n_seqs <= KV4_MAX_ROWS && r->table_width >= 1 && r->table_width <= KV4_MAX_ROWS;
+}
+// rows of heads of a tensor: an address and a stride that 16-byte accesses need
+static bool kv_q_rows_at(const void* p, int ld, int heads, int head_dim, int dtype) {
+  return p && (uintptr_t)p % 16 == 0 && ld >= heads * head_dim && ((size_t)ld * esize(dtype)) % 16 == 0;
+}
+static bool kv_q_arrays_ok(const sd_kv_q_pool* pool, const sd_kv_rows* r) {
+  return pool->data && (uintptr_t)pool->data % 16 == 0 && r->cu_rows && r->lengths && r->table &&
+         ((uintptr_t)r->cu_rows | (uintptr_t)r->lengths | (uintptr_t)r->table) % 4 == 0;
+}
+static bool head_norm_ok(const sd_head_norm* n) {
+  if (!n || (n->gain_dtype != SD_DTYPE_BF16 && n->gain_dtype != SD_DTYPE_F32)) return false;
+  if ((n->q_gain || n->k_gain) && !(n->eps > 0.f)) return false;
+  if (((uintptr_t)n->q_gain | (uintptr_t)n->k_gain) % esize(n->gain_dtype) || (uintptr_t)n->rope % 16) return false;
+  return !n->rope || (n->n_pos >= 1 && n->n_pos <= KV4_MAX_BLOCKS);
+}
+static void set_norm(Kv4Params& p, const sd_head_norm* n) {
+  p.q_gain = n->q_gain;
+  p.k_gain = n->k_gain;
+  p.gain_bf16 = n->gain_dtype == SD_DTYPE_BF16;
+  p.eps = n->eps;
+  p.rope = n->rope;
+  p.n_pos = n->n_pos;
+}
+static KvRows kv_rows(const sd_kv_rows* r) { return KvRows{r->cu_rows, r->lengths, r->table, r->n_seqs, r->table_width}; }
+static bool dtype_ok(int dtype) { return dtype == SD_DTYPE_BF16 || dtype == SD_DTYPE_F32; }
+
+size_t sd_kv_q_bytes(int n_blocks, int n_kv_heads, int head_dim) {
+  if (n_blocks < 1 || n_blocks > KV4_MAX_BLOCKS || !kv_q_heads_ok(0, n_kv_heads, head_dim)) return 0;
+  return (size_t)n_blocks * n_kv_heads * 17 * head_dim;
+}
+
+int sd_rope_table(int n_pos, int head_dim, double theta, float* rope, void* stream) {
+  if (n_pos < 0 || n_pos > KV4_MAX_BLOCKS || (head_dim != 64 && head_dim != 128) || !(theta > 0.0)) return SD_EINVAL;
+  if (n_pos == 0) return SD_OK;
+  if (!rope || (uintptr_t)rope % 16) return SD_EINVAL;
+  HIPCHK(launch_rope_table((float2*)rope, n_pos, head_dim / 2, theta, (hipStream_t)stream));
+  return SD_OK;
+}
+
+int sd_norm_rope(int M, int n_heads, int n_kv_heads, int head_dim, int dtype, const void* q, int ldq, const void* k, int ldk,
+                 const int32_t* positions, const sd_head_norm* norm, void* q_out, int ldq_out, void* k_out, int ldk_out,
+                 void* stream) {
+  if (M < 0 || M > KV4_MAX_ROWS || n_heads < 1 || !kv_q_heads_ok(n_heads, n_kv_heads, head_dim) || !dtype_ok(dtype) ||
+      !head_norm_ok(norm))
+    return SD_EINVAL;
+  if (M == 0) return SD_OK;
+  if (!kv_q_rows_at(q, ldq, n_heads, head_dim, dtype) || !kv_q_rows_at(k, ldk, n_kv_heads, head_dim, dtype) ||
+      !kv_q_rows_at(q_out, ldq_out, n_heads, head_dim, dtype) || !kv_q_rows_at(k_out, ldk_out, n_kv_heads, head_dim, dtype))
+    return SD_EINVAL;
+  if ((norm->rope && !positions) || (uintptr_t)positions % 4) return SD_EINVAL;
+  Kv4Params p{};
+  p.M = M;
+  p.H = n_heads;
+  p.KV = n_kv_heads;
+  p.q = q;
+  p.k = k;
+  p.ldq = ldq;
+  p.ldk = ldk;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  p.ldqo = ldq_out;
+  p.ldko = ldk_out;
+  p.positions = positions;
+  set_norm(p, norm);
+  HIPCHK(launch_kv4(KV4_HEADS, dtype == SD_DTYPE_F32 ? 1 : 0, head_dim, p, (hipStream_t)stream));
+  return SD_OK;
+}
+
+static int kv_write_q(Kv4Mode mode, const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int n_heads, int dtype, const void* q,
+                      int ldq, const void* k, int ldk, const void* v, int ldv, const sd_head_norm* norm, void* q_out, int ldq_out,
+                      void* stream) {
+  if (M < 0 || M > KV4_MAX_ROWS || !kv_q_pool_ok(pool) || !kv_q_rows_ok(rows) || !dtype_ok(dtype)) return SD_EINVAL;
+  const int KV = pool->n_kv_heads, hd = pool->head_dim;
+  if (mode == KV4_BOTH && (n_heads < 1 || !kv_q_heads_ok(n_heads, KV, hd) || !head_norm_ok(norm))) return SD_EINVAL;
+  if (M == 0 || rows->n_seqs == 0) return SD_OK;
+  if (!kv_q_rows_at(k, ldk, KV, hd, dtype) || !kv_q_rows_at(v, ldv, KV, hd, dtype) || !kv_q_arrays_ok(pool, rows)) return SD_EINVAL;
+  Kv4Params p{};
+  if (mode == KV4_BOTH) {
+    if (!kv_q_rows_at(q, ldq, n_heads, hd, dtype) || !kv_q_rows_at(q_out, ldq_out, n_heads, hd, dtype)) return SD_EINVAL;
+    p.H = n_heads;
+    p.q = q;
+    p.ldq = ldq;
+    p.q_out = q_out;
+    p.ldqo = ldq_out;
+    set_norm(p, norm);
+  }
+  p.M = M;
+  p.KV = KV;
+  p.k = k;
+  p.v = v;
+  p.ldk = ldk;
+  p.ldv = ldv;
+  p.rows = kv_rows(rows);
+  p.pool = (uint8_t*)pool->data;
+  p.n_blocks = pool->n_blocks;
+  HIPCHK(launch_kv4(mode, dtype == SD_DTYPE_F32 ? 1 : 0, hd, p, (hipStream_t)stream));
+  return SD_OK;
+}
+
+int sd_kv_append_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int dtype, const void* k, int ldk, const void* v,
+                   int ldv, void* stream) {
+  return kv_write_q(KV4_APPEND, pool, rows, M, 0, dtype, nullptr, 0, k, ldk, v, ldv, nullptr, nullptr, 0, stream);
+}
+
+int sd_norm_rope_append_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int n_heads, int dtype, const void* q, int ldq,
+                          const void* k, int ldk, const void* v, int ldv, const sd_head_norm* norm, void* q_out, int ldq_out,
+                          void* stream) {
+  return kv_write_q(KV4_BOTH, pool, rows, M, n_heads, dtype, q, ldq, k, ldk, v, ldv, norm, q_out, ldq_out, stream);
+}
+
+int sd_kv_read_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int dtype, void* k, int ldk, void* v, int ldv,
+                 void* stream) {
+  if (M < 0 || M > KV4_MAX_ROWS || !kv_q_pool_ok(pool) || !kv_q_rows_ok(rows) || !dtype_ok(dtype)) return SD_EINVAL;
+  if (M == 0 || rows->n_seqs == 0) return SD_OK;
+  if (!kv_q_rows_at(k, ldk, pool->n_kv_heads, pool->head_dim, dtype) ||
+      !kv_q_rows_at(v, ldv, pool->n_kv_heads, pool->head_dim, dtype) || !kv_q_arrays_ok(pool, rows))
+    return SD_EINVAL;
+  Kv4Params p{};
+  p.M = M;
+  p.KV = pool->n_kv_heads;
+  p.k_out = k;
+  p.v_out = v;
+  p.ldko = ldk;
+  p.ldvo = ldv;
+  p.rows = kv_rows(rows);
+  p.pool = (uint8_t*)pool->data;
+  p.n_blocks = pool->n_blocks;
+  HIPCHK(launch_kv4(KV4_READ, dtype == SD_DTYPE_F32 ? 1 : 0, pool->head_dim, p, (hipStream_t)stream));
+  return SD_OK;
+}
+
+size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len) {
+  if (M < 1 || M > KV4_MAX_ROWS || n_heads < 1 || !kv_q_heads_ok(n_heads, n_kv_heads, head_dim) || n_seqs < 1 ||
+      n_seqs > KV4_MAX_ROWS || max_len < 1)
+    return 0;
+  return 0;
+}
+
+int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int n_heads, int dtype, const void* q, int ldq,
+                   void* out, int ldo, int causal, float scale, int max_len, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  if (M < 0 || M > KV4_MAX_ROWS || !kv_q_pool_ok(pool) || !kv_q_rows_ok(rows) || !dtype_ok(dtype) || max_len < 0) return SD_EINVAL;
+  const int KV = pool->n_kv_heads, hd = pool->head_dim;
+  if (n_heads < 1 || !kv_q_heads_ok(n_heads, KV, hd)) return SD_EINVAL;
+  if (M == 0 || rows->n_seqs == 0) return SD_OK;
+  if (!kv_q_rows_at(q, ldq, n_heads, hd, dtype) || !kv_q_rows_at(out, ldo, n_heads, hd, dtype) || !kv_q_arrays_ok(pool, rows))
+    return SD_EINVAL;
+  const int len = max_len ? std::min(max_len, 16 * rows->table_width) : 16 * rows->table_width;
+  const size_t need = sd_attention_q_workspace_bytes(M, n_heads, KV, hd, rows->n_seqs, len);
+  if (need && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return SD_EINVAL;
+  Attn4Params p{};
+  p.M = M;
+  p.H = n_heads;
+  p.KV = KV;
+  p.q = q;
+  p.out = out;
+  p.ldq = ldq;
+  p.ldo = ldo;
+  p.pool = (const uint8_t*)pool->data;
+  p.n_blocks = pool->n_blocks;
+  p.rows = kv_rows(rows);
+  p.causal = causal != 0;
+  p.scale = scale;
+  HIPCHK(launch_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, p, (hipStream_t)stream));
+  return SD_OK;
+}
+
 const char* sd_last_error(void) { return g_last_error; }
 
 const char* sd_strerror(int code) {

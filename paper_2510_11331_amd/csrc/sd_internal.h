@@ -292,6 +292,50 @@ struct Gemm8Params {
 // PART leaves the K ranges' products in part for the caller to add (plans of more than one range)
 enum Gemm8Epi { EPI8_STORE = 0, EPI8_SWIGLU = 1, EPI8_SWIGLU_Q = 2, EPI8_PART = 3 };
 
+// ---------------------------------------------------------------- 4-bit KV cache (format: codes4.h)
+
+constexpr int KV4_MAX_HEADS = 1024, KV4_MAX_ROWS = 1 << 20, KV4_MAX_BLOCKS = 1 << 24;
+
+// rows of a pass: those of sequence b are cu[b] .. cu[b + 1] - 1 and the last positions of its len[b]
+struct KvRows {
+  const int32_t* cu;       // [B + 1]
+  const int32_t* len;      // [B]
+  const int32_t* table;    // [B, W] pages
+  int B, W;
+};
+
+struct Kv4Params {
+  int M, H, KV;
+  const void *q, *k, *v;   // [M, ..] heads of hd adjacent entries, row strides in entries
+  int ldq, ldk, ldv;
+  void *q_out, *k_out, *v_out;   // v_out: reading back only
+  int ldqo, ldko, ldvo;
+  const void *q_gain, *k_gain;   // [hd], or null: no norm
+  int gain_bf16;
+  float eps;
+  const float* rope;       // [n_pos, hd / 2, 2] (cos, sin), or null: no rotation
+  int n_pos;
+  const int32_t* positions;      // [M], where the rows are of no sequence
+  KvRows rows;
+  uint8_t* pool;           // [n_blocks, KV, 17 hd]
+  int n_blocks;
+};
+// HEADS: norm and rotation of queries and keys.  APPEND: keys and values into the pool.  BOTH: queries out, keys and
+// values into the pool.  READ: keys and values out of it.
+enum Kv4Mode { KV4_HEADS = 0, KV4_APPEND = 1, KV4_BOTH = 2, KV4_READ = 3 };
+
+struct Attn4Params {
+  int M, H, KV;
+  const void* q;           // [M, H, hd], row stride ldq
+  void* out;               // [M, H, hd], row stride ldo
+  int ldq, ldo;
+  const uint8_t* pool;
+  int n_blocks;
+  KvRows rows;
+  int causal;
+  float scale;
+};
+
 // ---------------------------------------------------------------- launchers
 // dtype: 0 bf16, 1 fp32 (same values as SD_DTYPE_*)
 
@@ -353,6 +397,8 @@ Gemm8Tile tile_of(const Gemm8Plan& plan, int M);
 // scratch, unless gate_up8_fused
 hipError_t launch_gate_up8(const Gemm8Params& p, float* h, bool exact, hipStream_t s);
 hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p, hipStream_t s);
+hipError_t launch_kv4(Kv4Mode mode, int dtype, int hd, const Kv4Params& p, hipStream_t s);
+hipError_t launch_attention4(int dtype, int hd, const Attn4Params& p, hipStream_t s);
 hipError_t launch_pack_linear(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 
 // GEMM geometry (shared by host planning and the kernel)

@@ -1,0 +1,284 @@
+"""Attention over a paged KV cache held in 4 bits, and what writes that cache:
+torch tensors in front of libsd's context-free calls (include/sd.h).
+
+A cache (KVCacheQ) is a pool of pages of 16 tokens; keys and values are e2m1
+codes with one power-of-two scale per 32 dimensions of a token and head, 17 / 64
+of the bytes of a 16-bit cache.  What a pass does is described once for all its
+layers (KVRows): which rows belong to which sequence, the sequences' lengths with
+these rows, and their pages.  A layer's attention on a QKV product is
+
+    q = norm_rope_append_q(cache, q, k, v, rows, rope, q_gain, k_gain, eps)
+    o = attention_q(q, cache, rows)
+
+norm_rope does the norms and the rotation alone, kv_append_q the writing,
+kv_read_q gives cached keys and values back.
+
+q, k, v are [rows, heads, head_dim], bfloat16 or float32, head_dim 64 or 128; a
+head's entries and a row's heads are adjacent, the rows may lie apart (views of
+one QKV product).  Every call enqueues on `stream` (default: the current stream
+of the tensors' device) and returns new tensors unless it is given some to write
+to.  Arguments that the kernels do not cover raise ValueError, or SDError where
+only the library sees it (sizes past its limits, addresses or strides off 16
+bytes, eps <= 0), before anything is enqueued.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from ._lib import SD_DTYPE_BF16, SD_DTYPE_F32, SD_OK, HeadNorm, KvQPool, KvRows, check, lib
+from .ffn_q import _elsewhere, _raw_stream
+
+PAGE = 16
+_DTYPES = {torch.bfloat16: SD_DTYPE_BF16, torch.float32: SD_DTYPE_F32}
+
+
+class KVCacheQ:
+    """A pool of pages: `data` is uint8 [n_blocks, n_kv_heads, 17 head_dim] on the GPU."""
+
+    __slots__ = ("data", "n_blocks", "n_kv_heads", "head_dim", "_index", "_pool", "_at")
+
+    def __init__(self, data: torch.Tensor):
+        if data.dim() != 3 or data.dtype != torch.uint8 or not data.is_contiguous() or data.shape[2] not in (17 * 64, 17 * 128):
+            raise ValueError("data: contiguous uint8 [n_blocks, n_kv_heads, 17 head_dim], head_dim 64 or 128")
+        n, kv, hd = data.shape[0], data.shape[1], data.shape[2] // 17
+        if data.numel() == 0 or lib().sd_kv_q_bytes(n, kv, hd) != data.numel():
+            raise ValueError(f"no cache of {n} pages of {kv} heads")
+        self.data, self.n_blocks, self.n_kv_heads, self.head_dim = data, n, kv, hd
+        self._index = data.get_device()
+        self._pool = KvQPool(data.data_ptr(), n, kv, hd)
+        self._at = C.addressof(self._pool)
+
+    @classmethod
+    def empty(cls, n_blocks: int, n_kv_heads: int, head_dim: int, device="cuda") -> "KVCacheQ":
+        """A cache whose pages hold nothing yet: only positions that were written may be read."""
+        return cls(torch.empty((n_blocks, n_kv_heads, 17 * head_dim), dtype=torch.uint8, device=device))
+
+
+class KVRows:
+    """The rows of a pass.  cu_rows [n + 1]: sequence b has the rows cu_rows[b] .. cu_rows[b + 1] - 1; lengths [n]: its
+    tokens with these rows, which are its last ones; table [n, width]: the pages of its positions 16 i .. 16 i + 15.  All
+    int32 on the GPU, read when a call runs: a captured pass follows what is written to them.  max_len: the longest length
+    that the work is to be split for (default: what the table holds)."""
+
+    __slots__ = ("cu_rows", "lengths", "table", "max_len", "_index", "_rows", "_at")
+
+    def __init__(self, cu_rows: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, max_len: Optional[int] = None):
+        n = lengths.shape[0] if lengths.dim() == 1 else -1
+        if n < 0 or cu_rows.shape != (n + 1,) or table.dim() != 2 or table.shape[0] != n or table.shape[1] < 1:
+            raise ValueError("cu_rows [n + 1], lengths [n], table [n, width]")
+        for t in (cu_rows, lengths, table):
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != table.get_device():
+                raise ValueError("cu_rows, lengths, table: contiguous int32 on one device")
+        if max_len is not None and max_len < 1:
+            raise ValueError("max_len: at least 1")
+        self.cu_rows, self.lengths, self.table = cu_rows, lengths, table
+        self.max_len = min(16 * table.shape[1], max_len or 16 * table.shape[1])
+        self._index = table.get_device()
+        self._rows = KvRows(cu_rows.data_ptr(), lengths.data_ptr(), table.data_ptr(), n, table.shape[1])
+        self._at = C.addressof(self._rows)
+
+
+def rope_table(n_pos: int, head_dim: int, theta: float = 10000.0, device="cuda",
+               stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """(cos, sin) of position theta^(-2 i / head_dim): float32 [n_pos, head_dim / 2, 2]."""
+    if n_pos < 0 or head_dim not in (64, 128) or not theta > 0:
+        raise ValueError("n_pos >= 0, head_dim 64 or 128, theta > 0")
+    out = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
+    there = _elsewhere(out, stream)
+    if there is not None:
+        with there:
+            check(lib().sd_rope_table(n_pos, head_dim, theta, out.data_ptr(), _raw_stream(out.get_device())), "sd_rope_table")
+        return out
+    check(lib().sd_rope_table(n_pos, head_dim, theta, out.data_ptr(), _raw_stream(out.get_device())), "sd_rope_table")
+    return out
+
+
+def _stride(x: torch.Tensor, what: str, M: int, heads: int, hd: int, dtype: torch.dtype, index: int) -> int:
+    """The row stride of heads [M, heads, hd]."""
+    if x.shape != (M, heads, hd) or x.dtype != dtype or x.get_device() != index:
+        raise ValueError(f"{what}: [{M}, {heads}, {hd}] {dtype} on the device of the others")
+    if M == 0:
+        return heads * hd
+    row, head, one = x.stride()
+    if one != 1 or (heads > 1 and head != hd):
+        raise ValueError(f"{what}: heads of adjacent entries, adjacent in their row")
+    if M == 1:
+        return heads * hd
+    if not heads * hd <= row < 1 << 31:
+        raise ValueError(f"{what}: rows apart by at least their length")
+    return row
+
+
+def _norm(q: torch.Tensor, hd: int, index: int, rope, q_gain, k_gain, eps: float) -> HeadNorm:
+    dt = torch.bfloat16
+    for g in (q_gain, k_gain):
+        if g is not None:
+            dt = g.dtype
+            if g.shape != (hd,) or dt not in _DTYPES or not g.is_contiguous() or g.get_device() != index:
+                raise ValueError("gains: contiguous [head_dim], bfloat16 or float32, on the device of q")
+    if q_gain is not None and k_gain is not None and q_gain.dtype != k_gain.dtype:
+        raise ValueError("gains of one type")
+    if rope is not None and (rope.dim() != 3 or rope.shape[1:] != (hd // 2, 2) or rope.dtype != torch.float32
+                             or not rope.is_contiguous() or rope.get_device() != index or rope.shape[0] < 1):
+        raise ValueError("rope: contiguous float32 [positions, head_dim / 2, 2] on the device of q")
+    return HeadNorm(None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
+                    None if rope is None else rope.data_ptr(), _DTYPES[dt], 0 if rope is None else rope.shape[0], eps)
+
+
+def _shape(x: torch.Tensor) -> Tuple[int, int, int, int]:
+    if x.dim() != 3 or x.dtype not in _DTYPES or x.shape[2] not in (64, 128) or x.shape[1] < 1:
+        raise ValueError("q, k, v: [rows, heads, head_dim], bfloat16 or float32, head_dim 64 or 128")
+    index = x.get_device()
+    if index < 0:
+        raise ValueError("tensors on a GPU are needed")
+    return (*x.shape, index)
+
+
+def norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
+              q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-5,
+              q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(q, k) with every head's RMS norm (gains [head_dim], None: no norm) and then its rotation by (cos, sin) =
+    rope[positions[row]] (rope None: no rotation; entries i and i + head_dim / 2 are a pair).  positions int32 [rows].
+    q_out, k_out: where they go (the inputs themselves, or memory that overlaps none)."""
+    M, H, hd, index = _shape(q)
+    there = _elsewhere(q, stream)
+    if there is not None:
+        with there:
+            return norm_rope(q, k, positions, rope, q_gain, k_gain, eps, q_out, k_out)
+    KV = k.shape[1] if k.dim() == 3 else 0
+    if KV < 1 or H % KV:
+        raise ValueError("k: [rows, heads, head_dim], its heads a divisor of the query heads")
+    ldq, ldk = _stride(q, "q", M, H, hd, q.dtype, index), _stride(k, "k", M, KV, hd, q.dtype, index)
+    n = _norm(q, hd, index, rope, q_gain, k_gain, eps)
+    if rope is not None and (positions is None or positions.shape != (M,) or positions.dtype != torch.int32
+                             or not positions.is_contiguous() or positions.get_device() != index):
+        raise ValueError("positions: contiguous int32 [rows] on the device of q")
+    ldqo, ldko = H * hd, KV * hd
+    if q_out is None:
+        q_out = torch.empty((M, H, hd), dtype=q.dtype, device=q.device)
+    else:
+        ldqo = _stride(q_out, "q_out", M, H, hd, q.dtype, index)
+    if k_out is None:
+        k_out = torch.empty((M, KV, hd), dtype=q.dtype, device=q.device)
+    else:
+        ldko = _stride(k_out, "k_out", M, KV, hd, q.dtype, index)
+    rc = lib().sd_norm_rope(M, H, KV, hd, _DTYPES[q.dtype], q.data_ptr(), ldq, k.data_ptr(), ldk,
+                            None if rope is None else positions.data_ptr(), C.addressof(n), q_out.data_ptr(), ldqo,
+                            k_out.data_ptr(), ldko, _raw_stream(index))
+    if rc != SD_OK:
+        check(rc, "sd_norm_rope")
+    return q_out, k_out
+
+
+def _same_device(cache: KVCacheQ, rows: KVRows, index: int) -> None:
+    if cache._index != index or rows._index != index:
+        raise ValueError("cache, rows and tensors on one device")
+
+
+def kv_append_q(cache: KVCacheQ, k: torch.Tensor, v: torch.Tensor, rows: KVRows,
+                stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Quantise the rows' keys and values into the cache, at their positions."""
+    M, KV, hd, index = _shape(k)
+    there = _elsewhere(k, stream)
+    if there is not None:
+        with there:
+            return kv_append_q(cache, k, v, rows)
+    if KV != cache.n_kv_heads or hd != cache.head_dim:
+        raise ValueError(f"k: [rows, {cache.n_kv_heads}, {cache.head_dim}]")
+    _same_device(cache, rows, index)
+    ldk, ldv = _stride(k, "k", M, KV, hd, k.dtype, index), _stride(v, "v", M, KV, hd, k.dtype, index)
+    rc = lib().sd_kv_append_q(cache._at, rows._at, M, _DTYPES[k.dtype], k.data_ptr(), ldk, v.data_ptr(), ldv, _raw_stream(index))
+    if rc != SD_OK:
+        check(rc, "sd_kv_append_q")
+
+
+def norm_rope_append_q(cache: KVCacheQ, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rows: KVRows,
+                       rope: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None,
+                       k_gain: Optional[torch.Tensor] = None, eps: float = 1e-5, q_out: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """norm_rope at the rows' positions: q is returned, k (its values in float32) and v go into the cache.  q_out: where
+    q goes (q itself, or memory that overlaps no input)."""
+    M, H, hd, index = _shape(q)
+    there = _elsewhere(q, stream)
+    if there is not None:
+        with there:
+            return norm_rope_append_q(cache, q, k, v, rows, rope, q_gain, k_gain, eps, q_out)
+    KV = cache.n_kv_heads
+    if hd != cache.head_dim or H % KV:
+        raise ValueError(f"q: heads of {cache.head_dim}, a multiple of {KV}")
+    _same_device(cache, rows, index)
+    ldq = _stride(q, "q", M, H, hd, q.dtype, index)
+    ldk, ldv = _stride(k, "k", M, KV, hd, q.dtype, index), _stride(v, "v", M, KV, hd, q.dtype, index)
+    n = _norm(q, hd, index, rope, q_gain, k_gain, eps)
+    ldqo = H * hd
+    if q_out is None:
+        q_out = torch.empty((M, H, hd), dtype=q.dtype, device=q.device)
+    else:
+        ldqo = _stride(q_out, "q_out", M, H, hd, q.dtype, index)
+    rc = lib().sd_norm_rope_append_q(cache._at, rows._at, M, H, _DTYPES[q.dtype], q.data_ptr(), ldq, k.data_ptr(), ldk,
+                                     v.data_ptr(), ldv, C.addressof(n), q_out.data_ptr(), ldqo, _raw_stream(index))
+    if rc != SD_OK:
+        check(rc, "sd_norm_rope_append_q")
+    return q_out
+
+
+def kv_read_q(cache: KVCacheQ, rows: KVRows, n_rows: int, dtype: torch.dtype = torch.bfloat16,
+              k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(k, v) [n_rows, heads, head_dim] of dtype at the rows' positions.  k_out, v_out: where they go."""
+    index = cache._index
+    there = _elsewhere(cache.data, stream)
+    if there is not None:
+        with there:
+            return kv_read_q(cache, rows, n_rows, dtype, k_out, v_out)
+    KV, hd = cache.n_kv_heads, cache.head_dim
+    if dtype not in _DTYPES or n_rows < 0:
+        raise ValueError("at least 0 rows, bfloat16 or float32")
+    _same_device(cache, rows, index)
+    ldk = ldv = KV * hd
+    if k_out is None:
+        k_out = torch.empty((n_rows, KV, hd), dtype=dtype, device=cache.data.device)
+    else:
+        ldk = _stride(k_out, "k_out", n_rows, KV, hd, dtype, index)
+    if v_out is None:
+        v_out = torch.empty((n_rows, KV, hd), dtype=dtype, device=cache.data.device)
+    else:
+        ldv = _stride(v_out, "v_out", n_rows, KV, hd, dtype, index)
+    rc = lib().sd_kv_read_q(cache._at, rows._at, n_rows, _DTYPES[dtype], k_out.data_ptr(), ldk, v_out.data_ptr(), ldv,
+                            _raw_stream(index))
+    if rc != SD_OK:
+        check(rc, "sd_kv_read_q")
+    return k_out, v_out
+
+
+def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = True, scale: Optional[float] = None,
+                out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """softmax(scale q K^T) V [rows, heads, head_dim] over the cached positions up to the row's own (causal) or all of its
+    sequence's; scale: head_dim^-0.5 unless given.  Query heads share kv heads in runs.  out: where it goes."""
+    M, H, hd, index = _shape(q)
+    there = _elsewhere(q, stream)
+    if there is not None:
+        with there:
+            return attention_q(q, cache, rows, causal, scale, out)
+    KV = cache.n_kv_heads
+    if hd != cache.head_dim or H % KV:
+        raise ValueError(f"q: heads of {cache.head_dim}, a multiple of {KV}")
+    _same_device(cache, rows, index)
+    ldq, ldo = _stride(q, "q", M, H, hd, q.dtype, index), H * hd
+    if out is None:
+        out = torch.empty((M, H, hd), dtype=q.dtype, device=q.device)
+    else:
+        ldo = _stride(out, "out", M, H, hd, q.dtype, index)
+    L = lib()
+    ws = L.sd_attention_q_workspace_bytes(M, H, KV, hd, rows._rows.n_seqs, rows.max_len)
+    work = torch.empty(ws, dtype=torch.uint8, device=q.device) if ws else None
+    rc = L.sd_attention_q(cache._at, rows._at, M, H, _DTYPES[q.dtype], q.data_ptr(), ldq, out.data_ptr(), ldo, causal,
+                          hd ** -0.5 if scale is None else scale, rows.max_len, work.data_ptr() if ws else None, ws,
+                          _raw_stream(index))
+    if rc != SD_OK:
+        check(rc, "sd_attention_q")
+    return out
