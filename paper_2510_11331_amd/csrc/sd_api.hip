@@ -1536,7 +1536,11 @@ size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int he
   if (M < 1 || M > KV4_MAX_ROWS || n_heads < 1 || !kv_q_heads_ok(n_heads, n_kv_heads, head_dim) || n_seqs < 1 ||
       n_seqs > KV4_MAX_ROWS || max_len < 1)
     return 0;
-  return 0;
+  // fp32 rows take the smaller workgroups, and so the larger sums
+  size_t n = 0;
+  for (int dtype : {0, 1})
+    n = std::max(n, attention4_part_floats(plan_attention4(dtype, M, n_heads, n_kv_heads, n_seqs, max_len), n_kv_heads, head_dim));
+  return n * sizeof(float);
 }
 
 int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int n_heads, int dtype, const void* q, int ldq,
@@ -1564,7 +1568,11 @@ int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int 
   p.rows = kv_rows(rows);
   p.causal = causal != 0;
   p.scale = scale;
-  HIPCHK(launch_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, p, (hipStream_t)stream));
+  const Attn4Plan plan = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, M, n_heads, KV, rows->n_seqs, len);
+  p.splits = plan.splits;
+  p.part_o = (float*)workspace;
+  p.part_ml = p.part_o + (size_t)plan.blocks * KV * plan.splits * 16 * plan.tiles * hd;
+  HIPCHK(launch_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, plan, p, (hipStream_t)stream));
   return SD_OK;
 }
 

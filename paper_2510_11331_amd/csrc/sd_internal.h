@@ -334,7 +334,14 @@ struct Attn4Params {
   KvRows rows;
   int causal;
   float scale;
+  int splits;              // ranges of the keys
+  float* part_o;           // their outputs [blocks, KV, splits, 16 tiles, hd] and (maximum, sum) (more than one)
+  float* part_ml;
 };
+// tiles of 16 query vectors in a workgroup, workgroups of such vectors at most, ranges of the keys
+struct Attn4Plan { int tiles, blocks, splits; };
+Attn4Plan plan_attention4(int dtype, int M, int H, int KV, int n_seqs, int max_len);
+size_t attention4_part_floats(const Attn4Plan& a, int KV, int hd);
 
 // ---------------------------------------------------------------- launchers
 // dtype: 0 bf16, 1 fp32 (same values as SD_DTYPE_*)
@@ -398,7 +405,7 @@ Gemm8Tile tile_of(const Gemm8Plan& plan, int M);
 hipError_t launch_gate_up8(const Gemm8Params& p, float* h, bool exact, hipStream_t s);
 hipError_t launch_gemm8(int epi, const Gemm8Plan& plan, const Gemm8Params& p, hipStream_t s);
 hipError_t launch_kv4(Kv4Mode mode, int dtype, int hd, const Kv4Params& p, hipStream_t s);
-hipError_t launch_attention4(int dtype, int hd, const Attn4Params& p, hipStream_t s);
+hipError_t launch_attention4(int dtype, int hd, const Attn4Plan& a, const Attn4Params& p, hipStream_t s);
 hipError_t launch_pack_linear(int dtype, const void* src, void* dst, int N, int K, hipStream_t s);
 
 // GEMM geometry (shared by host planning and the kernel)
