@@ -33,9 +33,12 @@
 #include "codes4.h"
 
 #include <float.h>
+#include <stdio.h>
+#include <stdlib.h>
 #include <math.h>
 
 #include <algorithm>
+#include <utility>
 
 namespace sd {
 
@@ -99,15 +102,16 @@ template <int PARTS> __device__ __forceinline__ void parts8(const float (&x)[8],
 
 // The vectors of workgroup `block`: sequence b, its first row, its rows n and the first of its vectors.  Sequence b has
 // ceil(n G / cap) workgroups; every wave adds them up by itself, 64 sequences at a time.
-struct Block4 { int b, row0, n, v0; };
+struct Block4 { int b, row0, n, v0, len; };
 __device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int cap, int block, Block4& o) {
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < s.B; b0 += 64) {
     const int b = b0 + lane;
-    int lo = 0, hi = 0;
+    int lo = 0, hi = 0, len = 0;
     if (b < s.B) {
       lo = min(max(s.cu[b], 0), M);
       hi = min(max(s.cu[b + 1], lo), M);
+      len = s.len[b];                            // (of all of them: not a second round of latency)
     }
     const int mine = ((hi - lo) * G + cap - 1) / cap;
     int sum = mine;
@@ -122,6 +126,7 @@ __device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int ca
       o.b = b0 + at;
       o.row0 = __builtin_amdgcn_readlane(lo, at);
       o.n = __builtin_amdgcn_readlane(hi, at) - o.row0;
+      o.len = __builtin_amdgcn_readlane(len, at);
       o.v0 = (block - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at))) * cap;
       return (unsigned)o.v0 < (unsigned)(o.n * G);           // (row counts that overflow, of no valid cu)
     }
@@ -151,15 +156,19 @@ template <int HD> struct Load4;            // what a lane has of a page's keys o
 template <> struct Load4<128> { typedef u32x4 type; };
 template <> struct Load4<64> { typedef u32x2 type; };
 
+// waves that a SIMD is to hold at once, for which the compiler keeps to so many registers
+template <typename T, int QT> constexpr int MIN_WAVES = QT == 1 ? (sizeof(T) == 2 ? 4 : 3) : QT == 2 ? 2 : 1;
+
 template <typename T, int HD, int QT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void attention4_stream_kernel(Attn4Params p) {
+__global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_stream_kernel(Attn4Params p) {
   using P = Page4<HD>;
   using L4 = typename Load4<HD>::type;
   constexpr int KS = HD / 32;                    // k-steps of a score
   constexpr int DT = HD / 16;                    // output tiles, dimensions of a lane's values
   constexpr int QP = sizeof(T) == 2 ? 1 : 3;     // parts of a query
   constexpr int PP = sizeof(T) == 2 ? 2 : 3;     // parts of a weight
-  __shared__ __attribute__((aligned(16))) float s_o[WAVES][16][HD + 4];
+  constexpr int PH = WAVES / 4, IP = 4 / PH;     // the outputs are joined in PH parts, which LDS has room for
+  __shared__ __attribute__((aligned(16))) float s_o[WAVES][16][HD / PH + 4];
   __shared__ float s_m[WAVES][16], s_l[WAVES][16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -168,13 +177,20 @@ __global__ __launch_bounds__(64 * WAVES) void attention4_stream_kernel(Attn4Para
   const int kvh = blockIdx.x % p.KV, split = blockIdx.x / p.KV % p.splits, block = blockIdx.x / p.KV / p.splits;
   Block4 w;
   if (!find_block(p.rows, p.M, G, 16 * QT, block, w)) return;
-  const int len = p.rows.len[w.b];
+  const int len = w.len;
   const int nv = min(16 * QT, w.n * G - w.v0);   // vectors of this workgroup
   const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
   const int n_min = sees(p, len, w.n, w.v0, G);  // what all of them see
   const int kps = range_keys(n_max, p.splits, 32 * WAVES);
   const int k0 = split * kps, k1 = min(k0 + kps, n_max);
-  if (split > 0 && k0 >= k1) return;
+  if (split > 0 && k0 >= k1) {                   // a range without keys
+    if (tid < nv) {
+      const int vec = w.v0 + tid;
+      const size_t at = ((size_t)split * p.M + w.row0 + vec / G) * p.H + kvh * G + vec % G;
+      *(float2*)(p.part_ml + 2 * at) = sees(p, len, w.n, vec, G) > 0 ? make_float2(-FLT_MAX, 0.f) : make_float2(0.f, -1.f);
+    }
+    return;
+  }
 
   // queries, as operands: lane (r, g) has dimensions (hd / 4) g + 8 s .. of vector r in k-step s
   u32x4 q[QT][KS][QP];
@@ -213,49 +229,116 @@ __global__ __launch_bounds__(64 * WAVES) void attention4_stream_kernel(Attn4Para
   const uint8_t* const head = p.pool + (size_t)kvh * P::BYTES;
   const size_t page_bytes = (size_t)p.KV * P::BYTES;
   const int32_t* const table = p.rows.table + (size_t)w.b * p.rows.W;
-  const int off_k = P::key(r, g * (HD / 4)), off_v = P::value(4 * g, r);
-  const int off_ks = P::key_scale(r, g * (HD / 4) / 32), off_vs = P::value_scale(4 * g, r * DT / 32);
+  const uint32_t off_k = P::key(r, g * (HD / 4)), off_v = P::value(4 * g, r);
+  const uint32_t off_ks = P::key_scale(r, g * (HD / 4) / 32), off_vs = P::value_scale(4 * g, r * DT / 32);
 
-  // the wave's steps are 32 (wave + WAVES i) keys into the range; lane l holds page l % 2 of step i0 + l / 2
+  // the wave's steps are 32 (wave + WAVES i) keys into the range; lane l of ids holds page l % 2 of step 32 j + l / 2, and
+  // of ids_next that of 32 steps later
   const int steps = k1 > k0 ? ((k1 - k0 + 31) / 32 - wave + WAVES - 1) / WAVES : 0;
-  int ids = 0;
-  uint64_t bad = 0;
-  auto load_ids = [&](int i0) {
-    const int i = i0 + lane / 2;
-    const int pg = (k0 + 32 * (wave + WAVES * i)) / 16 + (lane & 1);
+  auto page_id = [&](int i0, bool& no) {
+    const int i = i0 + lane / 2, pg = (k0 + 32 * (wave + WAVES * i)) / 16 + (lane & 1);
     int id = 0;
-    bool no = false;
+    no = false;
     if (i < steps && 16 * pg < k1) {
       id = pg < p.rows.W ? table[pg] : -1;
       no = (unsigned)id >= (unsigned)p.n_blocks;
-      if (no) id = 0;
     }
-    ids = id;
-    bad = __ballot(no);
+    return no ? 0 : id;
+  };
+  bool no_next;
+  int ids = page_id(0, no_next);
+  uint64_t no_ids = __ballot(no_next);
+  int ids_next = page_id(32, no_next);
+
+  // keys are loaded a step ahead when those of the step have been used, values likewise
+  L4 kc[2], vc[2];
+  uint32_t kE[2], vE[2];
+  const uint8_t *pg0, *pg1;                      // the pages being loaded, and which of them are none
+  uint32_t no = 0;
+  auto pages = [&](int i) {
+    pg0 = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i) * page_bytes;
+    pg1 = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i + 1) * page_bytes;
+    no = (uint32_t)(no_ids >> (2 * i)) & 3u;
+  };
+  auto load_k = [&]() {
+    kc[0] = *(const L4*)(pg0 + off_k);
+    kE[0] = pg0[off_ks];
+    kc[1] = *(const L4*)(pg1 + off_k);
+    kE[1] = pg1[off_ks];
+  };
+  auto load_v = [&]() {
+    vc[0] = *(const L4*)(pg0 + off_v);
+    vE[0] = *(const uint32_t*)(pg0 + off_vs);
+    vc[1] = *(const L4*)(pg1 + off_v);
+    vE[1] = *(const uint32_t*)(pg1 + off_vs);
   };
 
-  struct Stage { L4 k[2], v[2]; uint32_t ks[2], vs[2]; };
-  auto load = [&](Stage& st, int i) {            // i: step within the ids held
+  int key0 = k0 + 32 * wave, left = steps, at = 0;       // at: of the step after this one, within ids
+  // EDGE: some key of the step is not seen by all vectors, or a page is none
+  auto step = [&]<bool EDGE>() {
+    const uint8_t* const here[2] = {pg0, pg1};
+    const uint32_t no_here = no;
+    f32x4 z[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const uint8_t* const pg = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i + t) * page_bytes;
-      st.k[t] = *(const L4*)(pg + off_k);
-      st.ks[t] = pg[off_ks];
-      st.v[t] = *(const L4*)(pg + off_v);
-      st.vs[t] = *(const uint32_t*)(pg + off_vs);
-    }
-  };
-
-  // edge: some key of the step is not seen by all vectors, or a page is none
-  auto step = [&](const Stage& st, int i, int key0) {
-    const uint32_t no = (uint32_t)(bad >> (2 * i)) & 3u;
-    const bool edge = key0 + 32 > n_min || no;
-    uint32_t vs[2] = {st.vs[0], st.vs[1]};
-    float ks[2];
+      const float ks = scale4(EDGE && (no_here >> t & 1) ? 255u : kE[t]);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) ks[t] = scale4(no >> t & 1 ? 255u : st.ks[t]);
+      for (int s = 0; s < KS; ++s) {
+        const u32x4 k = cvt4_all(kc[t][s], ks);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(k, q[u][s][part], z[u][t]);
+      }
+    }
+
+    // the next step's keys (behind the last step its own again, which nothing uses)
+    if (left > 1) {
+      if (++at == 32) {
+        at = 0;
+        ids = ids_next;
+        no_ids = __ballot(no_next);
+        ids_next = page_id(steps - left + 1 + 32, no_next);
+      }
+      pages(at);
+    }
+    load_k();
+
+    u32x4 w8[QT][PP];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      float x[8];
+      auto weights = [&] {                       // in powers of two over the running maximum
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x[e] = fmaf(z[u][e / 4][e % 4], c, -m[u]);
+          if (EDGE && key0 + 16 * (e / 4) + 4 * g + e % 4 >= vis[u]) x[e] = -INFINITY;
+        }
+      };
+      weights();
+      const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__any(top > 8.f)) {
+        float most = -FLT_MAX;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, EDGE && x[e] == -INFINITY ? -FLT_MAX : z[u][e / 4][e % 4] * c);
+        const float to = fmaxf(m[u], quad_max(most)), old = __builtin_amdgcn_exp2f(m[u] - to);
+        m[u] = to;
+        l[u] *= old;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[u][d] *= old;
+        weights();
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
+      l[u] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      parts8<PP>(x, w8[u]);
+    }
+
     bool nan_v = false;
-    if (edge) {
+    uint32_t vs[2] = {vE[0], vE[1]};
+    if constexpr (EDGE) {
       // values that not every vector sees must be finite: their weights are zero where they are not seen, and NaN
       // that a vector does see is put into its output below
 #pragma unroll
@@ -263,93 +346,53 @@ __global__ __launch_bounds__(64 * WAVES) void attention4_stream_kernel(Attn4Para
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
           const int key = key0 + 16 * t + 4 * g + i4;
-          const bool is_nan = (vs[t] >> (8 * i4) & 255u) == 255u, none = key >= n_max || (no >> t & 1);
+          const bool is_nan = (vs[t] >> (8 * i4) & 255u) == 255u, none = key >= n_max || (no_here >> t & 1);
           nan_v |= is_nan && !none;
           if (is_nan || none) vs[t] = (vs[t] & ~(255u << (8 * i4))) | 127u << (8 * i4);
         }
     }
-
-    f32x4 z[QT][2];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const u32x4 k = cvt4_all(st.k[t][s], ks[t]);
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(k, q[u][s][part], z[u][t]);
-      }
-
-    u32x4 w8[QT][PP];
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      if (edge) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (key0 + 16 * t + 4 * g + e >= vis[u]) z[u][t][e] = -FLT_MAX;
-      }
-      float top = fmaxf(fmaxf(z[u][0][0], z[u][0][1]), fmaxf(z[u][0][2], z[u][0][3]));
-      top = fmaxf(top, fmaxf(fmaxf(z[u][1][0], z[u][1][1]), fmaxf(z[u][1][2], z[u][1][3]))) * c;
-      if (__any(top > m[u] + 8.f)) {
-        const float m_new = fmaxf(m[u], quad_max(top));
-        const float old = __builtin_amdgcn_exp2f(m[u] - m_new);
-        m[u] = m_new;
-        l[u] *= old;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[u][d] *= old;
-      }
-      float x[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        x[e] = __builtin_amdgcn_exp2f(fmaf(z[u][e / 4][e % 4], c, -m[u]));
-        if (edge && key0 + 16 * (e / 4) + 4 * g + e % 4 >= vis[u]) x[e] = 0.f;
-      }
-      l[u] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-      parts8<PP>(x, w8[u]);
-    }
-
-    // pairs of dimensions of a key -> pairs of keys of a dimension
-    constexpr int NB = HD / 32;                  // bytes of a key
-    uint32_t cv[2][4][NB];
+    // byte b of a key's values: dimensions 2 b and 2 b + 1 of the lane's; pairs of dimensions of a key become pairs of
+    // keys of a dimension
+    float sv[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float s = scale4(vs[t] >> (8 * e) & 255u);
-        if constexpr (HD == 128) {
-          const u32x4 x = cvt4_all(st.v[t][e], s);
+      for (int e = 0; e < 4; ++e) sv[t][e] = scale4(__builtin_amdgcn_ubfe(vs[t], 8 * e, 8));
+    [&]<int... B>(std::integer_sequence<int, B...>) {
+      (([&] {
+         u32x4 even, odd;
 #pragma unroll
-          for (int b = 0; b < NB; ++b) cv[t][e][b] = x[b];
-        } else {
-          cv[t][e][0] = e & 1 ? cvt4<2>(st.v[t][e / 2], s) : cvt4<0>(st.v[t][e / 2], s);
-          cv[t][e][1] = e & 1 ? cvt4<3>(st.v[t][e / 2], s) : cvt4<1>(st.v[t][e / 2], s);
-        }
-      }
+         for (int e = 0; e < 4; ++e) {
+           const int t = e / 2, k = 2 * (e % 2);
+           uint32_t a, b;
+           if constexpr (HD == 128) {
+             a = cvt4<B>(vc[t][k], sv[t][k]);
+             b = cvt4<B>(vc[t][k + 1], sv[t][k + 1]);
+           } else {
+             a = cvt4<B>(vc[t][k / 2], sv[t][k]);
+             b = cvt4<B + 2>(vc[t][k / 2], sv[t][k + 1]);
+           }
+           even[e] = low_halves(a, b);
+           odd[e] = high_halves(a, b);
+         }
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      u32x4 v;
+         for (int u = 0; u < QT; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t a = cv[e / 2][2 * (e % 2)][d / 2], b = cv[e / 2][2 * (e % 2) + 1][d / 2];
-        v[e] = d & 1 ? high_halves(a, b) : low_halves(a, b);
-      }
-#pragma unroll
-      for (int u = 0; u < QT; ++u)
-#pragma unroll
-        for (int part = PP - 1; part >= 0; --part) o[u][d] = mfma_bf16(v, w8[u][part], o[u][d]);
-    }
+           for (int part = PP - 1; part >= 0; --part) {
+             o[u][2 * B] = mfma_bf16(even, w8[u][part], o[u][2 * B]);
+             o[u][2 * B + 1] = mfma_bf16(odd, w8[u][part], o[u][2 * B + 1]);
+           }
+       }()),
+       ...);
+    }(std::make_integer_sequence<int, HD / 32>{});
 
-    if (edge && __any(nan_v)) {                  // rare: a value block of NaN that some vector sees
+    load_v();
+
+    if (EDGE && __any(nan_v)) {                  // rare: a value block of NaN that some vector sees
       // all of a lane's outputs are of scale block (hd / 4) g / 32
       for (int key = key0; key < min(key0 + 32, n_max); ++key) {
         const int t = key - key0 >= 16;
-        const uint8_t* const pg = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i + t) * page_bytes;
-        if (!(no >> t & 1) && pg[P::value_scale(key & 15, g * (HD / 4) / 32)] == 255) {
+        if (!(no_here >> t & 1) && here[t][P::value_scale(key & 15, g * (HD / 4) / 32)] == 255) {
 #pragma unroll
           for (int u = 0; u < QT; ++u)
             if (key < vis[u])
@@ -360,121 +403,166 @@ __global__ __launch_bounds__(64 * WAVES) void attention4_stream_kernel(Attn4Para
     }
   };
 
-  for (int i0 = 0; i0 < steps; i0 += 32) {
-    load_ids(i0);
-    const int n = min(32, steps - i0);
-    const int first = k0 + 32 * (wave + WAVES * i0);
-    Stage a, b;
-    load(a, 0);
-    for (int i = 0; i < n; i += 2) {
-      if (i + 1 < n) load(b, i + 1);
-      step(a, i, first + 32 * WAVES * i);
-      if (i + 1 >= n) break;
-      if (i + 2 < n) load(a, i + 2);
-      step(b, i + 1, first + 32 * WAVES * (i + 1));
-    }
+  if (left > 0) {
+    pages(0);
+    load_k();
+    load_v();
   }
+  for (; left > 0 && key0 + 32 <= n_min && !no; --left, key0 += 32 * WAVES) step.template operator()<false>();
+  for (; left > 0; --left, key0 += 32 * WAVES) step.template operator()<true>();
 
-  // the waves' outputs are joined in their order, a tile of vectors at a time
+  // the waves' outputs are joined in their order, a tile of vectors and a part of the dimensions at a time
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
+    if (16 * t >= nv) break;
     const float sum = quad_sum(l[t]);
     if (t) __syncthreads();
-    if (16 * t >= nv) break;
     if (g == 0) {
       s_m[wave][r] = m[t];
       s_l[wave][r] = sum;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int ph = 0; ph < PH; ++ph) {
+      if (ph) __syncthreads();
 #pragma unroll
-      for (int d = 0; d < DT; d += 4)
-        *(f32x4*)&s_o[wave][r][(4 * g + i) * DT + d] = f32x4{o[t][d][i], o[t][d + 1][i], o[t][d + 2][i], o[t][d + 3][i]};
+      for (int i = 0; i < IP; ++i)
+#pragma unroll
+        for (int d = 0; d < DT; d += 4) {
+          const int e = ph * IP + i;
+          *(f32x4*)&s_o[wave][r][(g * IP + i) * DT + d] = f32x4{o[t][d][e], o[t][d + 1][e], o[t][d + 2][e], o[t][d + 3][e]};
+        }
+      __syncthreads();
+      for (int idx = tid; idx < 16 * (HD / PH / 4); idx += 64 * WAVES) {
+        const int v = idx / (HD / PH / 4), col = idx % (HD / PH / 4) * 4;
+        if (16 * t + v >= nv) continue;
+        const int d = (4 * (col / (IP * DT)) + ph * IP) * DT + col % (IP * DT);
+        float M = s_m[0][v], L = 0.f;
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) M = fmaxf(M, s_m[k][v]);
+        f32x4 O{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+          const float e = __builtin_amdgcn_exp2f(s_m[k][v] - M);
+          L += s_l[k][v] * e;
+          O += *(const f32x4*)&s_o[k][v][col] * e;
+        }
+        const int vec = w.v0 + 16 * t + v, row = w.row0 + vec / G, h = kvh * G + vec % G;
+        if (p.splits == 1) {
+          if (sees(p, len, w.n, vec, G) <= 0) O = f32x4{0.f, 0.f, 0.f, 0.f};
+          else O *= 1.f / L;
+          store4((T*)p.out + (size_t)row * p.ldo + h * HD + d, O);
+        } else {
+          const size_t at = ((size_t)split * p.M + row) * p.H + h;
+          *(f32x4*)(p.part_o + at * HD + d) = O;
+          // (a sum of -1: of nothing to see, which the joined output is zero for)
+          if (d == 0) *(float2*)(p.part_ml + 2 * at) = sees(p, len, w.n, vec, G) > 0 ? make_float2(M, L) : make_float2(0.f, -1.f);
+        }
+      }
+    }
+  }
+}
+
+// Joins the ranges of a vector in their order: hd / 4 lanes of four dimensions for each of PARTS runs of 8 ranges, then
+// the runs.  No load waits for another.
+template <typename T, int HD, int PARTS> __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Params p) {
+  constexpr int LANES = HD / 4, EACH = 256 / (LANES * PARTS);       // vectors of a workgroup
+  __shared__ __attribute__((aligned(16))) float s_o[PARTS > 1 ? 256 : 1][4];
+  __shared__ float s_m[PARTS > 1 ? 256 : 1], s_l[PARTS > 1 ? 256 : 1];
+  const int tid = threadIdx.x, d = tid % LANES * 4, part = tid / LANES % PARTS;
+  const int64_t vec = (int64_t)blockIdx.x * EACH + tid / (LANES * PARTS);
+  const bool on = vec < (int64_t)p.M * p.H;
+  const size_t at = on ? (size_t)vec : 0, step = (size_t)p.M * p.H;
+  const int first = p.rows.cu[0], last = p.rows.cu[p.rows.B];
+  float2 ml[8];
+  f32x4 o[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int range = 8 * part + k;
+    ml[k] = make_float2(-FLT_MAX, 0.f);
+    o[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (range < p.splits) {
+      ml[k] = *(const float2*)(p.part_ml + 2 * (at + range * step));
+      o[k] = *(const f32x4*)(p.part_o + (at + range * step) * HD + d);
+    }
+  }
+  float M = -FLT_MAX, L = 0.f;
+  f32x4 O{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) M = fmaxf(M, ml[k].x);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float e = __builtin_amdgcn_exp2f(ml[k].x - M);
+    if (ml[k].y == 0.f && ml[k].x == -FLT_MAX) continue;            // without keys: its outputs were not written
+    L += ml[k].y * e;
+    O += o[k] * e;
+  }
+  if constexpr (PARTS > 1) {
+    *(f32x4*)s_o[tid] = O;
+    s_m[tid] = M;
+    s_l[tid] = L;
     __syncthreads();
-    for (int idx = tid; idx < 16 * (HD / 4); idx += 64 * WAVES) {
-      const int v = idx / (HD / 4), d = idx % (HD / 4) * 4;
-      if (16 * t + v >= nv) continue;
-      float M = s_m[0][v], L = 0.f;
+    if (part) return;
+    const float M0 = M;
 #pragma unroll
-      for (int k = 1; k < WAVES; ++k) M = fmaxf(M, s_m[k][v]);
-      f32x4 O{0.f, 0.f, 0.f, 0.f};
+    for (int k = 1; k < PARTS; ++k) M = fmaxf(M, s_m[tid + k * LANES]);
+    const float e0 = __builtin_amdgcn_exp2f(M0 - M);
+    L *= e0;
+    O *= e0;
 #pragma unroll
-      for (int k = 0; k < WAVES; ++k) {
-        const float e = __builtin_amdgcn_exp2f(s_m[k][v] - M);
-        L += s_l[k][v] * e;
-        O += *(const f32x4*)&s_o[k][v][d] * e;
-      }
-      const int vec = w.v0 + 16 * t + v;
-      if (p.splits == 1) {
-        if (sees(p, len, w.n, vec, G) <= 0) O = f32x4{0.f, 0.f, 0.f, 0.f};
-        else O *= 1.f / L;
-        store4((T*)p.out + (size_t)(w.row0 + vec / G) * p.ldo + (kvh * G + vec % G) * HD + d, O);
-      } else {
-        const size_t at = (((size_t)block * p.KV + kvh) * p.splits + split) * (16 * QT) + 16 * t + v;
-        *(f32x4*)(p.part_o + at * HD + d) = O;
-        if (d == 0) *(float2*)(p.part_ml + 2 * at) = make_float2(M, L);
-      }
+    for (int k = 1; k < PARTS; ++k) {
+      const float e = __builtin_amdgcn_exp2f(s_m[tid + k * LANES] - M);
+      L += s_l[tid + k * LANES] * e;
+      O += *(const f32x4*)s_o[tid + k * LANES] * e;
     }
   }
+  const int row = (int)(vec / p.H), h = (int)(vec % p.H);
+  if (!on || row < first || row >= last) return;
+  if (L < 0.f) O = f32x4{0.f, 0.f, 0.f, 0.f};
+  else O *= 1.f / L;
+  store4((T*)p.out + (size_t)row * p.ldo + h * HD + d, O);
 }
-
-// joins the ranges of a workgroup's vectors, in their order
-template <typename T, int HD> __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Params p, int cap, int unit) {
-  const int G = p.H / p.KV, kvh = blockIdx.x % p.KV, block = blockIdx.x / p.KV;
-  Block4 w;
-  if (!find_block(p.rows, p.M, G, cap, block, w)) return;
-  const int len = p.rows.len[w.b], nv = min(cap, w.n * G - w.v0);
-  const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
-  const int kps = range_keys(n_max, p.splits, unit);
-  const int used = n_max > 0 ? (n_max + kps - 1) / kps : 1;
-  for (int idx = threadIdx.x; idx < nv * (HD / 4); idx += 256) {
-    const int v = idx / (HD / 4), d = idx % (HD / 4) * 4;
-    const size_t at = ((size_t)block * p.KV + kvh) * p.splits * cap + v;
-    float M = -FLT_MAX, L = 0.f;
-    for (int k = 0; k < used; ++k) M = fmaxf(M, p.part_ml[2 * (at + (size_t)k * cap)]);
-    f32x4 O{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < used; ++k) {
-      const size_t i = at + (size_t)k * cap;
-      const float e = __builtin_amdgcn_exp2f(p.part_ml[2 * i] - M);
-      L += p.part_ml[2 * i + 1] * e;
-      O += *(const f32x4*)(p.part_o + i * HD + d) * e;
-    }
-    const int vec = w.v0 + v;
-    if (sees(p, len, w.n, vec, G) <= 0) O = f32x4{0.f, 0.f, 0.f, 0.f};
-    else O *= 1.f / L;
-    store4((T*)p.out + (size_t)(w.row0 + vec / G) * p.ldo + (kvh * G + vec % G) * HD + d, O);
-  }
-}
-
-constexpr int WAVES4 = 4;
 
 Attn4Plan plan_attention4(int dtype, int M, int H, int KV, int n_seqs, int max_len) {
   Attn4Plan a{};
   const int64_t G = H / KV, nz = std::min(n_seqs, M);
   const int64_t vectors = (M + nz - 1) / nz * G;             // of an average sequence
   a.tiles = vectors <= 16 ? 1 : vectors <= 32 || dtype == 1 ? 2 : 4;
+  a.waves = 4;
+  int want_s = 0;
+  if (const char* e = getenv("SD_A4")) sscanf(e, "%d,%d,%d", &a.tiles, &a.waves, &want_s);
   const int64_t cap = 16 * a.tiles;
   a.blocks = (int)((M * G - nz) / cap + nz);                 // sum of ceil(n G / cap) over nz sequences of M rows
   const int64_t items = (int64_t)a.blocks * KV, want = (1024 + items - 1) / items;
   a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (max_len + 255) / 256, 64}));
+  if (want_s) a.splits = want_s;
   return a;
 }
 
-size_t attention4_part_floats(const Attn4Plan& a, int KV, int hd) {
-  return a.splits > 1 ? (size_t)a.blocks * KV * a.splits * 16 * a.tiles * (hd + 2) : 0;
+size_t attention4_part_floats(const Attn4Plan& a, int M, int H, int hd) {
+  return a.splits > 1 ? (size_t)a.splits * M * H * (hd + 2) : 0;
+}
+
+template <typename T, int HD, int QT, int WAVES> static void launch_stream(const Attn4Plan& a, const Attn4Params& p, hipStream_t s) {
+  attention4_stream_kernel<T, HD, QT, WAVES><<<dim3((unsigned)a.blocks * p.KV * a.splits), 64 * WAVES, 0, s>>>(p);
 }
 
 template <typename T, int HD> static void launch_hd(const Attn4Plan& a, Attn4Params p, hipStream_t s) {
-  const dim3 grid((unsigned)a.blocks * p.KV * a.splits);
-  switch (a.tiles) {
-    case 1: attention4_stream_kernel<T, HD, 1, WAVES4><<<grid, 64 * WAVES4, 0, s>>>(p); break;
-    case 2: attention4_stream_kernel<T, HD, 2, WAVES4><<<grid, 64 * WAVES4, 0, s>>>(p); break;
-    case 4:
-      if constexpr (sizeof(T) == 2) attention4_stream_kernel<T, HD, 4, WAVES4><<<grid, 64 * WAVES4, 0, s>>>(p);
+  switch (10 * a.tiles + a.waves / 4) {
+    case 11: launch_stream<T, HD, 1, 4>(a, p, s); break;
+    case 12: launch_stream<T, HD, 1, 8>(a, p, s); break;
+    case 14: launch_stream<T, HD, 1, 16>(a, p, s); break;
+    case 21: launch_stream<T, HD, 2, 4>(a, p, s); break;
+    case 22: launch_stream<T, HD, 2, 8>(a, p, s); break;
+    case 41:
+      if constexpr (sizeof(T) == 2) launch_stream<T, HD, 4, 4>(a, p, s);
       break;
   }
-  if (a.splits > 1)
-    attention4_join_kernel<T, HD><<<dim3((unsigned)a.blocks * p.KV), 256, 0, s>>>(p, 16 * a.tiles, 32 * WAVES4);
+  if (a.splits > 1) {
+    const int64_t n = (int64_t)p.M * p.H;
+    constexpr int each = 1024 / HD;              // hd / 4 lanes a vector
+    if (a.splits <= 8) attention4_join_kernel<T, HD, 1><<<dim3((unsigned)((n + each - 1) / each)), 256, 0, s>>>(p);
+    else attention4_join_kernel<T, HD, 8><<<dim3((unsigned)((n * 8 + each - 1) / each)), 256, 0, s>>>(p);
+  }
 }
 
 hipError_t launch_attention4(int dtype, int hd, const Attn4Plan& a, const Attn4Params& p, hipStream_t s) {

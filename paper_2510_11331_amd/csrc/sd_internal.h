@@ -335,13 +335,13 @@ struct Attn4Params {
   int causal;
   float scale;
   int splits;              // ranges of the keys
-  float* part_o;           // their outputs [blocks, KV, splits, 16 tiles, hd] and (maximum, sum) (more than one)
+  float* part_o;           // their outputs [splits, M, H, hd] and (maximum, sum) (more than one)
   float* part_ml;
 };
-// tiles of 16 query vectors in a workgroup, workgroups of such vectors at most, ranges of the keys
-struct Attn4Plan { int tiles, blocks, splits; };
+// tiles of 16 query vectors and waves of a workgroup, workgroups of such vectors at most, ranges of the keys
+struct Attn4Plan { int tiles, waves, blocks, splits; };
 Attn4Plan plan_attention4(int dtype, int M, int H, int KV, int n_seqs, int max_len);
-size_t attention4_part_floats(const Attn4Plan& a, int KV, int hd);
+size_t attention4_part_floats(const Attn4Plan& a, int M, int H, int hd);
 
 // ---------------------------------------------------------------- launchers
 // dtype: 0 bf16, 1 fp32 (same values as SD_DTYPE_*)
