@@ -47,12 +47,18 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-template <int E> __device__ __forceinline__ uint32_t cvt4(uint32_t c, float s) {   // byte E
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, E));
+__device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <int E, bool F16 = false> __device__ __forceinline__ uint32_t cvt4(uint32_t c, float s) {   // byte E
+  if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, s, E));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, E));
 }
 __device__ __forceinline__ u32x4 cvt4_all(uint32_t c, float s) {
   return u32x4{cvt4<0>(c, s), cvt4<1>(c, s), cvt4<2>(c, s), cvt4<3>(c, s)};
@@ -156,6 +162,159 @@ template <int HD> struct Load4;            // what a lane has of a page's keys o
 template <> struct Load4<128> { typedef u32x4 type; };
 template <> struct Load4<64> { typedef u32x2 type; };
 
+// parts of a query, and of a weight that meets bf16 values
+template <typename T> constexpr int QUERY_PARTS = sizeof(T) == 2 ? 1 : 3;
+template <typename T> constexpr int WEIGHT_PARTS = sizeof(T) == 2 ? 2 : 3;
+
+// a vector's query as operands: lane (r, g) has dimensions (hd / 4) g + 8 s .. in k-step s
+template <typename T, int HD>
+__device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&q)[HD / 32][QUERY_PARTS<T>]) {
+#pragma unroll
+  for (int s = 0; s < HD / 32; ++s) {
+    if constexpr (sizeof(T) == 2) {
+      q[s][0] = ((const u32x4*)src)[s];
+      if (negative) q[s][0] ^= 0x80008000u;
+    } else {
+      const f32x4 a = ((const f32x4*)src)[2 * s], b = ((const f32x4*)src)[2 * s + 1];
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = negative ? -(e < 4 ? a[e] : b[e - 4]) : e < 4 ? a[e] : b[e - 4];
+      parts8<QUERY_PARTS<T>>(x, q[s]);
+    }
+  }
+}
+
+// Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> their weights x, with the running maximum m, the weights'
+// sum l and the outputs o that they go with.  edge: the vector sees the keys below vis only.
+template <int DT>
+__device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[2], float c, int key, int vis, float& m, float& l, f32x4 (&o)[DT],
+                                      float (&x)[8]) {
+  auto over = [&] {                              // in powers of two over the maximum
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(z[e / 4][e % 4], c, -m);
+    if (edge) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (key + 16 * (e / 4) + e % 4 >= vis) x[e] = -INFINITY;
+    }
+  };
+  over();
+  const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  if (__any(top > 8.f)) {
+    float most = -FLT_MAX;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e] == -INFINITY ? -FLT_MAX : z[e / 4][e % 4] * c);
+    const float to = fmaxf(m, quad_max(most)), old = __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    l *= old;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] *= old;
+    over();
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
+  l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
+// Two pages' values as a lane loads them (codes c, scales E) -> operands of tiles 2 B and 2 B + 1.  Byte B of a key holds
+// dimensions 2 B and 2 B + 1 of the lane's: pairs of dimensions of a key become pairs of keys of a dimension.
+template <int HD, int B, int PAGES, bool F16 = false>
+__device__ __forceinline__ void value_tiles(const typename Load4<HD>::type (&c)[PAGES], const float (&s)[PAGES][4],
+                                            uint32_t (&even)[2 * PAGES], uint32_t (&odd)[2 * PAGES]) {
+#pragma unroll
+  for (int e = 0; e < 2 * PAGES; ++e) {
+    const int t = e / 2, k = 2 * (e % 2);
+    uint32_t a, b;
+    if constexpr (HD == 128) {
+      a = cvt4<B, F16>(c[t][k], s[t][k]);
+      b = cvt4<B, F16>(c[t][k + 1], s[t][k + 1]);
+    } else {
+      a = cvt4<B, F16>(c[t][k / 2], s[t][k]);
+      b = cvt4<B + 2, F16>(c[t][k / 2], s[t][k + 1]);
+    }
+    even[e] = low_halves(a, b);
+    odd[e] = high_halves(a, b);
+  }
+}
+template <int PAGES> __device__ __forceinline__ void value_scales(const uint32_t (&E)[PAGES], float (&s)[PAGES][4]) {
+#pragma unroll
+  for (int t = 0; t < PAGES; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[t][e] = scale4(__builtin_amdgcn_ubfe(E[t], 8 * e, 8));
+}
+
+// o += the step's values, of two pages in registers, times the weights
+template <int HD, int QT, int PP>
+__device__ __forceinline__ void add_values(const typename Load4<HD>::type (&c)[2], const uint32_t (&E)[2],
+                                           const u32x4 (&w)[QT][PP], f32x4 (&o)[QT][HD / 16]) {
+  float s[2][4];
+  value_scales(E, s);
+  [&]<int... B>(std::integer_sequence<int, B...>) {
+    (([&] {
+       uint32_t even[4], odd[4];
+       value_tiles<HD, B>(c, s, even, odd);
+       const u32x4 a{even[0], even[1], even[2], even[3]}, b{odd[0], odd[1], odd[2], odd[3]};
+#pragma unroll
+       for (int u = 0; u < QT; ++u)
+#pragma unroll
+         for (int part = PP - 1; part >= 0; --part) {
+           o[u][2 * B] = mfma_bf16(a, w[u][part], o[u][2 * B]);
+           o[u][2 * B + 1] = mfma_bf16(b, w[u][part], o[u][2 * B + 1]);
+         }
+     }()),
+     ...);
+  }(std::make_integer_sequence<int, HD / 32>{});
+}
+
+// Values that not every vector sees must be finite: their weights are zero where they are not seen, and a NaN that a
+// vector does see is put into its output by put_nan.  key: the lane's first; no: pages that are none.  Whether there was
+// such a NaN.
+__device__ __forceinline__ bool clean_scales(uint32_t (&E)[2], int key, int n_max, uint32_t no) {
+  bool nan = false;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool is_nan = (E[t] >> (8 * e) & 255u) == 255u, none = key + 16 * t + e >= n_max || (no >> t & 1);
+      nan |= is_nan && !none;
+      if (is_nan || none) E[t] = (E[t] & ~(255u << (8 * e))) | 127u << (8 * e);
+    }
+  return nan;
+}
+// the value blocks of NaN among the step's keys; all of a lane's outputs are of scale block (hd / 4) g / 32
+template <int HD, int QT>
+__device__ __forceinline__ void put_nan(const uint8_t* const (&pages)[2], uint32_t no, int key0, int n_max, int g,
+                                        const int (&vis)[QT], f32x4 (&o)[QT][HD / 16]) {
+  for (int key = key0; key < min(key0 + 32, n_max); ++key) {
+    const int t = key - key0 >= 16;
+    if ((no >> t & 1) || pages[t][Page4<HD>::value_scale(key & 15, g * (HD / 4) / 32)] != 255) continue;
+#pragma unroll
+    for (int u = 0; u < QT; ++u)
+      if (key < vis[u])
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) o[u][d] = f32x4{NAN, NAN, NAN, NAN};
+  }
+}
+
+// A joined vector's four dimensions: the output itself, or a range's part of it
+template <typename T, int HD>
+__device__ __forceinline__ void emit(const Attn4Params& p, int split, int row, int h, int d, bool sees_any, float M, float L, f32x4 O) {
+  if (p.splits == 1) {
+    if (!sees_any) O = f32x4{0.f, 0.f, 0.f, 0.f};
+    else O *= 1.f / L;
+    store4((T*)p.out + (size_t)row * p.ldo + h * HD + d, O);
+  } else {
+    const size_t at = ((size_t)split * p.M + row) * p.H + h;
+    *(f32x4*)(p.part_o + at * HD + d) = O;
+    // (a sum of -1: of nothing to see, which the joined output is zero for)
+    if (d == 0) *(float2*)(p.part_ml + 2 * at) = sees_any ? make_float2(M, L) : make_float2(0.f, -1.f);
+  }
+}
+// a range without keys
+__device__ __forceinline__ void emit_nothing(const Attn4Params& p, int split, int row, int h, bool sees_any) {
+  *(float2*)(p.part_ml + 2 * (((size_t)split * p.M + row) * p.H + h)) = sees_any ? make_float2(-FLT_MAX, 0.f) : make_float2(0.f, -1.f);
+}
+
 // waves that a SIMD is to hold at once, for which the compiler keeps to so many registers
 template <typename T, int QT> constexpr int MIN_WAVES = QT == 1 ? (sizeof(T) == 2 ? 4 : 3) : QT == 2 ? 2 : 1;
 
@@ -165,8 +324,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
   using L4 = typename Load4<HD>::type;
   constexpr int KS = HD / 32;                    // k-steps of a score
   constexpr int DT = HD / 16;                    // output tiles, dimensions of a lane's values
-  constexpr int QP = sizeof(T) == 2 ? 1 : 3;     // parts of a query
-  constexpr int PP = sizeof(T) == 2 ? 2 : 3;     // parts of a weight
+  constexpr int QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
   constexpr int PH = WAVES / 4, IP = 4 / PH;     // the outputs are joined in PH parts, which LDS has room for
   __shared__ __attribute__((aligned(16))) float s_o[WAVES][16][HD / PH + 4];
   __shared__ float s_m[WAVES][16], s_l[WAVES][16];
@@ -183,16 +341,12 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
   const int n_min = sees(p, len, w.n, w.v0, G);  // what all of them see
   const int kps = range_keys(n_max, p.splits, 32 * WAVES);
   const int k0 = split * kps, k1 = min(k0 + kps, n_max);
-  if (split > 0 && k0 >= k1) {                   // a range without keys
-    if (tid < nv) {
-      const int vec = w.v0 + tid;
-      const size_t at = ((size_t)split * p.M + w.row0 + vec / G) * p.H + kvh * G + vec % G;
-      *(float2*)(p.part_ml + 2 * at) = sees(p, len, w.n, vec, G) > 0 ? make_float2(-FLT_MAX, 0.f) : make_float2(0.f, -1.f);
-    }
+  if (split > 0 && k0 >= k1) {
+    const int vec = w.v0 + tid;
+    if (tid < nv) emit_nothing(p, split, w.row0 + vec / G, kvh * G + vec % G, sees(p, len, w.n, vec, G) > 0);
     return;
   }
 
-  // queries, as operands: lane (r, g) has dimensions (hd / 4) g + 8 s .. of vector r in k-step s
   u32x4 q[QT][KS][QP];
   int vis[QT];
 #pragma unroll
@@ -200,19 +354,8 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
     const int v = w.v0 + 16 * t + r;
     const bool on = 16 * t + r < nv;
     vis[t] = on ? sees(p, len, w.n, v, G) : 0;
-    const T* const src = (const T*)p.q + (size_t)(w.row0 + (on ? v / G : 0)) * p.ldq + (kvh * G + (on ? v % G : 0)) * HD + g * (HD / 4);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      if constexpr (sizeof(T) == 2) {
-        q[t][s][0] = ((const u32x4*)src)[s];
-        if (p.scale < 0.f) q[t][s][0] ^= 0x80008000u;      // the sign of the scale goes into the queries
-      } else {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = p.scale < 0.f ? -src[8 * s + e] : src[8 * s + e];
-        parts8<QP>(x, q[t][s]);
-      }
-    }
+    load_query<T, HD>((const T*)p.q + (size_t)(w.row0 + (on ? v / G : 0)) * p.ldq + (kvh * G + (on ? v % G : 0)) * HD + g * (HD / 4),
+                      p.scale < 0.f, q[t]);                // the sign of the scale goes into the queries
   }
   const float c = fabsf(p.scale) * 1.4426950408889634f;
 
@@ -310,97 +453,14 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       float x[8];
-      auto weights = [&] {                       // in powers of two over the running maximum
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x[e] = fmaf(z[u][e / 4][e % 4], c, -m[u]);
-          if (EDGE && key0 + 16 * (e / 4) + 4 * g + e % 4 >= vis[u]) x[e] = -INFINITY;
-        }
-      };
-      weights();
-      const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__any(top > 8.f)) {
-        float most = -FLT_MAX;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, EDGE && x[e] == -INFINITY ? -FLT_MAX : z[u][e / 4][e % 4] * c);
-        const float to = fmaxf(m[u], quad_max(most)), old = __builtin_amdgcn_exp2f(m[u] - to);
-        m[u] = to;
-        l[u] *= old;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[u][d] *= old;
-        weights();
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
-      l[u] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      weigh(EDGE, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x);
       parts8<PP>(x, w8[u]);
     }
 
-    bool nan_v = false;
-    uint32_t vs[2] = {vE[0], vE[1]};
-    if constexpr (EDGE) {
-      // values that not every vector sees must be finite: their weights are zero where they are not seen, and NaN
-      // that a vector does see is put into its output below
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const int key = key0 + 16 * t + 4 * g + i4;
-          const bool is_nan = (vs[t] >> (8 * i4) & 255u) == 255u, none = key >= n_max || (no_here >> t & 1);
-          nan_v |= is_nan && !none;
-          if (is_nan || none) vs[t] = (vs[t] & ~(255u << (8 * i4))) | 127u << (8 * i4);
-        }
-    }
-    // byte b of a key's values: dimensions 2 b and 2 b + 1 of the lane's; pairs of dimensions of a key become pairs of
-    // keys of a dimension
-    float sv[2][4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sv[t][e] = scale4(__builtin_amdgcn_ubfe(vs[t], 8 * e, 8));
-    [&]<int... B>(std::integer_sequence<int, B...>) {
-      (([&] {
-         u32x4 even, odd;
-#pragma unroll
-         for (int e = 0; e < 4; ++e) {
-           const int t = e / 2, k = 2 * (e % 2);
-           uint32_t a, b;
-           if constexpr (HD == 128) {
-             a = cvt4<B>(vc[t][k], sv[t][k]);
-             b = cvt4<B>(vc[t][k + 1], sv[t][k + 1]);
-           } else {
-             a = cvt4<B>(vc[t][k / 2], sv[t][k]);
-             b = cvt4<B + 2>(vc[t][k / 2], sv[t][k + 1]);
-           }
-           even[e] = low_halves(a, b);
-           odd[e] = high_halves(a, b);
-         }
-#pragma unroll
-         for (int u = 0; u < QT; ++u)
-#pragma unroll
-           for (int part = PP - 1; part >= 0; --part) {
-             o[u][2 * B] = mfma_bf16(even, w8[u][part], o[u][2 * B]);
-             o[u][2 * B + 1] = mfma_bf16(odd, w8[u][part], o[u][2 * B + 1]);
-           }
-       }()),
-       ...);
-    }(std::make_integer_sequence<int, HD / 32>{});
-
+    const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here);
+    add_values<HD>(vc, vE, w8, o);
     load_v();
-
-    if (EDGE && __any(nan_v)) {                  // rare: a value block of NaN that some vector sees
-      // all of a lane's outputs are of scale block (hd / 4) g / 32
-      for (int key = key0; key < min(key0 + 32, n_max); ++key) {
-        const int t = key - key0 >= 16;
-        if (!(no_here >> t & 1) && here[t][P::value_scale(key & 15, g * (HD / 4) / 32)] == 255) {
-#pragma unroll
-          for (int u = 0; u < QT; ++u)
-            if (key < vis[u])
-#pragma unroll
-              for (int d = 0; d < DT; ++d) o[u][d] = f32x4{NAN, NAN, NAN, NAN};
-        }
-      }
-    }
+    if (EDGE && __any(nan)) put_nan<HD>(here, no_here, key0, n_max, g, vis, o);
   };
 
   if (left > 0) {
@@ -447,18 +507,256 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
           O += *(const f32x4*)&s_o[k][v][col] * e;
         }
         const int vec = w.v0 + 16 * t + v, row = w.row0 + vec / G, h = kvh * G + vec % G;
-        if (p.splits == 1) {
-          if (sees(p, len, w.n, vec, G) <= 0) O = f32x4{0.f, 0.f, 0.f, 0.f};
-          else O *= 1.f / L;
-          store4((T*)p.out + (size_t)row * p.ldo + h * HD + d, O);
-        } else {
-          const size_t at = ((size_t)split * p.M + row) * p.H + h;
-          *(f32x4*)(p.part_o + at * HD + d) = O;
-          // (a sum of -1: of nothing to see, which the joined output is zero for)
-          if (d == 0) *(float2*)(p.part_ml + 2 * at) = sees(p, len, w.n, vec, G) > 0 ? make_float2(M, L) : make_float2(0.f, -1.f);
-        }
+        emit<T, HD>(p, split, row, h, d, sees(p, len, w.n, vec, G) > 0, M, L, O);
       }
     }
+  }
+}
+
+// Prefill: 64 QT vectors a workgroup, 16 QT a wave, and the keys in LDS: each wave converts a quarter of a step's 32 keys
+// for all four, while they take the step before it.
+//
+// bf16 outputs: the values are held as fp16, which their codes times scales of 2^-23 to 2^13 are exactly, so that a weight
+// is one fp16 part (off by 2^-12 of itself, an eighth of the output's own rounding) and half the products of the second
+// matrix are saved.  A step with a value outside that range (or with NaN) is taken from the cache in bf16, as above.  fp32 outputs: values in
+// bf16 and three parts.
+template <typename T, int HD, int QT>
+__global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) {
+  using P = Page4<HD>;
+  using L4 = typename Load4<HD>::type;
+  constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
+  constexpr bool F16 = sizeof(T) == 2;
+  __shared__ u32x4 s_k[2][2][KS][64];            // [buffer][page][k-step][lane]
+  __shared__ u32x4 s_v[2][DT][64];               // [buffer][tile][lane]: four keys of either page
+  __shared__ int s_direct[2];                    // step + 1 whose values are not in LDS
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const int G = p.H / p.KV;
+  const int kvh = blockIdx.x % p.KV, split = blockIdx.x / p.KV % p.splits;
+  const int block = p.blocks - 1 - (int)(blockIdx.x / p.KV / p.splits);      // the rows that see most go first
+  Block4 w;
+  if (!find_block(p.rows, p.M, G, 64 * QT, block, w)) return;
+  const int len = w.len;
+  const int nv = min(64 * QT, w.n * G - w.v0);
+  const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
+  const int kps = range_keys(n_max, p.splits, 32);
+  const int k0 = split * kps, k1 = min(k0 + kps, n_max);
+  if (split > 0 && k0 >= k1) {
+    const int vec = w.v0 + tid;
+    if (tid < nv) emit_nothing(p, split, w.row0 + vec / G, kvh * G + vec % G, sees(p, len, w.n, vec, G) > 0);
+    return;
+  }
+
+  // this wave's vectors
+  const int first = w.v0 + 16 * QT * wave, on = min(16 * QT, nv - 16 * QT * wave);
+  const int mine_min = on > 0 ? sees(p, len, w.n, first, G) : 0;
+  const int mine_max = on > 0 ? min(k1, sees(p, len, w.n, first + on - 1, G)) : 0;
+  u32x4 q[QT][KS][QP];
+  int vis[QT];
+  float m[QT], l[QT];
+  f32x4 o[QT][DT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int v = first + 16 * t + r;
+    const bool is = 16 * t + r < on;
+    vis[t] = is ? sees(p, len, w.n, v, G) : 0;
+    load_query<T, HD>((const T*)p.q + (size_t)(w.row0 + (is ? v / G : 0)) * p.ldq + (kvh * G + (is ? v % G : 0)) * HD + g * (HD / 4),
+                      p.scale < 0.f, q[t]);
+    m[t] = -FLT_MAX;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c = fabsf(p.scale) * 1.4426950408889634f;
+
+  // Conversion: wave 2 a + b takes half a of page b of a step: k-steps KS / 2 a .., and tiles DT / 2 a .. of all 16 keys.
+  // Lane l of ids holds its page of step 64 j + l.
+  const int half = wave >> 1, mypage = wave & 1;
+  const uint8_t* const head = p.pool + (size_t)kvh * P::BYTES;
+  const size_t page_bytes = (size_t)p.KV * P::BYTES;
+  const int32_t* const table = p.rows.table + (size_t)w.b * p.rows.W;
+  const int steps = (k1 - k0 + 31) / 32;
+  const uint32_t off_k = P::key(r, g * (HD / 4) + half * (HD / 8)), off_v = P::value(4 * g, r);
+  const uint32_t off_ks = P::key_scale(r, g * (HD / 4) / 32), off_vs = P::value_scale(4 * g, r * DT / 32);
+  auto page_id = [&](int i0, bool& no) {
+    const int pg = k0 / 16 + 2 * (i0 + lane) + mypage;
+    int id = 0;
+    no = false;
+    if (16 * pg < k1) {
+      id = pg < p.rows.W ? table[pg] : -1;
+      no = (unsigned)id >= (unsigned)p.n_blocks;
+    }
+    return no ? 0 : id;
+  };
+  int ids = 0;
+  uint64_t no_ids = 0;
+  uint32_t kc[KS / 2], kE, vE;
+  L4 vc;
+  bool none;
+  auto load = [&](int i) {                       // of step i, in order
+    if (i % 64 == 0) {
+      bool no;
+      ids = page_id(i, no);
+      no_ids = __ballot(no);
+    }
+    const uint8_t* const pg = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, i % 64) * page_bytes;
+    none = no_ids >> (i % 64) & 1;
+    if constexpr (KS == 4) {
+      const u32x2 k = *(const u32x2*)(pg + off_k);
+      kc[0] = k[0];
+      kc[1] = k[1];
+    } else {
+      kc[0] = *(const uint32_t*)(pg + off_k);
+    }
+    kE = pg[off_ks];
+    vc = *(const L4*)(pg + off_v);
+    vE = *(const uint32_t*)(pg + off_vs);
+  };
+  auto convert = [&](int i) {                    // what load left, into the buffer of step i
+    const float ks = scale4(none ? 255u : kE);
+#pragma unroll
+    for (int s = 0; s < KS / 2; ++s) s_k[i & 1][mypage][half * (KS / 2) + s][lane] = cvt4_all(kc[s], ks);
+    const int key = k0 + 32 * i + 16 * mypage + 4 * g;
+    bool direct = false;
+    if (none) {                                  // (its keys are NaN)
+      vc = L4{};
+      vE = 0x7f7f7f7fu;
+    }
+    if (k0 + 32 * i + 32 > n_max) {              // no value behind the last key
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (key + e >= n_max) {
+          if constexpr (HD == 128) vc[e] = 0;
+          else vc[e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
+          vE = (vE & ~(255u << (8 * e))) | 127u << (8 * e);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t E = __builtin_amdgcn_ubfe(vE, 8 * e, 8);
+      uint32_t codes;
+      if constexpr (HD == 128) codes = vc[e];
+      else codes = e & 1 ? vc[e / 2] >> 16 : vc[e / 2] & 0xffffu;
+      direct |= F16 ? E - 104u > 36u && ((codes & 0x77777777u) != 0 || E == 255u) : E == 255u;
+    }
+    if (__any(direct) && lane == 0) s_direct[i & 1] = i + 1;
+    float s[1][4];
+    const uint32_t Es[1] = {vE};
+    value_scales(Es, s);
+    const L4 cs[1] = {vc};
+    [&]<int... B>(std::integer_sequence<int, B...>) {
+      (([&] {
+         if (B / (DT / 4) != half) return;
+         uint32_t even[2], odd[2];
+         value_tiles<HD, B, 1, F16>(cs, s, even, odd);
+         ((u32x2*)&s_v[i & 1][2 * B][lane])[mypage] = u32x2{even[0], even[1]};
+         ((u32x2*)&s_v[i & 1][2 * B + 1][lane])[mypage] = u32x2{odd[0], odd[1]};
+       }()),
+       ...);
+    }(std::make_integer_sequence<int, HD / 32>{});
+  };
+
+  auto take = [&](int i, int key0) {
+    const int buf = i & 1;
+    const bool edge = key0 + 32 > mine_min;
+    f32x4 z[QT][2];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) z[u][0] = z[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 k = s_k[buf][t][s][lane];
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(k, q[u][s][part], z[u][t]);
+      }
+    float x[QT][8];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) weigh(edge, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x[u]);
+    if (s_direct[buf] == i + 1) {                // rare
+      const uint8_t* pages[2];
+      uint32_t no = 0;
+      L4 c2[2];
+      uint32_t E2[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int pg = key0 / 16 + t;
+        int id = 16 * pg >= k1 ? 0 : pg < p.rows.W ? __builtin_amdgcn_readfirstlane(table[pg]) : -1;
+        if ((unsigned)id >= (unsigned)p.n_blocks) {
+          id = 0;
+          no |= 1u << t;
+        }
+        pages[t] = head + (size_t)(uint32_t)id * page_bytes;
+        c2[t] = *(const L4*)(pages[t] + off_v);
+        E2[t] = *(const uint32_t*)(pages[t] + off_vs);
+      }
+      const bool nan = clean_scales(E2, key0 + 4 * g, n_max, no);
+      u32x4 w8[QT][PP];
+#pragma unroll
+      for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
+      add_values<HD>(c2, E2, w8, o);
+      const uint8_t* const at[2] = {pages[0], pages[1]};
+      if (__any(nan)) put_nan<HD>(at, no, key0, n_max, g, vis, o);
+      return;
+    }
+    if constexpr (F16) {
+      u32x4 w8[QT];
+#pragma unroll
+      for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w8[u][e] = __builtin_bit_cast(uint32_t, f16x2{(f16_t)x[u][2 * e], (f16_t)x[u][2 * e + 1]});
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const u32x4 v = s_v[buf][d][lane];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) o[u][d] = mfma_f16(v, w8[u], o[u][d]);
+      }
+    } else {
+      u32x4 w8[QT][PP];
+#pragma unroll
+      for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const u32x4 v = s_v[buf][d][lane];
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int part = PP - 1; part >= 0; --part) o[u][d] = mfma_bf16(v, w8[u][part], o[u][d]);
+      }
+    }
+  };
+
+  if (tid < 2) s_direct[tid] = 0;
+  __syncthreads();
+  if (steps > 0) {
+    load(0);
+    convert(0);
+    if (steps > 1) load(1);
+  }
+  __syncthreads();
+  for (int i = 0; i < steps; ++i) {
+    if (i + 1 < steps) convert(i + 1);
+    if (i + 2 < steps) load(i + 2);
+    const int key0 = k0 + 32 * i;
+    if (key0 < mine_max) take(i, key0);
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const float sum = quad_sum(l[t]);
+    const int vec = first + 16 * t + r;
+    if (16 * t + r >= on) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int d = 0; d < DT; d += 4)
+        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], sum,
+                    f32x4{o[t][d][e], o[t][d + 1][e], o[t][d + 2][e], o[t][d + 3][e]});
   }
 }
 
@@ -530,6 +828,7 @@ Attn4Plan plan_attention4(int dtype, int M, int H, int KV, int n_seqs, int max_l
   a.waves = 4;
   int want_s = 0;
   if (const char* e = getenv("SD_A4")) sscanf(e, "%d,%d,%d", &a.tiles, &a.waves, &want_s);
+  if (a.waves == 0) a.tiles = dtype == 1 ? 4 : 8;     // tile kernel
   const int64_t cap = 16 * a.tiles;
   a.blocks = (int)((M * G - nz) / cap + nz);                 // sum of ceil(n G / cap) over nz sequences of M rows
   const int64_t items = (int64_t)a.blocks * KV, want = (1024 + items - 1) / items;
@@ -547,10 +846,13 @@ template <typename T, int HD, int QT, int WAVES> static void launch_stream(const
 }
 
 template <typename T, int HD> static void launch_hd(const Attn4Plan& a, Attn4Params p, hipStream_t s) {
-  switch (10 * a.tiles + a.waves / 4) {
+  p.blocks = a.blocks;
+  if (a.waves == 0) {
+    constexpr int QT = sizeof(T) == 2 ? 2 : 1;
+    attention4_tile_kernel<T, HD, QT><<<dim3((unsigned)a.blocks * p.KV * a.splits), 256, 0, s>>>(p);
+  } else switch (10 * a.tiles + a.waves / 4) {
     case 11: launch_stream<T, HD, 1, 4>(a, p, s); break;
     case 12: launch_stream<T, HD, 1, 8>(a, p, s); break;
-    case 14: launch_stream<T, HD, 1, 16>(a, p, s); break;
     case 21: launch_stream<T, HD, 2, 4>(a, p, s); break;
     case 22: launch_stream<T, HD, 2, 8>(a, p, s); break;
     case 41:

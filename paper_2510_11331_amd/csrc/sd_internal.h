@@ -334,7 +334,7 @@ struct Attn4Params {
   KvRows rows;
   int causal;
   float scale;
-  int splits;              // ranges of the keys
+  int blocks, splits;      // workgroups of vectors at most, ranges of the keys
   float* part_o;           // their outputs [splits, M, H, hd] and (maximum, sum) (more than one)
   float* part_ml;
 };

@@ -99,18 +99,19 @@ def norm_rope(x, gain, cs, eps):
 
 
 def attention(q, k, v, seen, scale):
-    """q [n, H, hd], k and v [len, KV, hd], seen [n, len] -> (out, what fp32 arithmetic may be off by before its
-    rounding to the output's type).
+    """q [n, H, hd], k and v [len, KV, hd], seen [n, len] -> (out, err): what the arithmetic may be off by before its
+    rounding to the output's type, err[0] of fp32 and err[1] of bf16 outputs.
 
     A score is a sum of hd products, off by at most (hd + 4) steps (2 U32 each: the matrix unit may cut) of the sum of
     their magnitudes; a weight by e^(twice that), and by the rounding of the exponential's argument and result
-    (8 + |score|) steps.  The weighted sum and the weights' sum are of at most n / 2 + 128 additions in a row.  Weights
-    enter the product in at least 16 bits (2^-16) for bf16 outputs, in 23 for fp32 ones: the caller adds that.  A weight
+    (8 + |score|) steps.  The weighted sum and the weights' sum are of at most n / 2 + 128 additions in a row.  A weight
     is held relative to the largest, which is 1, in fp32, whose normal numbers end at 2^-126: what is smaller may be
-    lost, from the weight and from the parts it is split into (at most three)."""
+    lost, from the weight and from the parts it is split into (at most three).  It enters the product in 23 bits for
+    fp32 outputs; for bf16 ones as two bf16 parts or as one fp16 number: 11 bits, a step's half being 2^-12 of it, and
+    2^-25 below fp16's normal numbers."""
     n, H, hd = q.shape
     KV = k.shape[1]
-    out, err = np.zeros((n, H, hd)), np.zeros((n, H, hd))
+    out, err = np.zeros((n, H, hd)), np.zeros((2, n, H, hd))
     with np.errstate(invalid="ignore", over="ignore"):
         for h in range(H):
             j = h // (H // KV)
@@ -126,5 +127,8 @@ def attention(q, k, v, seen, scale):
                 out[i, h] = p @ vv
                 e = 2 * (hd + 4) * 2 * U32 * mag.max() + (8 + np.abs(z).max()) * 2 * U32 + (m.sum() / 2 + 128) * 2 * U32
                 # of the weighted sum, and of the sum that it is divided by
-                err[i, h] = 2 * e * (p @ np.abs(vv)) + 4 * m.sum() * 2.0 ** -126 * np.abs(vv).max(0)
+                a, top = p @ np.abs(vv), np.abs(vv).max(0)
+                err[:, i, h] = 2 * e * a + 4 * m.sum() * 2.0 ** -126 * top
+                err[0, i, h] += 2.0 ** -23 * a
+                err[1, i, h] += 2.0 ** -12 * a + m.sum() * 2.0 ** -25 * top
     return out, err
