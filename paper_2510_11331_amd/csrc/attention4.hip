@@ -162,6 +162,24 @@ template <int HD> struct Load4;            // what a lane has of a page's keys o
 template <> struct Load4<128> { typedef u32x4 type; };
 template <> struct Load4<64> { typedef u32x2 type; };
 
+// A page of one head as a buffer: its address is the wave's, a lane's offset within it does not change from page to
+// page, so that a load costs no vector arithmetic.
+template <int HD> __device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const uint8_t* pg) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pg), (short)0, Page4<HD>::BYTES, 0x00020000);
+}
+template <typename V> __device__ __forceinline__ V page_load(__amdgpu_buffer_rsrc_t b, uint32_t off) {
+  if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0));
+  else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(b, off, 0, 0));
+  else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
+  else return __builtin_amdgcn_raw_buffer_load_b8(b, off, 0, 0);
+}
+// every wave's LDS accesses are done; loads from memory stay in flight
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // parts of a query, and of a weight that meets bf16 values
 template <typename T> constexpr int QUERY_PARTS = sizeof(T) == 2 ? 1 : 3;
 template <typename T> constexpr int WEIGHT_PARTS = sizeof(T) == 2 ? 2 : 3;
@@ -186,8 +204,9 @@ __device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&
 
 // Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> their weights x, with the running maximum m, the weights'
 // sum l and the outputs o that they go with.  edge: the vector sees the keys below vis only.
+// Whether the maximum has moved.
 template <int DT>
-__device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[2], float c, int key, int vis, float& m, float& l, f32x4 (&o)[DT],
+__device__ __forceinline__ bool weigh(bool edge, const f32x4 (&z)[2], float c, int key, int vis, float& m, float& l, f32x4 (&o)[DT],
                                       float (&x)[8]) {
   auto over = [&] {                              // in powers of two over the maximum
 #pragma unroll
@@ -199,8 +218,12 @@ __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[2], float c, i
     }
   };
   over();
-  const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-  if (__any(top > 8.f)) {
+  bool moved = false;
+  // (as integers: negative numbers below all others, NaN above)
+  int top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, __float_as_int(x[e]));
+  if (__any(top > 0x41000000)) {                 // 8.0
     float most = -FLT_MAX;
 #pragma unroll
     for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e] == -INFINITY ? -FLT_MAX : z[e / 4][e % 4] * c);
@@ -210,10 +233,14 @@ __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[2], float c, i
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] *= old;
     over();
+    moved = true;
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
-  l += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+  return moved;
+}
+__device__ __forceinline__ float sum8(const float (&x)[8]) {
+  return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
 // Two pages' values as a lane loads them (codes c, scales E) -> operands of tiles 2 B and 2 B + 1.  Byte B of a key holds
@@ -404,16 +431,18 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
     no = (uint32_t)(no_ids >> (2 * i)) & 3u;
   };
   auto load_k = [&]() {
-    kc[0] = *(const L4*)(pg0 + off_k);
-    kE[0] = pg0[off_ks];
-    kc[1] = *(const L4*)(pg1 + off_k);
-    kE[1] = pg1[off_ks];
+    const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
+    kc[0] = page_load<L4>(b0, off_k);
+    kE[0] = page_load<uint8_t>(b0, off_ks);
+    kc[1] = page_load<L4>(b1, off_k);
+    kE[1] = page_load<uint8_t>(b1, off_ks);
   };
   auto load_v = [&]() {
-    vc[0] = *(const L4*)(pg0 + off_v);
-    vE[0] = *(const uint32_t*)(pg0 + off_vs);
-    vc[1] = *(const L4*)(pg1 + off_v);
-    vE[1] = *(const uint32_t*)(pg1 + off_vs);
+    const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
+    vc[0] = page_load<L4>(b0, off_v);
+    vE[0] = page_load<uint32_t>(b0, off_vs);
+    vc[1] = page_load<L4>(b1, off_v);
+    vE[1] = page_load<uint32_t>(b1, off_vs);
   };
 
   int key0 = k0 + 32 * wave, left = steps, at = 0;       // at: of the step after this one, within ids
@@ -454,6 +483,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
     for (int u = 0; u < QT; ++u) {
       float x[8];
       weigh(EDGE, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x);
+      l[u] += sum8(x);
       parts8<PP>(x, w8[u]);
     }
 
@@ -516,7 +546,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 // Prefill: 64 QT vectors a workgroup, 16 QT a wave, and the keys in LDS: each wave converts a quarter of a step's 32 keys
 // for all four, while they take the step before it.
 //
-// bf16 outputs: the values are held as fp16, which their codes times scales of 2^-23 to 2^13 are exactly, so that a weight
+// bf16 outputs: the values are held as fp16, which their codes times scales of 2^-23 to 2^8 are exactly, so that a weight
 // is one fp16 part (off by 2^-12 of itself, an eighth of the output's own rounding) and half the products of the second
 // matrix are saved.  A step with a value outside that range (or with NaN) is taken from the cache in bf16, as above.  fp32 outputs: values in
 // bf16 and three parts.
@@ -554,8 +584,8 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   const int mine_max = on > 0 ? min(k1, sees(p, len, w.n, first + on - 1, G)) : 0;
   u32x4 q[QT][KS][QP];
   int vis[QT];
-  float m[QT], l[QT];
-  f32x4 o[QT][DT];
+  float m[QT], no_sum = 0.f;
+  f32x4 o[QT][DT], l[QT];                        // l: the weights' sum, four times, as the product with a tile of ones
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     const int v = first + 16 * t + r;
@@ -564,7 +594,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
     load_query<T, HD>((const T*)p.q + (size_t)(w.row0 + (is ? v / G : 0)) * p.ldq + (kvh * G + (is ? v % G : 0)) * HD + g * (HD / 4),
                       p.scale < 0.f, q[t]);
     m[t] = -FLT_MAX;
-    l[t] = 0.f;
+    l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -600,25 +630,24 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
       ids = page_id(i, no);
       no_ids = __ballot(no);
     }
-    const uint8_t* const pg = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, i % 64) * page_bytes;
+    const auto pg = page_buffer<HD>(head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, i % 64) * page_bytes);
     none = no_ids >> (i % 64) & 1;
     if constexpr (KS == 4) {
-      const u32x2 k = *(const u32x2*)(pg + off_k);
+      const u32x2 k = page_load<u32x2>(pg, off_k);
       kc[0] = k[0];
       kc[1] = k[1];
     } else {
-      kc[0] = *(const uint32_t*)(pg + off_k);
+      kc[0] = page_load<uint32_t>(pg, off_k);
     }
-    kE = pg[off_ks];
-    vc = *(const L4*)(pg + off_v);
-    vE = *(const uint32_t*)(pg + off_vs);
+    kE = page_load<uint8_t>(pg, off_ks);
+    vc = page_load<L4>(pg, off_v);
+    vE = page_load<uint32_t>(pg, off_vs);
   };
   auto convert = [&](int i) {                    // what load left, into the buffer of step i
     const float ks = scale4(none ? 255u : kE);
 #pragma unroll
     for (int s = 0; s < KS / 2; ++s) s_k[i & 1][mypage][half * (KS / 2) + s][lane] = cvt4_all(kc[s], ks);
     const int key = k0 + 32 * i + 16 * mypage + 4 * g;
-    bool direct = false;
     if (none) {                                  // (its keys are NaN)
       vc = L4{};
       vE = 0x7f7f7f7fu;
@@ -632,15 +661,19 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
           vE = (vE & ~(255u << (8 * e))) | 127u << (8 * e);
         }
     }
+    // the four scales at once: E + 24 of 128 to 159 (a carry from a byte is of one that is outside)
+    if (__any(((vE + 0x18181818u) & 0xe0e0e0e0u) != 0x80808080u)) {
+      bool direct = false;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t E = __builtin_amdgcn_ubfe(vE, 8 * e, 8);
-      uint32_t codes;
-      if constexpr (HD == 128) codes = vc[e];
-      else codes = e & 1 ? vc[e / 2] >> 16 : vc[e / 2] & 0xffffu;
-      direct |= F16 ? E - 104u > 36u && ((codes & 0x77777777u) != 0 || E == 255u) : E == 255u;
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t E = __builtin_amdgcn_ubfe(vE, 8 * e, 8);
+        uint32_t codes;
+        if constexpr (HD == 128) codes = vc[e];
+        else codes = e & 1 ? vc[e / 2] >> 16 : vc[e / 2] & 0xffffu;
+        direct |= E == 255u || (F16 && E - 104u > 31u && (codes & 0x77777777u) != 0);
+      }
+      if (__any(direct) && lane == 0) s_direct[i & 1] = i + 1;
     }
-    if (__any(direct) && lane == 0) s_direct[i & 1] = i + 1;
     float s[1][4];
     const uint32_t Es[1] = {vE};
     value_scales(Es, s);
@@ -657,6 +690,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
     }(std::make_integer_sequence<int, HD / 32>{});
   };
 
+  const u32x4 ones_bf16 = u32x4{} + 0x3f803f80u;
   auto take = [&](int i, int key0) {
     const int buf = i & 1;
     const bool edge = key0 + 32 > mine_min;
@@ -675,7 +709,10 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
       }
     float x[QT][8];
 #pragma unroll
-    for (int u = 0; u < QT; ++u) weigh(edge, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x[u]);
+    for (int u = 0; u < QT; ++u) {
+      const float before = m[u];
+      if (weigh(edge, z[u], c, key0 + 4 * g, vis[u], m[u], no_sum, o[u], x[u])) l[u] *= __builtin_amdgcn_exp2f(before - m[u]);
+    }
     if (s_direct[buf] == i + 1) {                // rare
       const uint8_t* pages[2];
       uint32_t no = 0;
@@ -698,6 +735,10 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
 #pragma unroll
       for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
       add_values<HD>(c2, E2, w8, o);
+#pragma unroll
+      for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int part = PP - 1; part >= 0; --part) l[u] = mfma_bf16(ones_bf16, w8[u][part], l[u]);
       const uint8_t* const at[2] = {pages[0], pages[1]};
       if (__any(nan)) put_nan<HD>(at, no, key0, n_max, g, vis, o);
       return;
@@ -715,6 +756,8 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
 #pragma unroll
         for (int u = 0; u < QT; ++u) o[u][d] = mfma_f16(v, w8[u], o[u][d]);
       }
+#pragma unroll
+      for (int u = 0; u < QT; ++u) l[u] = mfma_f16(u32x4{} + 0x3c003c00u, w8[u], l[u]);
     } else {
       u32x4 w8[QT][PP];
 #pragma unroll
@@ -727,35 +770,38 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
 #pragma unroll
           for (int part = PP - 1; part >= 0; --part) o[u][d] = mfma_bf16(v, w8[u][part], o[u][d]);
       }
+#pragma unroll
+      for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int part = PP - 1; part >= 0; --part) l[u] = mfma_bf16(ones_bf16, w8[u][part], l[u]);
     }
   };
 
   if (tid < 2) s_direct[tid] = 0;
-  __syncthreads();
+  lds_barrier();
   if (steps > 0) {
     load(0);
     convert(0);
     if (steps > 1) load(1);
   }
-  __syncthreads();
+  lds_barrier();
   for (int i = 0; i < steps; ++i) {
     if (i + 1 < steps) convert(i + 1);
     if (i + 2 < steps) load(i + 2);
     const int key0 = k0 + 32 * i;
     if (key0 < mine_max) take(i, key0);
-    __syncthreads();
+    lds_barrier();
   }
 
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    const float sum = quad_sum(l[t]);
     const int vec = first + 16 * t + r;
     if (16 * t + r >= on) continue;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int d = 0; d < DT; d += 4)
-        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], sum,
+        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], l[t][0],
                     f32x4{o[t][d][e], o[t][d + 1][e], o[t][d + 2][e], o[t][d + 3][e]});
   }
 }
