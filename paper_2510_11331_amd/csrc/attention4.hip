@@ -202,9 +202,9 @@ __device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&
   }
 }
 
-// Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> their weights x, with the running maximum m, the weights'
-// sum l and the outputs o that they go with.  edge: the vector sees the keys below vis only.
-// Whether the maximum has moved.
+// Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> the logarithms x of their weights, with the running maximum
+// m, the weights' sum l and the outputs o that they go with.  edge: the vector sees the keys below vis only.  Whether the
+// maximum has moved.
 template <int DT>
 __device__ __forceinline__ bool weigh(bool edge, const f32x4 (&z)[2], float c, int key, int vis, float& m, float& l, f32x4 (&o)[DT],
                                       float (&x)[8]) {
@@ -235,9 +235,11 @@ __device__ __forceinline__ bool weigh(bool edge, const f32x4 (&z)[2], float c, i
     over();
     moved = true;
   }
+  return moved;
+}
+__device__ __forceinline__ void exp8(float (&x)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
-  return moved;
 }
 __device__ __forceinline__ float sum8(const float (&x)[8]) {
   return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
@@ -342,16 +344,131 @@ __device__ __forceinline__ void emit_nothing(const Attn4Params& p, int split, in
   *(float2*)(p.part_ml + 2 * (((size_t)split * p.M + row) * p.H + h)) = sees_any ? make_float2(-FLT_MAX, 0.f) : make_float2(0.f, -1.f);
 }
 
+// A wave's keys first .. first + 31, from there on each `stride` further, up to `end`: the scores of its vectors q (of
+// which all see n_min keys, vector r of tile t vis[t], and none more than n_max), their weights, and the values times these.
+// FULL: steps that all vectors see whole are taken by code without masks.
+template <typename T, int HD, int QT, bool FULL>
+__device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, int first, int stride, int end, int n_min, int n_max,
+                                          const u32x4 (&q)[QT][HD / 32][QUERY_PARTS<T>], float c, const int (&vis)[QT],
+                                          float (&m)[QT], float (&l)[QT], f32x4 (&o)[QT][HD / 16]) {
+  using P = Page4<HD>;
+  using L4 = typename Load4<HD>::type;
+  constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const uint8_t* const head = p.pool + (size_t)kvh * P::BYTES;
+  const size_t page_bytes = (size_t)p.KV * P::BYTES;
+  const int32_t* const table = p.rows.table + (size_t)b * p.rows.W;
+  const uint32_t off_k = P::key(r, g * (HD / 4)), off_v = P::value(4 * g, r);
+  const uint32_t off_ks = P::key_scale(r, g * (HD / 4) / 32), off_vs = P::value_scale(4 * g, r * DT / 32);
+
+  // lane l of ids holds page l % 2 of step 32 j + l / 2, and of ids_next that of 32 steps later
+  const int steps = end > first ? (end - first + stride - 1) / stride : 0;
+  auto page_id = [&](int i0, bool& no) {
+    const int i = i0 + lane / 2, pg = (first + stride * i) / 16 + (lane & 1);
+    int id = 0;
+    no = false;
+    if (i < steps && 16 * pg < end) {
+      id = pg < p.rows.W ? table[pg] : -1;
+      no = (unsigned)id >= (unsigned)p.n_blocks;
+    }
+    return no ? 0 : id;
+  };
+  bool no_next;
+  int ids = page_id(0, no_next);
+  uint64_t no_ids = __ballot(no_next);
+  int ids_next = page_id(32, no_next);
+
+  // keys are loaded a step ahead when those of the step have been used, values likewise
+  L4 kc[2], vc[2];
+  uint32_t kE[2], vE[2];
+  const uint8_t *pg0, *pg1;                      // the pages being loaded, and which of them are none
+  uint32_t no = 0;
+  auto pages = [&](int i) {
+    pg0 = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i) * page_bytes;
+    pg1 = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i + 1) * page_bytes;
+    no = (uint32_t)(no_ids >> (2 * i)) & 3u;
+  };
+  auto load_k = [&]() {
+    const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
+    kc[0] = page_load<L4>(b0, off_k);
+    kE[0] = page_load<uint8_t>(b0, off_ks);
+    kc[1] = page_load<L4>(b1, off_k);
+    kE[1] = page_load<uint8_t>(b1, off_ks);
+  };
+  auto load_v = [&]() {
+    const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
+    vc[0] = page_load<L4>(b0, off_v);
+    vE[0] = page_load<uint32_t>(b0, off_vs);
+    vc[1] = page_load<L4>(b1, off_v);
+    vE[1] = page_load<uint32_t>(b1, off_vs);
+  };
+
+  int key0 = first, left = steps, at = 0;       // at: of the step after this one, within ids
+  // EDGE: some key of the step is not seen by all vectors, or a page is none
+  auto step = [&]<bool EDGE>() {
+    const uint8_t* const here[2] = {pg0, pg1};
+    const uint32_t no_here = no;
+    f32x4 z[QT][2];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const float ks = scale4(EDGE && (no_here >> t & 1) ? 255u : kE[t]);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const u32x4 k = cvt4_all(kc[t][s], ks);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(k, q[u][s][part], z[u][t]);
+      }
+    }
+
+    // the next step's keys (behind the last step its own again, which nothing uses)
+    if (left > 1) {
+      if (++at == 32) {
+        at = 0;
+        ids = ids_next;
+        no_ids = __ballot(no_next);
+        ids_next = page_id(steps - left + 1 + 32, no_next);
+      }
+      pages(at);
+    }
+    load_k();
+
+    u32x4 w8[QT][PP];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      float x[8];
+      weigh(EDGE, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x);
+      exp8(x);
+      l[u] += sum8(x);
+      parts8<PP>(x, w8[u]);
+    }
+
+    const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here);
+    add_values<HD>(vc, vE, w8, o);
+    load_v();
+    if (EDGE && __any(nan)) put_nan<HD>(here, no_here, key0, n_max, g, vis, o);
+  };
+
+  if (left > 0) {
+    pages(0);
+    load_k();
+    load_v();
+  }
+  if constexpr (FULL)
+    for (; left > 0 && key0 + 32 <= n_min && !no; --left, key0 += stride) step.template operator()<false>();
+  for (; left > 0; --left, key0 += stride) step.template operator()<true>();
+}
+
+
 // waves that a SIMD is to hold at once, for which the compiler keeps to so many registers
 template <typename T, int QT> constexpr int MIN_WAVES = QT == 1 ? (sizeof(T) == 2 ? 4 : 3) : QT == 2 ? 2 : 1;
 
 template <typename T, int HD, int QT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_stream_kernel(Attn4Params p) {
-  using P = Page4<HD>;
-  using L4 = typename Load4<HD>::type;
-  constexpr int KS = HD / 32;                    // k-steps of a score
-  constexpr int DT = HD / 16;                    // output tiles, dimensions of a lane's values
-  constexpr int QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
+  constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>;
   constexpr int PH = WAVES / 4, IP = 4 / PH;     // the outputs are joined in PH parts, which LDS has room for
   __shared__ __attribute__((aligned(16))) float s_o[WAVES][16][HD / PH + 4];
   __shared__ float s_m[WAVES][16], s_l[WAVES][16];
@@ -396,110 +513,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
     for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const uint8_t* const head = p.pool + (size_t)kvh * P::BYTES;
-  const size_t page_bytes = (size_t)p.KV * P::BYTES;
-  const int32_t* const table = p.rows.table + (size_t)w.b * p.rows.W;
-  const uint32_t off_k = P::key(r, g * (HD / 4)), off_v = P::value(4 * g, r);
-  const uint32_t off_ks = P::key_scale(r, g * (HD / 4) / 32), off_vs = P::value_scale(4 * g, r * DT / 32);
-
-  // the wave's steps are 32 (wave + WAVES i) keys into the range; lane l of ids holds page l % 2 of step 32 j + l / 2, and
-  // of ids_next that of 32 steps later
-  const int steps = k1 > k0 ? ((k1 - k0 + 31) / 32 - wave + WAVES - 1) / WAVES : 0;
-  auto page_id = [&](int i0, bool& no) {
-    const int i = i0 + lane / 2, pg = (k0 + 32 * (wave + WAVES * i)) / 16 + (lane & 1);
-    int id = 0;
-    no = false;
-    if (i < steps && 16 * pg < k1) {
-      id = pg < p.rows.W ? table[pg] : -1;
-      no = (unsigned)id >= (unsigned)p.n_blocks;
-    }
-    return no ? 0 : id;
-  };
-  bool no_next;
-  int ids = page_id(0, no_next);
-  uint64_t no_ids = __ballot(no_next);
-  int ids_next = page_id(32, no_next);
-
-  // keys are loaded a step ahead when those of the step have been used, values likewise
-  L4 kc[2], vc[2];
-  uint32_t kE[2], vE[2];
-  const uint8_t *pg0, *pg1;                      // the pages being loaded, and which of them are none
-  uint32_t no = 0;
-  auto pages = [&](int i) {
-    pg0 = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i) * page_bytes;
-    pg1 = head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, 2 * i + 1) * page_bytes;
-    no = (uint32_t)(no_ids >> (2 * i)) & 3u;
-  };
-  auto load_k = [&]() {
-    const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
-    kc[0] = page_load<L4>(b0, off_k);
-    kE[0] = page_load<uint8_t>(b0, off_ks);
-    kc[1] = page_load<L4>(b1, off_k);
-    kE[1] = page_load<uint8_t>(b1, off_ks);
-  };
-  auto load_v = [&]() {
-    const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
-    vc[0] = page_load<L4>(b0, off_v);
-    vE[0] = page_load<uint32_t>(b0, off_vs);
-    vc[1] = page_load<L4>(b1, off_v);
-    vE[1] = page_load<uint32_t>(b1, off_vs);
-  };
-
-  int key0 = k0 + 32 * wave, left = steps, at = 0;       // at: of the step after this one, within ids
-  // EDGE: some key of the step is not seen by all vectors, or a page is none
-  auto step = [&]<bool EDGE>() {
-    const uint8_t* const here[2] = {pg0, pg1};
-    const uint32_t no_here = no;
-    f32x4 z[QT][2];
-#pragma unroll
-    for (int t = 0; t < QT; ++t) z[t][0] = z[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float ks = scale4(EDGE && (no_here >> t & 1) ? 255u : kE[t]);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const u32x4 k = cvt4_all(kc[t][s], ks);
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(k, q[u][s][part], z[u][t]);
-      }
-    }
-
-    // the next step's keys (behind the last step its own again, which nothing uses)
-    if (left > 1) {
-      if (++at == 32) {
-        at = 0;
-        ids = ids_next;
-        no_ids = __ballot(no_next);
-        ids_next = page_id(steps - left + 1 + 32, no_next);
-      }
-      pages(at);
-    }
-    load_k();
-
-    u32x4 w8[QT][PP];
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      float x[8];
-      weigh(EDGE, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x);
-      l[u] += sum8(x);
-      parts8<PP>(x, w8[u]);
-    }
-
-    const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here);
-    add_values<HD>(vc, vE, w8, o);
-    load_v();
-    if (EDGE && __any(nan)) put_nan<HD>(here, no_here, key0, n_max, g, vis, o);
-  };
-
-  if (left > 0) {
-    pages(0);
-    load_k();
-    load_v();
-  }
-  for (; left > 0 && key0 + 32 <= n_min && !no; --left, key0 += 32 * WAVES) step.template operator()<false>();
-  for (; left > 0; --left, key0 += 32 * WAVES) step.template operator()<true>();
+  take_keys<T, HD, QT, true>(p, kvh, w.b, k0 + 32 * wave, 32 * WAVES, k1, n_min, n_max, q, c, vis, m, l, o);
 
   // the waves' outputs are joined in their order, a tile of vectors and a part of the dimensions at a time
 #pragma unroll
@@ -548,7 +562,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 //
 // bf16 outputs: the values are held as fp16, which their codes times scales of 2^-23 to 2^8 are exactly, so that a weight
 // is one fp16 part (off by 2^-12 of itself, an eighth of the output's own rounding) and half the products of the second
-// matrix are saved.  A step with a value outside that range (or with NaN) is taken from the cache in bf16, as above.  fp32 outputs: values in
+// matrix are saved.  A workgroup that meets a value outside that range (or NaN) takes the rest of its keys as above.  fp32 outputs: values in
 // bf16 and three parts.
 template <typename T, int HD, int QT>
 __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) {
@@ -557,19 +571,22 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
   constexpr bool F16 = sizeof(T) == 2;
   __shared__ u32x4 s_k[2][2][KS][64];            // [buffer][page][k-step][lane]
-  __shared__ u32x4 s_v[2][DT][64];               // [buffer][tile][lane]: four keys of either page
-  __shared__ int s_direct[2];                    // step + 1 whose values are not in LDS
+  __shared__ u32x4 s_v[3][DT][64];               // [buffer][tile][lane]: four keys of either page
+  __shared__ int s_leave[3];                     // step + 1 that is not for the loop over LDS
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int G = p.H / p.KV;
   const int kvh = blockIdx.x % p.KV, split = blockIdx.x / p.KV % p.splits;
-  const int block = p.blocks - 1 - (int)(blockIdx.x / p.KV / p.splits);      // the rows that see most go first
+  // the rows that see most go first; where all workgroups run at once, two to a CU, a long one meets a short one there
+  const int order = blockIdx.x / p.KV / p.splits, part = (p.blocks + 1) / 2;
+  const int block = order >= part && (int64_t)p.blocks * p.KV * p.splits <= 512 ? order - part : p.blocks - 1 - order;
   Block4 w;
   if (!find_block(p.rows, p.M, G, 64 * QT, block, w)) return;
   const int len = w.len;
   const int nv = min(64 * QT, w.n * G - w.v0);
   const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
+  const int n_min = sees(p, len, w.n, w.v0, G);
   const int kps = range_keys(n_max, p.splits, 32);
   const int k0 = split * kps, k1 = min(k0 + kps, n_max);
   if (split > 0 && k0 >= k1) {
@@ -621,187 +638,183 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   };
   int ids = 0;
   uint64_t no_ids = 0;
-  uint32_t kc[KS / 2], kE, vE;
-  L4 vc;
-  bool none;
-  auto load = [&](int i) {                       // of step i, in order
+  // what is loaded of a step, four steps ahead of its use
+  struct Raw {
+    u32x2 kc;                                    // codes of keys (HD 64: one of them)
+    uint32_t kE, vE;                             // scales
+    L4 vc;                                       // codes of values
+    bool none;                                   // no page
+  } raw[2];
+  auto load = [&](Raw& a, int i) {               // step i, in order (behind the last: any page)
     if (i % 64 == 0) {
       bool no;
       ids = page_id(i, no);
       no_ids = __ballot(no);
     }
     const auto pg = page_buffer<HD>(head + (size_t)(uint32_t)__builtin_amdgcn_readlane(ids, i % 64) * page_bytes);
-    none = no_ids >> (i % 64) & 1;
-    if constexpr (KS == 4) {
-      const u32x2 k = page_load<u32x2>(pg, off_k);
-      kc[0] = k[0];
-      kc[1] = k[1];
-    } else {
-      kc[0] = page_load<uint32_t>(pg, off_k);
-    }
-    kE = page_load<uint8_t>(pg, off_ks);
-    vc = page_load<L4>(pg, off_v);
-    vE = page_load<uint32_t>(pg, off_vs);
+    a.none = no_ids >> (i % 64) & 1;
+    if constexpr (KS == 4) a.kc = page_load<u32x2>(pg, off_k);
+    else a.kc[0] = page_load<uint32_t>(pg, off_k);
+    a.kE = page_load<uint8_t>(pg, off_ks);
+    a.vc = page_load<L4>(pg, off_v);
+    a.vE = page_load<uint32_t>(pg, off_vs);
   };
-  auto convert = [&](int i) {                    // what load left, into the buffer of step i
-    const float ks = scale4(none ? 255u : kE);
+  auto put_keys = [&](const Raw& a, int kb) {
 #pragma unroll
-    for (int s = 0; s < KS / 2; ++s) s_k[i & 1][mypage][half * (KS / 2) + s][lane] = cvt4_all(kc[s], ks);
-    const int key = k0 + 32 * i + 16 * mypage + 4 * g;
-    if (none) {                                  // (its keys are NaN)
-      vc = L4{};
-      vE = 0x7f7f7f7fu;
-    }
-    if (k0 + 32 * i + 32 > n_max) {              // no value behind the last key
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (key + e >= n_max) {
-          if constexpr (HD == 128) vc[e] = 0;
-          else vc[e / 2] &= e & 1 ? 0xffffu : 0xffff0000u;
-          vE = (vE & ~(255u << (8 * e))) | 127u << (8 * e);
-        }
-    }
-    // the four scales at once: E + 24 of 128 to 159 (a carry from a byte is of one that is outside)
-    if (__any(((vE + 0x18181818u) & 0xe0e0e0e0u) != 0x80808080u)) {
-      bool direct = false;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t E = __builtin_amdgcn_ubfe(vE, 8 * e, 8);
-        uint32_t codes;
-        if constexpr (HD == 128) codes = vc[e];
-        else codes = e & 1 ? vc[e / 2] >> 16 : vc[e / 2] & 0xffffu;
-        direct |= E == 255u || (F16 && E - 104u > 31u && (codes & 0x77777777u) != 0);
-      }
-      if (__any(direct) && lane == 0) s_direct[i & 1] = i + 1;
-    }
+    for (int s = 0; s < KS / 2; ++s) s_k[kb][mypage][half * (KS / 2) + s][lane] = cvt4_all(a.kc[s], scale4(a.kE));
+  };
+  auto put_values = [&](const Raw& a, int vb) {
     float s[1][4];
-    const uint32_t Es[1] = {vE};
+    const uint32_t Es[1] = {a.vE};
     value_scales(Es, s);
-    const L4 cs[1] = {vc};
+    // the half's bytes of every key, by a shift that does not depend on it
+    L4 mine = a.vc;
+#pragma unroll
+    for (int e = 0; e < HD / 32; ++e) mine[e] = a.vc[e] >> (8 * (HD / 64) * half);
+    const L4 cs[1] = {mine};
     [&]<int... B>(std::integer_sequence<int, B...>) {
       (([&] {
-         if (B / (DT / 4) != half) return;
          uint32_t even[2], odd[2];
          value_tiles<HD, B, 1, F16>(cs, s, even, odd);
-         ((u32x2*)&s_v[i & 1][2 * B][lane])[mypage] = u32x2{even[0], even[1]};
-         ((u32x2*)&s_v[i & 1][2 * B + 1][lane])[mypage] = u32x2{odd[0], odd[1]};
+         u32x2* const to = (u32x2*)&s_v[vb][half * (DT / 2) + 2 * B][lane] + mypage;
+         to[0] = u32x2{even[0], even[1]};
+         to[2 * 64] = u32x2{odd[0], odd[1]};
        }()),
        ...);
-    }(std::make_integer_sequence<int, HD / 32>{});
+    }(std::make_integer_sequence<int, HD / 64>{});
+  };
+  // what load left of step i, into its buffers
+  auto convert = [&](const Raw& a, int i, int kb, int vb) {
+    put_keys(a, kb);
+    put_values(a, vb);
+    // fp16: the four scales at once, E + 24 of 128 to 159 (a carry from a byte is of one that is outside); else only NaN
+    const bool outside = F16 ? ((a.vE + 0x18181818u) & 0xe0e0e0e0u) != 0x80808080u
+                             : (a.vE & 255u) == 255u || (a.vE >> 8 & 255u) == 255u || (a.vE >> 16 & 255u) == 255u || a.vE >> 24 == 255u;
+    if (a.none || __any(outside)) {
+      bool leave = a.none;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t E = a.vE >> (8 * e) & 255u;
+        uint32_t codes;
+        if constexpr (HD == 128) codes = a.vc[e];
+        else codes = e & 1 ? a.vc[e / 2] >> 16 : a.vc[e / 2] & 0xffffu;
+        leave |= E == 255u || (F16 && E - 104u > 31u && (codes & 0x77777777u) != 0);      // (zeros have E = 1)
+      }
+      if (__any(leave) && lane == 0) s_leave[vb] = i + 1;
+    }
   };
 
-  const u32x4 ones_bf16 = u32x4{} + 0x3f803f80u;
-  auto take = [&](int i, int key0) {
-    const int buf = i & 1;
-    const bool edge = key0 + 32 > mine_min;
-    f32x4 z[QT][2];
+  f32x4 z[QT][2];
+  u32x4 kf[KS][2];
+  auto read_keys = [&](int kb) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) kf[s][t] = s_k[kb][t][s][lane];
+  };
+  auto scores = [&]() {
 #pragma unroll
     for (int u = 0; u < QT; ++u) z[u][0] = z[u][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const u32x4 k = s_k[buf][t][s][lane];
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int u = 0; u < QT; ++u)
 #pragma unroll
-          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(k, q[u][s][part], z[u][t]);
-      }
-    float x[QT][8];
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      const float before = m[u];
-      if (weigh(edge, z[u], c, key0 + 4 * g, vis[u], m[u], no_sum, o[u], x[u])) l[u] *= __builtin_amdgcn_exp2f(before - m[u]);
-    }
-    if (s_direct[buf] == i + 1) {                // rare
-      const uint8_t* pages[2];
-      uint32_t no = 0;
-      L4 c2[2];
-      uint32_t E2[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int pg = key0 / 16 + t;
-        int id = 16 * pg >= k1 ? 0 : pg < p.rows.W ? __builtin_amdgcn_readfirstlane(table[pg]) : -1;
-        if ((unsigned)id >= (unsigned)p.n_blocks) {
-          id = 0;
-          no |= 1u << t;
-        }
-        pages[t] = head + (size_t)(uint32_t)id * page_bytes;
-        c2[t] = *(const L4*)(pages[t] + off_v);
-        E2[t] = *(const uint32_t*)(pages[t] + off_vs);
-      }
-      const bool nan = clean_scales(E2, key0 + 4 * g, n_max, no);
-      u32x4 w8[QT][PP];
-#pragma unroll
-      for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
-      add_values<HD>(c2, E2, w8, o);
-#pragma unroll
-      for (int u = 0; u < QT; ++u)
-#pragma unroll
-        for (int part = PP - 1; part >= 0; --part) l[u] = mfma_bf16(ones_bf16, w8[u][part], l[u]);
-      const uint8_t* const at[2] = {pages[0], pages[1]};
-      if (__any(nan)) put_nan<HD>(at, no, key0, n_max, g, vis, o);
-      return;
-    }
-    if constexpr (F16) {
-      u32x4 w8[QT];
-#pragma unroll
-      for (int u = 0; u < QT; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          w8[u][e] = __builtin_bit_cast(uint32_t, f16x2{(f16_t)x[u][2 * e], (f16_t)x[u][2 * e + 1]});
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const u32x4 v = s_v[buf][d][lane];
-#pragma unroll
-        for (int u = 0; u < QT; ++u) o[u][d] = mfma_f16(v, w8[u], o[u][d]);
-      }
-#pragma unroll
-      for (int u = 0; u < QT; ++u) l[u] = mfma_f16(u32x4{} + 0x3c003c00u, w8[u], l[u]);
-    } else {
-      u32x4 w8[QT][PP];
-#pragma unroll
-      for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const u32x4 v = s_v[buf][d][lane];
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int part = PP - 1; part >= 0; --part) o[u][d] = mfma_bf16(v, w8[u][part], o[u][d]);
-      }
-#pragma unroll
-      for (int u = 0; u < QT; ++u)
-#pragma unroll
-        for (int part = PP - 1; part >= 0; --part) l[u] = mfma_bf16(ones_bf16, w8[u][part], l[u]);
-    }
+          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(kf[s][t], q[u][s][part], z[u][t]);
   };
-
-  if (tid < 2) s_direct[tid] = 0;
-  lds_barrier();
-  if (steps > 0) {
-    load(0);
-    convert(0);
-    if (steps > 1) load(1);
-  }
-  lds_barrier();
-  for (int i = 0; i < steps; ++i) {
-    if (i + 1 < steps) convert(i + 1);
-    if (i + 2 < steps) load(i + 2);
-    const int key0 = k0 + 32 * i;
-    if (key0 < mine_max) take(i, key0);
+  // Steps that all vectors see whole, while the workgroup meets no value outside fp16, no NaN and no page that is none.
+  // Step i: its weights; the scores of step i + 1; its values; the conversion of step i + 2; the loads of step i + 4
+  const int full = max(0, min(k1, n_min) - k0) / 32;
+  int i = 0;
+  if (full > 0) {
+    if (tid < 3) s_leave[tid] = 0;
     lds_barrier();
+    load(raw[0], 0);
+    load(raw[1], 1);
+    convert(raw[0], 0, 0, 0);
+    load(raw[0], 2);
+    convert(raw[1], 1, 1, 1);
+    load(raw[1], 3);
+    lds_barrier();
+    read_keys(0);
+    scores();
+    int vb = 0, leave = s_leave[0];
+    lds_barrier();
+    auto next = [&]<int S>() {                   // step i, S = i % 2
+      if (i >= full || __builtin_amdgcn_readfirstlane(leave) == i + 1) return false;
+      const int after = vb == 2 ? 0 : vb + 1;
+      read_keys(1 - S);
+      leave = s_leave[after];
+      float x[QT][8];
+#pragma unroll
+      for (int u = 0; u < QT; ++u) {
+        const float before = m[u];
+        if (weigh(false, z[u], c, 0, 0, m[u], no_sum, o[u], x[u])) l[u] *= __builtin_amdgcn_exp2f(before - m[u]);
+      }
+      u32x4 vf[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[d] = s_v[vb][d][lane];
+      scores();
+#pragma unroll
+      for (int u = 0; u < QT; ++u) exp8(x[u]);
+      if constexpr (F16) {
+        u32x4 w8[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            w8[u][e] = __builtin_bit_cast(uint32_t, f16x2{(f16_t)x[u][2 * e], (f16_t)x[u][2 * e + 1]});
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+#pragma unroll
+          for (int u = 0; u < QT; ++u) o[u][d] = mfma_f16(vf[d], w8[u], o[u][d]);
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u) l[u] = mfma_f16(u32x4{} + 0x3c003c00u, w8[u], l[u]);
+      } else {
+        u32x4 w8[QT][PP];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int part = PP - 1; part >= 0; --part) o[u][d] = mfma_bf16(vf[d], w8[u][part], o[u][d]);
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int part = PP - 1; part >= 0; --part) l[u] = mfma_bf16(u32x4{} + 0x3f803f80u, w8[u][part], l[u]);
+      }
+      convert(raw[S], i + 2, S, vb == 0 ? 2 : vb - 1);     // (the buffers of steps i and i - 1)
+      load(raw[S], i + 4);
+      lds_barrier();
+      vb = after;
+      ++i;
+      return true;
+    };
+    while (next.template operator()<0>() && next.template operator()<1>()) {}
   }
+
+  // the others (behind the first keys that some vector does not see, 128 at most per head of a row): each wave by itself
+  float sums[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) sums[t] = g == 0 ? l[t][0] : 0.f;
+  take_keys<T, HD, QT, false>(p, kvh, w.b, k0 + 32 * i, 32, mine_max, mine_min, mine_max, q, c, vis, m, sums, o);
 
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
+    const float sum = quad_sum(sums[t]);
     const int vec = first + 16 * t + r;
     if (16 * t + r >= on) continue;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int d = 0; d < DT; d += 4)
-        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], l[t][0],
+        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], sum,
                     f32x4{o[t][d][e], o[t][d + 1][e], o[t][d + 2][e], o[t][d + 3][e]});
   }
 }
