@@ -202,40 +202,42 @@ __device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&
   }
 }
 
-// Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> the logarithms x of their weights, with the running maximum
-// m, the weights' sum l and the outputs o that they go with.  edge: the vector sees the keys below vis only.  Whether the
-// maximum has moved.
-template <int DT>
-__device__ __forceinline__ bool weigh(bool edge, const f32x4 (&z)[2], float c, int key, int vis, float& m, float& l, f32x4 (&o)[DT],
-                                      float (&x)[8]) {
-  auto over = [&] {                              // in powers of two over the maximum
+// Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> the logarithms x of their weights, with the running maxima
+// m, and what goes with these: the weights' sums l and the outputs o.  edge: vector t sees the keys below vis[t] only.
+template <int QT, int DT, typename L>
+__device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float c, int key, const int (&vis)[QT], float (&m)[QT],
+                                      L (&l)[QT], f32x4 (&o)[QT][DT], float (&x)[QT][8]) {
+  auto over = [&](int t) {                       // in powers of two over the maximum
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(z[e / 4][e % 4], c, -m);
+    for (int e = 0; e < 8; ++e) x[t][e] = fmaf(z[t][e / 4][e % 4], c, -m[t]);
     if (edge) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (key + 16 * (e / 4) + e % 4 >= vis) x[e] = -INFINITY;
+        if (key + 16 * (e / 4) + e % 4 >= vis[t]) x[t][e] = -INFINITY;
     }
   };
-  over();
-  bool moved = false;
   // (as integers: negative numbers below all others, NaN above)
   int top = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_int(x[e]));
-  if (__any(top > 0x41000000)) {                 // 8.0
-    float most = -FLT_MAX;
+  for (int t = 0; t < QT; ++t) {
+    over(t);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = fmaxf(most, x[e] == -INFINITY ? -FLT_MAX : z[e / 4][e % 4] * c);
-    const float to = fmaxf(m, quad_max(most)), old = __builtin_amdgcn_exp2f(m - to);
-    m = to;
-    l *= old;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] *= old;
-    over();
-    moved = true;
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_int(x[t][e]));
   }
-  return moved;
+  if (__any(top > 0x41000000)) {                 // 8.0
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float most = -FLT_MAX;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, x[t][e] == -INFINITY ? -FLT_MAX : z[t][e / 4][e % 4] * c);
+      const float to = fmaxf(m[t], quad_max(most)), old = __builtin_amdgcn_exp2f(m[t] - to);
+      m[t] = to;
+      l[t] *= old;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] *= old;
+      over(t);
+    }
+  }
 }
 __device__ __forceinline__ void exp8(float (&x)[8]) {
 #pragma unroll
@@ -437,13 +439,13 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
     load_k();
 
     u32x4 w8[QT][PP];
+    float x[QT][8];
+    weigh(EDGE, z, c, key0 + 4 * g, vis, m, l, o, x);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-      float x[8];
-      weigh(EDGE, z[u], c, key0 + 4 * g, vis[u], m[u], l[u], o[u], x);
-      exp8(x);
-      l[u] += sum8(x);
-      parts8<PP>(x, w8[u]);
+      exp8(x[u]);
+      l[u] += sum8(x[u]);
+      parts8<PP>(x[u], w8[u]);
     }
 
     const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here);
@@ -601,7 +603,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   const int mine_max = on > 0 ? min(k1, sees(p, len, w.n, first + on - 1, G)) : 0;
   u32x4 q[QT][KS][QP];
   int vis[QT];
-  float m[QT], no_sum = 0.f;
+  float m[QT];
   f32x4 o[QT][DT], l[QT];                        // l: the weights' sum, four times, as the product with a tile of ones
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -748,11 +750,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
       read_keys(1 - S);
       leave = s_leave[after];
       float x[QT][8];
-#pragma unroll
-      for (int u = 0; u < QT; ++u) {
-        const float before = m[u];
-        if (weigh(false, z[u], c, 0, 0, m[u], no_sum, o[u], x[u])) l[u] *= __builtin_amdgcn_exp2f(before - m[u]);
-      }
+      weigh(false, z, c, 0, vis, m, l, o, x);
       u32x4 vf[DT];
 #pragma unroll
       for (int d = 0; d < DT; ++d) vf[d] = s_v[vb][d][lane];
