@@ -167,9 +167,10 @@ template <> struct Load4<64> { typedef u32x2 type; };
 template <int HD> __device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const uint8_t* pg) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(pg), (short)0, Page4<HD>::BYTES, 0x00020000);
 }
-template <typename V> __device__ __forceinline__ V page_load(__amdgpu_buffer_rsrc_t b, uint32_t off) {
-  if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0));
-  else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(b, off, 0, 0));
+template <typename V, bool NT = false> __device__ __forceinline__ V page_load(__amdgpu_buffer_rsrc_t b, uint32_t off) {
+  constexpr int AUX = NT ? 2 : 0;                // 2: non-temporal
+  if constexpr (sizeof(V) == 16) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, AUX));
+  else if constexpr (sizeof(V) == 8) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(b, off, 0, AUX));
   else if constexpr (sizeof(V) == 4) return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
   else return __builtin_amdgcn_raw_buffer_load_b8(b, off, 0, 0);
 }
@@ -348,11 +349,11 @@ __device__ __forceinline__ void emit_nothing(const Attn4Params& p, int split, in
 
 // A wave's keys first .. first + 31, from there on each `stride` further, up to `end`: the scores of its vectors q (of
 // which all see n_min keys, vector r of tile t vis[t], and none more than n_max), their weights, and the values times these.
-// FULL: steps that all vectors see whole are taken by code without masks.
-template <typename T, int HD, int QT, bool FULL>
+// FULL: steps that all vectors see whole are taken by code without masks.  guessed: guess_id is the lane's first page id.
+template <typename T, int HD, int QT, bool FULL, bool NT>
 __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, int first, int stride, int end, int n_min, int n_max,
                                           const u32x4 (&q)[QT][HD / 32][QUERY_PARTS<T>], float c, const int (&vis)[QT],
-                                          float (&m)[QT], float (&l)[QT], f32x4 (&o)[QT][HD / 16]) {
+                                          float (&m)[QT], float (&l)[QT], f32x4 (&o)[QT][HD / 16], bool guessed, int guess_id) {
   using P = Page4<HD>;
   using L4 = typename Load4<HD>::type;
   constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
@@ -365,20 +366,20 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
 
   // lane l of ids holds page l % 2 of step 32 j + l / 2, and of ids_next that of 32 steps later
   const int steps = end > first ? (end - first + stride - 1) / stride : 0;
-  auto page_id = [&](int i0, bool& no) {
+  auto page_id = [&](int i0, bool& no, bool known) {
     const int i = i0 + lane / 2, pg = (first + stride * i) / 16 + (lane & 1);
     int id = 0;
     no = false;
     if (i < steps && 16 * pg < end) {
-      id = pg < p.rows.W ? table[pg] : -1;
+      id = known ? guess_id : pg < p.rows.W ? table[pg] : -1;
       no = (unsigned)id >= (unsigned)p.n_blocks;
     }
     return no ? 0 : id;
   };
   bool no_next;
-  int ids = page_id(0, no_next);
+  int ids = page_id(0, no_next, guessed);
   uint64_t no_ids = __ballot(no_next);
-  int ids_next = page_id(32, no_next);
+  int ids_next = page_id(32, no_next, false);
 
   // keys are loaded a step ahead when those of the step have been used, values likewise
   L4 kc[2], vc[2];
@@ -392,16 +393,16 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
   };
   auto load_k = [&]() {
     const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
-    kc[0] = page_load<L4>(b0, off_k);
+    kc[0] = page_load<L4, NT>(b0, off_k);
     kE[0] = page_load<uint8_t>(b0, off_ks);
-    kc[1] = page_load<L4>(b1, off_k);
+    kc[1] = page_load<L4, NT>(b1, off_k);
     kE[1] = page_load<uint8_t>(b1, off_ks);
   };
   auto load_v = [&]() {
     const auto b0 = page_buffer<HD>(pg0), b1 = page_buffer<HD>(pg1);
-    vc[0] = page_load<L4>(b0, off_v);
+    vc[0] = page_load<L4, NT>(b0, off_v);
     vE[0] = page_load<uint32_t>(b0, off_vs);
-    vc[1] = page_load<L4>(b1, off_v);
+    vc[1] = page_load<L4, NT>(b1, off_v);
     vE[1] = page_load<uint32_t>(b1, off_vs);
   };
 
@@ -432,7 +433,7 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
         at = 0;
         ids = ids_next;
         no_ids = __ballot(no_next);
-        ids_next = page_id(steps - left + 1 + 32, no_next);
+        ids_next = page_id(steps - left + 1 + 32, no_next, false);
       }
       pages(at);
     }
@@ -468,17 +469,20 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
 // waves that a SIMD is to hold at once, for which the compiler keeps to so many registers
 template <typename T, int QT> constexpr int MIN_WAVES = QT == 1 ? (sizeof(T) == 2 ? 4 : 3) : QT == 2 ? 2 : 1;
 
-template <typename T, int HD, int QT, int WAVES>
+template <typename T, int HD, int QT, int WAVES, bool NT>
 __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_stream_kernel(Attn4Params p) {
   constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>;
-  constexpr int PH = WAVES / 4, IP = 4 / PH;     // the outputs are joined in PH parts, which LDS has room for
-  __shared__ __attribute__((aligned(16))) float s_o[WAVES][16][HD / PH + 4];
+  constexpr int ROWS = 64 / WAVES;               // vectors that are joined at a time
+  __shared__ __attribute__((aligned(16))) float s_o[WAVES][ROWS][HD + 4];
   __shared__ float s_m[WAVES][16], s_l[WAVES][16];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int G = p.H / p.KV;
   const int kvh = blockIdx.x % p.KV, split = blockIdx.x / p.KV % p.splits, block = blockIdx.x / p.KV / p.splits;
+  // one block a sequence is the usual case: its first pages' ids are on their way while the sequence is looked up
+  const int guess = min(block, p.rows.B - 1), guess_page = 2 * wave + 2 * WAVES * (lane / 2) + (lane & 1);
+  const int guess_id = p.splits == 1 && guess_page < p.rows.W ? p.rows.table[(size_t)guess * p.rows.W + guess_page] : -1;
   Block4 w;
   if (!find_block(p.rows, p.M, G, 16 * QT, block, w)) return;
   const int len = w.len;
@@ -515,33 +519,31 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
     for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  take_keys<T, HD, QT, true>(p, kvh, w.b, k0 + 32 * wave, 32 * WAVES, k1, n_min, n_max, q, c, vis, m, l, o);
+  take_keys<T, HD, QT, true, NT>(p, kvh, w.b, k0 + 32 * wave, 32 * WAVES, k1, n_min, n_max, q, c, vis, m, l, o,
+                                 p.splits == 1 && w.b == guess, guess_id);
 
-  // the waves' outputs are joined in their order, a tile of vectors and a part of the dimensions at a time
+  // the waves' outputs are joined in their order
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     if (16 * t >= nv) break;
     const float sum = quad_sum(l[t]);
-    if (t) __syncthreads();
-    if (g == 0) {
-      s_m[wave][r] = m[t];
-      s_l[wave][r] = sum;
-    }
+    for (int v0 = 0; v0 < min(16, nv - 16 * t); v0 += ROWS) {
+      if (t || v0) __syncthreads();
+      if (v0 == 0 && g == 0) {
+        s_m[wave][r] = m[t];
+        s_l[wave][r] = sum;
+      }
+      if ((unsigned)(r - v0) < (unsigned)ROWS) {
 #pragma unroll
-    for (int ph = 0; ph < PH; ++ph) {
-      if (ph) __syncthreads();
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < IP; ++i)
-#pragma unroll
-        for (int d = 0; d < DT; d += 4) {
-          const int e = ph * IP + i;
-          *(f32x4*)&s_o[wave][r][(g * IP + i) * DT + d] = f32x4{o[t][d][e], o[t][d + 1][e], o[t][d + 2][e], o[t][d + 3][e]};
-        }
+          for (int d = 0; d < DT; d += 4)
+            *(f32x4*)&s_o[wave][r - v0][(4 * g + i) * DT + d] = f32x4{o[t][d][i], o[t][d + 1][i], o[t][d + 2][i], o[t][d + 3][i]};
+      }
       __syncthreads();
-      for (int idx = tid; idx < 16 * (HD / PH / 4); idx += 64 * WAVES) {
-        const int v = idx / (HD / PH / 4), col = idx % (HD / PH / 4) * 4;
+      for (int idx = tid; idx < ROWS * (HD / 4); idx += 64 * WAVES) {
+        const int v = v0 + idx / (HD / 4), d = idx % (HD / 4) * 4;
         if (16 * t + v >= nv) continue;
-        const int d = (4 * (col / (IP * DT)) + ph * IP) * DT + col % (IP * DT);
         float M = s_m[0][v], L = 0.f;
 #pragma unroll
         for (int k = 1; k < WAVES; ++k) M = fmaxf(M, s_m[k][v]);
@@ -550,10 +552,10 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
         for (int k = 0; k < WAVES; ++k) {
           const float e = __builtin_amdgcn_exp2f(s_m[k][v] - M);
           L += s_l[k][v] * e;
-          O += *(const f32x4*)&s_o[k][v][col] * e;
+          O += *(const f32x4*)&s_o[k][v - v0][d] * e;
         }
-        const int vec = w.v0 + 16 * t + v, row = w.row0 + vec / G, h = kvh * G + vec % G;
-        emit<T, HD>(p, split, row, h, d, sees(p, len, w.n, vec, G) > 0, M, L, O);
+        const int vec = w.v0 + 16 * t + v;
+        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, d, sees(p, len, w.n, vec, G) > 0, M, L, O);
       }
     }
   }
@@ -579,28 +581,20 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int G = p.H / p.KV;
-  const int kvh = blockIdx.x % p.KV, split = blockIdx.x / p.KV % p.splits;
+  const int kvh = blockIdx.x % p.KV, order = blockIdx.x / p.KV, part = (p.blocks + 1) / 2;
   // the rows that see most go first; where all workgroups run at once, two to a CU, a long one meets a short one there
-  const int order = blockIdx.x / p.KV / p.splits, part = (p.blocks + 1) / 2;
-  const int block = order >= part && (int64_t)p.blocks * p.KV * p.splits <= 512 ? order - part : p.blocks - 1 - order;
+  const int block = order >= part && (int64_t)p.blocks * p.KV <= 512 ? order - part : p.blocks - 1 - order;
   Block4 w;
   if (!find_block(p.rows, p.M, G, 64 * QT, block, w)) return;
   const int len = w.len;
   const int nv = min(64 * QT, w.n * G - w.v0);
   const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
   const int n_min = sees(p, len, w.n, w.v0, G);
-  const int kps = range_keys(n_max, p.splits, 32);
-  const int k0 = split * kps, k1 = min(k0 + kps, n_max);
-  if (split > 0 && k0 >= k1) {
-    const int vec = w.v0 + tid;
-    if (tid < nv) emit_nothing(p, split, w.row0 + vec / G, kvh * G + vec % G, sees(p, len, w.n, vec, G) > 0);
-    return;
-  }
 
   // this wave's vectors
   const int first = w.v0 + 16 * QT * wave, on = min(16 * QT, nv - 16 * QT * wave);
   const int mine_min = on > 0 ? sees(p, len, w.n, first, G) : 0;
-  const int mine_max = on > 0 ? min(k1, sees(p, len, w.n, first + on - 1, G)) : 0;
+  const int mine_max = on > 0 ? loop_keys(p, sees(p, len, w.n, first + on - 1, G)) : 0;
   u32x4 q[QT][KS][QP];
   int vis[QT];
   float m[QT];
@@ -625,14 +619,13 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   const uint8_t* const head = p.pool + (size_t)kvh * P::BYTES;
   const size_t page_bytes = (size_t)p.KV * P::BYTES;
   const int32_t* const table = p.rows.table + (size_t)w.b * p.rows.W;
-  const int steps = (k1 - k0 + 31) / 32;
   const uint32_t off_k = P::key(r, g * (HD / 4) + half * (HD / 8)), off_v = P::value(4 * g, r);
   const uint32_t off_ks = P::key_scale(r, g * (HD / 4) / 32), off_vs = P::value_scale(4 * g, r * DT / 32);
   auto page_id = [&](int i0, bool& no) {
-    const int pg = k0 / 16 + 2 * (i0 + lane) + mypage;
+    const int pg = 2 * (i0 + lane) + mypage;
     int id = 0;
     no = false;
-    if (16 * pg < k1) {
+    if (16 * pg < n_max) {
       id = pg < p.rows.W ? table[pg] : -1;
       no = (unsigned)id >= (unsigned)p.n_blocks;
     }
@@ -728,7 +721,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   };
   // Steps that all vectors see whole, while the workgroup meets no value outside fp16, no NaN and no page that is none.
   // Step i: its weights; the scores of step i + 1; its values; the conversion of step i + 2; the loads of step i + 4
-  const int full = max(0, min(k1, n_min) - k0) / 32;
+  const int full = max(0, min(n_max, n_min)) / 32;
   int i = 0;
   if (full > 0) {
     if (tid < 3) s_leave[tid] = 0;
@@ -801,7 +794,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   float sums[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) sums[t] = g == 0 ? l[t][0] : 0.f;
-  take_keys<T, HD, QT, false>(p, kvh, w.b, k0 + 32 * i, 32, mine_max, mine_min, mine_max, q, c, vis, m, sums, o);
+  take_keys<T, HD, QT, false, false>(p, kvh, w.b, 32 * i, 32, mine_max, mine_min, mine_max, q, c, vis, m, sums, o, false, 0);
 
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -812,7 +805,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int d = 0; d < DT; d += 4)
-        emit<T, HD>(p, split, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], sum,
+        emit<T, HD>(p, 0, w.row0 + vec / G, kvh * G + vec % G, (4 * g + e) * DT + d, vis[t] > 0, m[t], sum,
                     f32x4{o[t][d][e], o[t][d + 1][e], o[t][d + 2][e], o[t][d + 3][e]});
   }
 }
@@ -877,20 +870,34 @@ template <typename T, int HD, int PARTS> __global__ __launch_bounds__(256) void 
   store4((T*)p.out + (size_t)row * p.ldo + h * HD + d, O);
 }
 
-Attn4Plan plan_attention4(int dtype, int M, int H, int KV, int n_seqs, int max_len) {
+Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, int max_len) {
   Attn4Plan a{};
   const int64_t G = H / KV, nz = std::min(n_seqs, M);
   const int64_t vectors = (M + nz - 1) / nz * G;             // of an average sequence
-  a.tiles = vectors <= 16 ? 1 : vectors <= 32 || dtype == 1 ? 2 : 4;
-  a.waves = 4;
-  int want_s = 0;
-  if (const char* e = getenv("SD_A4")) sscanf(e, "%d,%d,%d", &a.tiles, &a.waves, &want_s);
-  if (a.waves == 0) a.tiles = dtype == 1 ? 4 : 8;     // tile kernel
-  const int64_t cap = 16 * a.tiles;
-  a.blocks = (int)((M * G - nz) / cap + nz);                 // sum of ceil(n G / cap) over nz sequences of M rows
-  const int64_t items = (int64_t)a.blocks * KV, want = (1024 + items - 1) / items;
-  a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, (max_len + 255) / 256, 64}));
-  if (want_s) a.splits = want_s;
+  auto blocks = [&](int64_t cap) { return (M * G - nz) / cap + nz; };   // sum of ceil(n G / cap) over nz sequences of M rows
+  auto typical = [&](int64_t cap) { return nz * ((vectors + cap - 1) / cap) * KV; };    // ... of alike sequences, and heads
+  const int64_t steps = (max_len + 31) / 32;
+  a.tile_kernel = dtype == 0 && vectors >= 128 && typical(128) >= 256;
+  a.tiles = a.tile_kernel ? 8 : vectors > 16 && dtype == 0 && typical(16) * steps >= 28 * 1024 ? 2 : 1;
+  a.blocks = (int)blocks(16 * a.tiles);
+  const int64_t items = typical(16 * a.tiles);
+  a.waves = a.tile_kernel || a.tiles == 2 || (dtype == 1 && hd == 128 && items >= 512) || (items >= 1024 && steps < 24) ? 4 : 8;
+  a.splits = 1;
+  if (items <= 64 && max_len >= 1536) {
+    a.waves = 4;
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / items, max_len / 256, 64}));
+  } else if (items <= 128 && max_len >= 2560) {
+    a.splits = a.waves == 8 ? 2 : 4;
+  }
+  a.stream = !a.tile_kernel && vectors <= 16 * a.tiles && (double)nz * max_len * KV * 17 * hd / 16 > 268435456.0;
+  if (const char* e = getenv("SD_A4")) {
+    int t, w, sp;
+    if (sscanf(e, "%d,%d,%d", &t, &w, &sp) == 3) {
+      a.tile_kernel = w == 0;
+      a.tiles = t; a.waves = w ? w : 4; a.splits = sp; a.blocks = (int)blocks(16 * t);
+      a.stream = false;
+    }
+  }
   return a;
 }
 
@@ -899,22 +906,24 @@ size_t attention4_part_floats(const Attn4Plan& a, int M, int H, int hd) {
 }
 
 template <typename T, int HD, int QT, int WAVES> static void launch_stream(const Attn4Plan& a, const Attn4Params& p, hipStream_t s) {
-  attention4_stream_kernel<T, HD, QT, WAVES><<<dim3((unsigned)a.blocks * p.KV * a.splits), 64 * WAVES, 0, s>>>(p);
+  const dim3 grid((unsigned)a.blocks * p.KV * a.splits);
+  if (a.stream) attention4_stream_kernel<T, HD, QT, WAVES, true><<<grid, 64 * WAVES, 0, s>>>(p);
+  else attention4_stream_kernel<T, HD, QT, WAVES, false><<<grid, 64 * WAVES, 0, s>>>(p);
 }
 
 template <typename T, int HD> static void launch_hd(const Attn4Plan& a, Attn4Params p, hipStream_t s) {
   p.blocks = a.blocks;
-  if (a.waves == 0) {
-    constexpr int QT = sizeof(T) == 2 ? 2 : 1;
-    attention4_tile_kernel<T, HD, QT><<<dim3((unsigned)a.blocks * p.KV * a.splits), 256, 0, s>>>(p);
-  } else switch (10 * a.tiles + a.waves / 4) {
-    case 11: launch_stream<T, HD, 1, 4>(a, p, s); break;
-    case 12: launch_stream<T, HD, 1, 8>(a, p, s); break;
-    case 21: launch_stream<T, HD, 2, 4>(a, p, s); break;
-    case 22: launch_stream<T, HD, 2, 8>(a, p, s); break;
-    case 41:
-      if constexpr (sizeof(T) == 2) launch_stream<T, HD, 4, 4>(a, p, s);
-      break;
+  p.splits = a.splits;
+  if constexpr (sizeof(T) == 2) {
+    if (a.tile_kernel) {
+      attention4_tile_kernel<T, HD, 2><<<dim3((unsigned)a.blocks * p.KV), 256, 0, s>>>(p);
+      return;
+    }
+    if (a.tiles == 2) launch_stream<T, HD, 2, 4>(a, p, s);
+  }
+  if (a.tiles == 1) {
+    if (a.waves == 8) launch_stream<T, HD, 1, 8>(a, p, s);
+    else launch_stream<T, HD, 1, 4>(a, p, s);
   }
   if (a.splits > 1) {
     const int64_t n = (int64_t)p.M * p.H;

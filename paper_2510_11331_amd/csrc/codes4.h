@@ -61,20 +61,35 @@ __device__ __forceinline__ void decode4(uint32_t c, float s, float (&x)[8]) {
   x[4] = d[0]; x[5] = d[1]; x[6] = e[0]; x[7] = e[1];
 }
 
+// Where the sequences start and end, and their lengths: in LDS for up to PLACES of them, so that looking a row up costs
+// one round of memory latency; past that from memory.
+constexpr int PLACES = 1024;
+struct Places {
+  int cu[PLACES + 1], len[PLACES];
+  __device__ __forceinline__ void load(const KvRows& s) {
+    if (s.B > PLACES) return;
+    for (int i = threadIdx.x; i <= s.B; i += blockDim.x) {
+      cu[i] = s.cu[i];
+      if (i < s.B) len[i] = s.len[i];
+    }
+  }
+};
 // Sequence of row r (the last one that starts at or before it) and its
 // position; false where r belongs to none.  cu is read within [0, B] whatever
 // it holds.
-__device__ __forceinline__ bool row_place(const KvRows& s, int r, int& b, int& pos) {
-  int lo = 0, hi = s.B;                          // cu[lo] <= r < cu[hi], if r is of a sequence
-  if (s.cu[0] > r || s.cu[s.B] <= r) return false;
+__device__ __forceinline__ bool row_place(const KvRows& s, const Places& at, int r, int& b, int& pos) {
+  const bool near = s.B <= PLACES;
+  auto cu = [&](int i) { return near ? at.cu[i] : s.cu[i]; };
+  if (cu(0) > r || cu(s.B) <= r) return false;
+  int lo = 0, hi = s.B;                          // cu[lo] <= r < cu[hi]
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (s.cu[mid] <= r) lo = mid;
+    if (cu(mid) <= r) lo = mid;
     else hi = mid;
   }
   b = lo;
-  const int len = s.len[b];
-  pos = len > 0 ? len - (s.cu[lo + 1] - r) : -1;   // cu[lo + 1] > r
+  const int len = near ? at.len[b] : s.len[b];
+  pos = len > 0 ? len - (cu(lo + 1) - r) : -1;   // cu[lo + 1] > r
   return true;
 }
 // page of a position, or -1

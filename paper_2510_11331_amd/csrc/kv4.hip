@@ -59,23 +59,36 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
   const int per_row = (MODE == KV4_HEADS || MODE == KV4_BOTH ? p.H : 0) + (MODE == KV4_HEADS ? 1 : 2) * p.KV;
   const int64_t item = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
   const int i = threadIdx.x % LANES;
+  __shared__ Places s_places;
+  if constexpr (MODE != KV4_HEADS) {
+    s_places.load(p.rows);
+    __syncthreads();
+  }
   if (item >= (int64_t)p.M * per_row) return;    // whole heads: the shuffles below stay within one
   const int row = (int)(item / per_row), h0 = (int)(item % per_row);
   const int nq = MODE == KV4_HEADS || MODE == KV4_BOTH ? p.H : 0;
   const int what = h0 < nq ? 0 : h0 < nq + p.KV ? 1 : 2;      // query, key, value
   const int h = what == 0 ? h0 : what == 1 ? h0 - nq : h0 - nq - p.KV;
 
+  float x[2][8];
+  if constexpr (MODE != KV4_READ) {              // (rows of no sequence are read all the same)
+    const T* const src = what == 0   ? (const T*)p.q + (size_t)row * p.ldq
+                         : what == 1 ? (const T*)p.k + (size_t)row * p.ldk
+                                     : (const T*)p.v + (size_t)row * p.ldv;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) load8(src + h * HD + half * (HD / 2) + 8 * i, x[half]);
+  }
+
   int b = 0, pos = 0, page = -1;
   if constexpr (MODE == KV4_HEADS) {
     if (p.positions) pos = p.positions[row];
   } else {
-    if (!row_place(p.rows, row, b, pos)) return;
+    if (!row_place(p.rows, s_places, row, b, pos)) return;
     page = what ? row_page(p.rows, b, pos, p.n_blocks) : -1;
   }
   const int t = pos & 15;
   uint8_t* const pg = p.pool + ((size_t)max(page, 0) * p.KV + h) * P::BYTES;
 
-  float x[2][8];
   if constexpr (MODE == KV4_READ) {
     T* const out = (T*)(what == 1 ? p.k_out : p.v_out) + (size_t)row * (what == 1 ? p.ldko : p.ldvo) + h * HD;
 #pragma unroll
@@ -100,12 +113,6 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
     }
     return;
   }
-
-  const T* const src = what == 0   ? (const T*)p.q + (size_t)row * p.ldq
-                       : what == 1 ? (const T*)p.k + (size_t)row * p.ldk
-                                   : (const T*)p.v + (size_t)row * p.ldv;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) load8(src + h * HD + half * (HD / 2) + 8 * i, x[half]);
 
   if (MODE != KV4_APPEND && what != 2) {
     double y[2][8];

@@ -1539,7 +1539,7 @@ size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int he
   // fp32 rows take the smaller workgroups, and so the larger sums
   size_t n = 0;
   for (int dtype : {0, 1})
-    n = std::max(n, attention4_part_floats(plan_attention4(dtype, M, n_heads, n_kv_heads, n_seqs, max_len), M, n_heads, head_dim));
+    n = std::max(n, attention4_part_floats(plan_attention4(dtype, head_dim, M, n_heads, n_kv_heads, n_seqs, max_len), M, n_heads, head_dim));
   return n * sizeof(float);
 }
 
@@ -1568,8 +1568,7 @@ int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int 
   p.rows = kv_rows(rows);
   p.causal = causal != 0;
   p.scale = scale;
-  const Attn4Plan plan = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, M, n_heads, KV, rows->n_seqs, len);
-  p.splits = plan.splits;
+  const Attn4Plan plan = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, M, n_heads, KV, rows->n_seqs, len);
   p.part_o = (float*)workspace;
   p.part_ml = p.part_o + (size_t)plan.splits * M * n_heads * hd;
   HIPCHK(launch_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, plan, p, (hipStream_t)stream));
