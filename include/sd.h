@@ -417,7 +417,7 @@ int sd_plan_gate_up_q(int M, int F, int K, int fast, sd_linear_q_plan *out);
  *     (cu_rows [n_seqs + 1] ascending from 0, at most M) and, with them,
  *     lengths[b] tokens: row r is at position lengths[b] - cu_rows[b + 1] + r,
  *     token position % 16 of page table[b, position / 16].  Rows at or behind
- *     cu_rows[n_seqs] are of no sequence: they are not read, and what belongs
+ *     cu_rows[n_seqs] are of no sequence: they are not used, and what belongs
  *     to them is left as it was.  The three arrays are int32 on the device, so
  *     that a captured call follows what they hold.
  *     A position before the first, behind the table's width or whose table
@@ -495,6 +495,17 @@ size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int he
 int sd_attention_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int n_heads, int dtype, const void *q, int ldq,
                    void *out, int ldo, int causal, float scale, int max_len, void *workspace, size_t workspace_bytes,
                    void *stream);
+
+/* How sd_attention_q runs (host only): the choice the launch itself makes.
+ * SD_EINVAL: a size that the call refuses, or no rows. */
+typedef struct sd_attention_q_plan {
+    int shared;             /* 1: keys and values converted once for a workgroup, in LDS; 0: by each wave */
+    int vectors, waves;     /* of a workgroup: query vectors (heads of rows) at most */
+    int key_ranges;         /* whose outputs a second kernel joins (1: none) */
+    int streamed;           /* 1: loads that do not stay in the caches       */
+} sd_attention_q_plan;
+int sd_plan_attention_q(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len, int dtype,
+                        sd_attention_q_plan *out);
 
 /* Copy slot state to out [B, 4] int32 (device): committed target length
  * P, next input token x0, pending draft input (-1 if none), KV capacity. */

@@ -23,7 +23,7 @@ EXPORTS = ("sd_kv_pool_bytes", "sd_workspace_bytes", "sd_plan_projection", "sd_i
            "sd_pack_linear", "sd_linear_q_bytes", "sd_linear_q_workspace_bytes", "sd_pack_linear_q", "sd_add_rmsnorm_q", "sd_linear_q",
            "sd_linear_q_fast", "sd_gate_up_q_workspace_bytes", "sd_gate_up_q", "sd_gate_up_q_fast",
            "sd_plan_linear_q", "sd_plan_gate_up_q", "sd_kv_q_bytes", "sd_rope_table", "sd_norm_rope", "sd_kv_append_q",
-           "sd_norm_rope_append_q", "sd_kv_read_q", "sd_attention_q_workspace_bytes", "sd_attention_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
+           "sd_norm_rope_append_q", "sd_kv_read_q", "sd_attention_q_workspace_bytes", "sd_attention_q", "sd_plan_attention_q", "sd_sched_latency", "sd_sched_batching", "sd_sched_plan", "sd_sched_uplink")
 
 
 class ModelCfg(C.Structure):
@@ -73,6 +73,10 @@ class KvRows(C.Structure):
 class HeadNorm(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q_gain", "k_gain", "rope")] + [("gain_dtype", C.c_int), ("n_pos", C.c_int),
                                                                           ("eps", C.c_float)]
+
+
+class AttentionQPlan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("shared", "vectors", "waves", "key_ranges", "streamed")]
 
 
 class SchedModel(C.Structure):
@@ -152,6 +156,7 @@ def lib():
         "sd_norm_rope_append_q": (I, [P, P, I, I, I, P, I, P, I, P, I, P, P, I, P]),
         "sd_kv_read_q": (I, [P, P, I, I, P, I, P, I, P]),
         "sd_attention_q_workspace_bytes": (C.c_size_t, [I, I, I, I, I, I]),
+        "sd_plan_attention_q": (I, [I, I, I, I, I, I, I, C.POINTER(AttentionQPlan)]),
         "sd_attention_q": (I, [P, P, I, I, I, P, I, P, I, I, F, I, P, C.c_size_t, P]),
         "sd_sched_latency": (I, [C.POINTER(SchedCfg), I, C.POINTER(C.c_int32), I, C.POINTER(C.c_int32), I,
                                  C.POINTER(C.c_double)]),

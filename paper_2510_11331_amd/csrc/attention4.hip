@@ -33,8 +33,6 @@
 #include "codes4.h"
 
 #include <float.h>
-#include <stdio.h>
-#include <stdlib.h>
 #include <math.h>
 
 #include <algorithm>
@@ -889,15 +887,7 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   } else if (items <= 128 && max_len >= 2560) {
     a.splits = a.waves == 8 ? 2 : 4;
   }
-  a.stream = !a.tile_kernel && vectors <= 16 * a.tiles && (double)nz * max_len * KV * 17 * hd / 16 > 268435456.0;
-  if (const char* e = getenv("SD_A4")) {
-    int t, w, sp;
-    if (sscanf(e, "%d,%d,%d", &t, &w, &sp) == 3) {
-      a.tile_kernel = w == 0;
-      a.tiles = t; a.waves = w ? w : 4; a.splits = sp; a.blocks = (int)blocks(16 * t);
-      a.stream = false;
-    }
-  }
+  a.stream = !a.tile_kernel && vectors <= 16 * a.tiles && (double)nz * max_len * KV * 17 * hd / 16 > 536870912.0;
   return a;
 }
 

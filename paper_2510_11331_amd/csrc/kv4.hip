@@ -53,6 +53,14 @@ __device__ __forceinline__ void gain8(const void* g, int bf16, int i, double (&x
   for (int e = 0; e < 8; ++e) x[e] = bf16 ? bf2f(((const bf16_t*)g)[i + e]) : ((const float*)g)[i + e];
 }
 
+// x^-1/2 for x > 0: the hardware's estimate (24 bits) and two steps of Newton's iteration, each of which squares the error
+__device__ __forceinline__ double rsqrt64(double x) {
+  if (x == INFINITY) return 0.0;
+  double y = __builtin_amdgcn_rsq(x);
+  y = y * fma(-0.5 * x * y, y, 1.5);
+  return y * fma(-0.5 * x * y, y, 1.5);
+}
+
 template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) void kv4_kernel(Kv4Params p) {
   using P = Page4<HD>;
   constexpr int LANES = HD / 16;
@@ -126,7 +134,7 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
         for (int e = 0; e < 8; ++e) sum += (double)x[half][e] * x[half][e];
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-      r = 1.0 / sqrt(sum / HD + p.eps);
+      r = rsqrt64(sum / HD + p.eps);
     }
 #pragma unroll
     for (int half = 0; half < 2; ++half) {

@@ -1532,15 +1532,25 @@ int sd_kv_read_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int dt
   return SD_OK;
 }
 
+static bool attention_q_sizes_ok(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len) {
+  return M >= 1 && M <= KV4_MAX_ROWS && n_heads >= 1 && kv_q_heads_ok(n_heads, n_kv_heads, head_dim) && n_seqs >= 1 &&
+         n_seqs <= KV4_MAX_ROWS && max_len >= 1;
+}
+
 size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len) {
-  if (M < 1 || M > KV4_MAX_ROWS || n_heads < 1 || !kv_q_heads_ok(n_heads, n_kv_heads, head_dim) || n_seqs < 1 ||
-      n_seqs > KV4_MAX_ROWS || max_len < 1)
-    return 0;
-  // fp32 rows take the smaller workgroups, and so the larger sums
+  if (!attention_q_sizes_ok(M, n_heads, n_kv_heads, head_dim, n_seqs, max_len)) return 0;
   size_t n = 0;
   for (int dtype : {0, 1})
     n = std::max(n, attention4_part_floats(plan_attention4(dtype, head_dim, M, n_heads, n_kv_heads, n_seqs, max_len), M, n_heads, head_dim));
   return n * sizeof(float);
+}
+
+int sd_plan_attention_q(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len, int dtype,
+                        sd_attention_q_plan* out) {
+  if (!out || !attention_q_sizes_ok(M, n_heads, n_kv_heads, head_dim, n_seqs, max_len) || !dtype_ok(dtype)) return SD_EINVAL;
+  const Attn4Plan a = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, head_dim, M, n_heads, n_kv_heads, n_seqs, max_len);
+  *out = sd_attention_q_plan{a.tile_kernel, 16 * a.tiles, a.waves, a.splits, a.stream};
+  return SD_OK;
 }
 
 int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int n_heads, int dtype, const void* q, int ldq,

@@ -112,23 +112,26 @@ def attention(q, k, v, seen, scale):
     n, H, hd = q.shape
     KV = k.shape[1]
     out, err = np.zeros((n, H, hd)), np.zeros((2, n, H, hd))
-    with np.errstate(invalid="ignore", over="ignore"):
+    if k.shape[0] == 0:
+        return out, err
+    count, some = seen.sum(1)[:, None], seen.any(1)
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
         for h in range(H):
-            j = h // (H // KV)
-            for i in range(n):
-                m = seen[i]
-                if not m.any():
-                    continue
-                kk, vv = k[m, j], v[m, j]
-                z = kk @ q[i, h] * scale
-                mag = np.abs(kk) @ np.abs(q[i, h]) * abs(scale)
-                p = np.exp(z - z.max())
-                p /= p.sum()
-                out[i, h] = p @ vv
-                e = 2 * (hd + 4) * 2 * U32 * mag.max() + (8 + np.abs(z).max()) * 2 * U32 + (m.sum() / 2 + 128) * 2 * U32
-                # of the weighted sum, and of the sum that it is divided by
-                a, top = p @ np.abs(vv), np.abs(vv).max(0)
-                err[:, i, h] = 2 * e * a + 4 * m.sum() * 2.0 ** -126 * top
-                err[0, i, h] += 2.0 ** -23 * a
-                err[1, i, h] += 2.0 ** -12 * a + m.sum() * 2.0 ** -25 * top
+            kk, vv = k[:, h // (H // KV)], v[:, h // (H // KV)]
+            z = np.where(seen, q[:, h] @ kk.T * scale, -np.inf)
+            mag = np.where(seen, np.abs(q[:, h]) @ np.abs(kk).T * abs(scale), 0.0)
+            p = np.exp(z - z.max(1, keepdims=True))
+            p = np.where(seen, p / p.sum(1, keepdims=True), 0.0)
+            clean = np.where(np.isfinite(vv), vv, 0.0)
+            o, a = p @ clean, p @ np.abs(clean)                       # 0 times NaN is none where a row does not see it
+            o[(seen.astype(float) @ (~np.isfinite(vv)).astype(float)) > 0] = np.nan
+            # of the weighted sum, and of the sum that it is divided by
+            e = 2 * (hd + 4) * 2 * U32 * mag.max(1) + (8 + np.abs(np.where(seen, z, 0.0)).max(1)) * 2 * U32
+            e = e[:, None] + (count / 2 + 128) * 2 * U32
+            top = np.abs(clean).max(0)
+            err[:, :, h] = 2 * e * a + 4 * count * 2.0 ** -126 * top
+            err[0, :, h] += 2.0 ** -23 * a
+            err[1, :, h] += 2.0 ** -12 * a + count * 2.0 ** -25 * top
+            out[:, h] = np.where(some[:, None], o, 0.0)
+    err[:, ~some] = 0.0
     return out, err

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import kvplans
 import kvref
 from kvref import HALF, U32
 from sdcase import say
@@ -459,6 +460,68 @@ def test_pages_past_32_bits(KV, hd):
     for b in range(2):
         s = slice(b * n, b * n + n)
         close(got[s], *kvref.attention(q64[s], k64[s], v64[s], np.tril(np.ones((n, n), bool)), hd ** -0.5), "fp32")
+
+
+@pytest.mark.parametrize("case", kvplans.CASES, ids=lambda c: c[0])
+def test_attention_plans(case):
+    """Every kernel, on lengths around its steps and ranges, causal and over all keys; needles among the keys."""
+    from paper_2510_11331_amd import attention_q
+    name, rows, lengths, H, KV, hd, dtype, width, want_plan = case
+    say("plan", name)
+    r = np.random.default_rng([H, KV, hd, len(rows)])
+    rows = [min(n, m) for n, m in zip(rows, lengths)]
+    c = Case(r, rows, lengths, KV, hd, width=width)
+    assert kvplans.plan(c.M, H, KV, hd, dtype, len(rows), 16 * width) == want_plan
+    c.fill(r)
+    q = r.normal(size=(c.M, H, hd))
+    for b, m in enumerate(lengths):                      # every other row and head looks for a key of its own
+        k, _ = c.pool.get(*c.at(b, np.arange(m)))
+        for i in range(c.cu[b], c.cu[b + 1]):
+            h = np.arange(i % 2, H, 2)
+            q[i, h] = 1.5 * hd ** 0.5 * k[r.integers(0, c.pos[i] + 1, size=len(h)), h // (H // KV)] / (hd / 8)
+    x = t(q.astype(np.float32), dtype)
+    for causal in (True, False):
+        close(host(attention_q(x, c.cache(), c.desc, causal)), *c.attention(host(x), causal), dtype)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("what", ["large", "small", "tiny", "zero", "nan value", "nan key", "no page", "all sizes"])
+def test_attention_shared_values(what, hd):
+    """The kernel that shares converted values between its waves: values that its 16-bit form does not hold, NaN and
+    pages that are none, in the first steps, in the middle and among the last rows' own keys."""
+    from paper_2510_11331_amd import KVRows, attention_q
+    say("shared values", what, hd)
+    r = np.random.default_rng(12)
+    rows, lengths, H, KV = [520, 520], [700, 555], 32, 16
+    assert kvplans.plan(sum(rows), H, KV, hd, "bf16", 2, 16 * 44)[0] == 1
+    for at in (3, 40, 130, 690):
+        c = Case(r, rows, lengths, KV, hd)
+        c.fill(r)
+        x = r.normal(size=(2, 1, KV, hd)).astype(np.float32)
+        table = c.table.copy()
+        if what == "large":
+            x[1] *= 1e6
+        elif what == "small":
+            x[1] *= 1e-9
+        elif what == "tiny":
+            x[1] = 1e-40
+        elif what == "zero":
+            x[1] = 0
+        elif what == "nan value":
+            x[1, 0, 3, hd - 1] = np.nan
+        elif what == "nan key":
+            x[0, 0, 3, 0] = np.inf
+        elif what == "all sizes":
+            x[1] *= 2.0 ** r.integers(-40, 30, size=(1, KV, 1))
+        c.pool.put(*c.at(0, np.array([at])), x[0], x[1])
+        q, q64 = heads(r, c.M, H, hd, "bf16")
+        want, err = c.attention(q64)
+        if what == "no page":
+            table[0, at // 16] = -1
+            want[:rows[0]][c.pos[:rows[0]] >= at // 16 * 16] = np.nan
+        got = host(attention_q(q, c.cache(), KVRows(c.desc.cu_rows, c.desc.lengths, t(table))))
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        close(got, want, err, "bf16")
 
 
 # ------------------------------------------------------------------ as a program runs them

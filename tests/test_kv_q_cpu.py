@@ -150,3 +150,45 @@ def test_row_strides():
     for y in (x[:, ::2], x[:, :, :32], x.expand(5, 10, 64).transpose(0, 1), x.double(), x[:1].expand(5, 10, 64)):
         with pytest.raises(ValueError):
             _stride(y, "y", *y.shape[:2], 64, f, -1)
+
+
+@needs_lib
+def test_plans():
+    """The GPU cases run on the kernels that they name, and there is no kernel that none of them runs on."""
+    import kvplans
+    seen = set()
+    for name, rows, lengths, H, KV, hd, dtype, width, want in kvplans.CASES:
+        got = kvplans.plan(sum(rows), H, KV, hd, dtype, len(rows), 16 * width)
+        assert got == want, (name, got)
+        seen.add(kvplans.kind(got, hd, dtype))
+    parts = lambda k: (k[:6], (k[0], k[1], k[6]))             # the first kernel, and the second
+    first, second = {parts(k)[0] for k in seen}, {parts(k)[1] for k in seen}
+    missing = {}
+    for hd in (64, 128):
+        for dtype in ("bf16", "fp32"):
+            for B in (1, 2, 7, 16, 33, 64, 200):
+                for n in (1, 2, 5, 17, 100, 700, 2048):
+                    for H, KV in ((1, 1), (8, 1), (40, 5), (32, 8), (32, 32), (64, 8), (128, 128), (640, 64)):
+                        for length in (16, 500, 1500, 1600, 3000, 9000, 33000, 400000):
+                            k = kvplans.kind(kvplans.plan(B * n, H, KV, hd, dtype, B, length), hd, dtype)
+                            for part, have in zip(parts(k), (first, second)):
+                                if part not in have:
+                                    missing.setdefault(part, (B, n, H, KV, length))
+    assert not missing
+
+
+@needs_lib
+def test_workspace():
+    """Key ranges need it, whole and aligned."""
+    from paper_2510_11331_amd import _lib
+    L, E, A = _lib.lib(), _lib.SD_EINVAL, 1 << 20
+    pool, rows = _lib.KvQPool(A, 3000, 8, 128), _lib.KvRows(A, A, A, 1, 2048)
+    n = L.sd_attention_q_workspace_bytes(1, 32, 8, 128, 1, 32768)
+    assert n >= 32 * 2 * (128 + 2) * 4 and L.sd_attention_q_workspace_bytes(1, 32, 8, 128, 1, 1000) == 0
+    call = lambda ws, size, max_len: L.sd_attention_q(C.addressof(pool), C.addressof(rows), 1, 32, 0, A, 4096, A, 4096, 1, 0.1, max_len, ws,
+                                                      size, None)
+    assert call(None, n, 0) == call(A, n - 4, 0) == call(A + 4, n, 0) == call(None, 0, 10 ** 6) == E
+    p = _lib.AttentionQPlan()
+    for bad in ((0, 8, 8, 64, 1, 100, 0), (1, 9, 8, 64, 1, 100, 0), (1, 8, 8, 64, 0, 100, 0), (1, 8, 8, 64, 1, 0, 0), (1, 8, 8, 64, 1, 100, 2)):
+        assert L.sd_plan_attention_q(*bad, C.byref(p)) == E, bad
+    assert L.sd_plan_attention_q(1, 8, 8, 64, 1, 100, 0, None) == E
