@@ -47,10 +47,20 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
   }
 }
 
-// 8 entries of a gain (aligned to its entries only)
-__device__ __forceinline__ void gain8(const void* g, int bf16, int i, double (&x)[8]) {
+// 8 entries of a gain, which is aligned to its entries only (wide loads of any address are within the memory unit's rules)
+__device__ __forceinline__ void gain8(const void* g, int bf16, int i, float (&x)[8]) {
+  typedef uint16_t halves8 __attribute__((ext_vector_type(8), aligned(2)));
+  typedef float floats4 __attribute__((ext_vector_type(4), aligned(4)));
+  if (bf16) {
+    const halves8 a = *(const halves8*)((const bf16_t*)g + i);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = bf16 ? bf2f(((const bf16_t*)g)[i + e]) : ((const float*)g)[i + e];
+    for (int e = 0; e < 8; ++e) x[e] = bf2f(a[e]);
+  } else {
+    const floats4* const f = (const floats4*)((const float*)g + i);
+    const floats4 a = f[0], b = f[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
+  }
 }
 
 // x^-1/2 for x > 0: the hardware's estimate (24 bits) and two steps of Newton's iteration, each of which squares the error
@@ -123,44 +133,43 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
   }
 
   if (MODE != KV4_APPEND && what != 2) {
-    double y[2][8];
-    double r = 1.0;
+    // The gain and the rotation are read before the sum that they wait for.
     const void* const gain = what == 0 ? p.q_gain : p.k_gain;
+    float g[2][8];
+    if (gain) {
+      gain8(gain, p.gain_bf16, 8 * i, g[0]);
+      gain8(gain, p.gain_bf16, HD / 2 + 8 * i, g[1]);
+    }
+    float4 w[4] = {};
+    if (p.rope) {
+      const bool in = (unsigned)pos < (unsigned)p.n_pos;
+      const float4* const cs = (const float4*)(p.rope + ((size_t)(in ? pos : 0) * (HD / 2) + 8 * i) * 2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = in ? cs[e] : make_float4(NAN, NAN, NAN, NAN);
+    }
+    double r = 1.0;
     if (gain) {
       double sum = 0.0;
 #pragma unroll
       for (int half = 0; half < 2; ++half)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += (double)x[half][e] * x[half][e];
+        for (int e = 0; e < 8; ++e) sum = fma((double)x[half][e], (double)x[half][e], sum);
 #pragma unroll
       for (int o = LANES / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
       r = rsqrt64(sum / HD + p.eps);
+    } else {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[half][e] = 1.0f;
     }
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      double g[8];
-      if (gain) gain8(gain, p.gain_bf16, half * (HD / 2) + 8 * i, g);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[half][e] = gain ? x[half][e] * r * g[e] : x[half][e];
+    for (int e = 0; e < 8; ++e) {
+      const double y0 = x[0][e] * r * g[0][e], y1 = x[1][e] * r * g[1][e];
+      const double c = e % 2 ? w[e / 2].z : w[e / 2].x, sn = e % 2 ? w[e / 2].w : w[e / 2].y;
+      x[0][e] = (float)(p.rope ? y0 * c - y1 * sn : y0);
+      x[1][e] = (float)(p.rope ? y1 * c + y0 * sn : y1);
     }
-    if (p.rope) {
-      const bool in = (unsigned)pos < (unsigned)p.n_pos;
-      const float4* const cs = (const float4*)(p.rope + ((size_t)(in ? pos : 0) * (HD / 2) + 8 * i) * 2);
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        float4 w = cs[e / 2];
-        if (!in) w = make_float4(NAN, NAN, NAN, NAN);
-        const double a0 = y[0][e], b0 = y[1][e], a1 = y[0][e + 1], b1 = y[1][e + 1];
-        y[0][e] = a0 * w.x - b0 * w.y;
-        y[1][e] = b0 * w.x + a0 * w.y;
-        y[0][e + 1] = a1 * w.z - b1 * w.w;
-        y[1][e + 1] = b1 * w.z + a1 * w.w;
-      }
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[half][e] = (float)y[half][e];
     if (MODE == KV4_HEADS || what == 0) {
       T* const out = what == 0 ? (T*)p.q_out + (size_t)row * p.ldqo : (T*)p.k_out + (size_t)row * p.ldko;
 #pragma unroll

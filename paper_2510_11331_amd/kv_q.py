@@ -29,7 +29,7 @@ from typing import Optional, Tuple
 import torch
 
 from ._lib import SD_DTYPE_BF16, SD_DTYPE_F32, SD_OK, HeadNorm, KvQPool, KvRows, check, lib
-from .ffn_q import _elsewhere, _raw_stream
+from .ffn_q import _current_device, _elsewhere, _raw_stream
 
 PAGE = 16
 _DTYPES = {torch.bfloat16: SD_DTYPE_BF16, torch.float32: SD_DTYPE_F32}
@@ -63,7 +63,7 @@ class KVRows:
     int32 on the GPU, read when a call runs: a captured pass follows what is written to them.  max_len: the longest length
     that the work is to be split for (default: what the table holds)."""
 
-    __slots__ = ("cu_rows", "lengths", "table", "max_len", "_index", "_rows", "_at")
+    __slots__ = ("cu_rows", "lengths", "table", "max_len", "_index", "_rows", "_at", "_workspace")
 
     def __init__(self, cu_rows: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, max_len: Optional[int] = None):
         n = lengths.shape[0] if lengths.dim() == 1 else -1
@@ -79,6 +79,7 @@ class KVRows:
         self._index = table.get_device()
         self._rows = KvRows(cu_rows.data_ptr(), lengths.data_ptr(), table.data_ptr(), n, table.shape[1])
         self._at = C.addressof(self._rows)
+        self._workspace = {}                       # bytes of an attention's workspace, by (rows, heads, kv heads, head_dim)
 
 
 def rope_table(n_pos: int, head_dim: int, theta: float = 10000.0, device="cuda",
@@ -100,41 +101,44 @@ def _stride(x: torch.Tensor, what: str, M: int, heads: int, hd: int, dtype: torc
     """The row stride of heads [M, heads, hd]."""
     if x.shape != (M, heads, hd) or x.dtype != dtype or x.get_device() != index:
         raise ValueError(f"{what}: [{M}, {heads}, {hd}] {dtype} on the device of the others")
-    if M == 0:
-        return heads * hd
     row, head, one = x.stride()
-    if one != 1 or (heads > 1 and head != hd):
+    if M < 2:
+        row = heads * hd
+        if M == 0:
+            return row
+    if one != 1 or (head != hd and heads > 1):
         raise ValueError(f"{what}: heads of adjacent entries, adjacent in their row")
-    if M == 1:
-        return heads * hd
     if not heads * hd <= row < 1 << 31:
         raise ValueError(f"{what}: rows apart by at least their length")
     return row
 
 
-def _norm(q: torch.Tensor, hd: int, index: int, rope, q_gain, k_gain, eps: float) -> HeadNorm:
-    dt = torch.bfloat16
-    for g in (q_gain, k_gain):
+def _norm(hd: int, index: int, rope, q_gain, k_gain, eps: float) -> HeadNorm:
+    dt, at = None, [None, None]
+    for i, g in enumerate((q_gain, k_gain)):
         if g is not None:
-            dt = g.dtype
-            if g.shape != (hd,) or dt not in _DTYPES or not g.is_contiguous() or g.get_device() != index:
+            if g.shape != (hd,) or g.dtype not in _DTYPES or not g.is_contiguous() or g.get_device() != index:
                 raise ValueError("gains: contiguous [head_dim], bfloat16 or float32, on the device of q")
-    if q_gain is not None and k_gain is not None and q_gain.dtype != k_gain.dtype:
-        raise ValueError("gains of one type")
-    if rope is not None and (rope.dim() != 3 or rope.shape[1:] != (hd // 2, 2) or rope.dtype != torch.float32
-                             or not rope.is_contiguous() or rope.get_device() != index or rope.shape[0] < 1):
+            if dt is not None and g.dtype != dt:
+                raise ValueError("gains of one type")
+            dt, at[i] = g.dtype, g.data_ptr()
+    code = SD_DTYPE_BF16 if dt is None else _DTYPES[dt]
+    if rope is None:
+        return HeadNorm(at[0], at[1], None, code, 0, eps)
+    shape = rope.shape
+    if (shape[1:] != (hd // 2, 2) or shape[0] < 1 or rope.dtype != torch.float32 or not rope.is_contiguous()
+            or rope.get_device() != index):
         raise ValueError("rope: contiguous float32 [positions, head_dim / 2, 2] on the device of q")
-    return HeadNorm(None if q_gain is None else q_gain.data_ptr(), None if k_gain is None else k_gain.data_ptr(),
-                    None if rope is None else rope.data_ptr(), _DTYPES[dt], 0 if rope is None else rope.shape[0], eps)
+    return HeadNorm(at[0], at[1], rope.data_ptr(), code, shape[0], eps)
 
 
 def _shape(x: torch.Tensor) -> Tuple[int, int, int, int]:
-    if x.dim() != 3 or x.dtype not in _DTYPES or x.shape[2] not in (64, 128) or x.shape[1] < 1:
+    shape, index = x.shape, x.get_device()
+    if len(shape) != 3 or x.dtype not in _DTYPES or shape[2] not in (64, 128) or shape[1] < 1:
         raise ValueError("q, k, v: [rows, heads, head_dim], bfloat16 or float32, head_dim 64 or 128")
-    index = x.get_device()
     if index < 0:
         raise ValueError("tensors on a GPU are needed")
-    return (*x.shape, index)
+    return (*shape, index)
 
 
 def norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
@@ -145,25 +149,24 @@ def norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor
     rope[positions[row]] (rope None: no rotation; entries i and i + head_dim / 2 are a pair).  positions int32 [rows].
     q_out, k_out: where they go (the inputs themselves, or memory that overlaps none)."""
     M, H, hd, index = _shape(q)
-    there = _elsewhere(q, stream)
-    if there is not None:
-        with there:
+    if stream is not None or index != _current_device():
+        with _elsewhere(q, stream):
             return norm_rope(q, k, positions, rope, q_gain, k_gain, eps, q_out, k_out)
     KV = k.shape[1] if k.dim() == 3 else 0
     if KV < 1 or H % KV:
         raise ValueError("k: [rows, heads, head_dim], its heads a divisor of the query heads")
     ldq, ldk = _stride(q, "q", M, H, hd, q.dtype, index), _stride(k, "k", M, KV, hd, q.dtype, index)
-    n = _norm(q, hd, index, rope, q_gain, k_gain, eps)
+    n = _norm(hd, index, rope, q_gain, k_gain, eps)
     if rope is not None and (positions is None or positions.shape != (M,) or positions.dtype != torch.int32
                              or not positions.is_contiguous() or positions.get_device() != index):
         raise ValueError("positions: contiguous int32 [rows] on the device of q")
     ldqo, ldko = H * hd, KV * hd
     if q_out is None:
-        q_out = torch.empty((M, H, hd), dtype=q.dtype, device=q.device)
+        q_out = torch.empty(M, H, hd, dtype=q.dtype, device=q.device)
     else:
         ldqo = _stride(q_out, "q_out", M, H, hd, q.dtype, index)
     if k_out is None:
-        k_out = torch.empty((M, KV, hd), dtype=q.dtype, device=q.device)
+        k_out = torch.empty(M, KV, hd, dtype=q.dtype, device=q.device)
     else:
         ldko = _stride(k_out, "k_out", M, KV, hd, q.dtype, index)
     rc = lib().sd_norm_rope(M, H, KV, hd, _DTYPES[q.dtype], q.data_ptr(), ldq, k.data_ptr(), ldk,
@@ -183,9 +186,8 @@ def kv_append_q(cache: KVCacheQ, k: torch.Tensor, v: torch.Tensor, rows: KVRows,
                 stream: Optional[torch.cuda.Stream] = None) -> None:
     """Quantise the rows' keys and values into the cache, at their positions."""
     M, KV, hd, index = _shape(k)
-    there = _elsewhere(k, stream)
-    if there is not None:
-        with there:
+    if stream is not None or index != _current_device():
+        with _elsewhere(k, stream):
             return kv_append_q(cache, k, v, rows)
     if KV != cache.n_kv_heads or hd != cache.head_dim:
         raise ValueError(f"k: [rows, {cache.n_kv_heads}, {cache.head_dim}]")
@@ -203,9 +205,8 @@ def norm_rope_append_q(cache: KVCacheQ, q: torch.Tensor, k: torch.Tensor, v: tor
     """norm_rope at the rows' positions: q is returned, k (its values in float32) and v go into the cache.  q_out: where
     q goes (q itself, or memory that overlaps no input)."""
     M, H, hd, index = _shape(q)
-    there = _elsewhere(q, stream)
-    if there is not None:
-        with there:
+    if stream is not None or index != _current_device():
+        with _elsewhere(q, stream):
             return norm_rope_append_q(cache, q, k, v, rows, rope, q_gain, k_gain, eps, q_out)
     KV = cache.n_kv_heads
     if hd != cache.head_dim or H % KV:
@@ -213,10 +214,10 @@ def norm_rope_append_q(cache: KVCacheQ, q: torch.Tensor, k: torch.Tensor, v: tor
     _same_device(cache, rows, index)
     ldq = _stride(q, "q", M, H, hd, q.dtype, index)
     ldk, ldv = _stride(k, "k", M, KV, hd, q.dtype, index), _stride(v, "v", M, KV, hd, q.dtype, index)
-    n = _norm(q, hd, index, rope, q_gain, k_gain, eps)
+    n = _norm(hd, index, rope, q_gain, k_gain, eps)
     ldqo = H * hd
     if q_out is None:
-        q_out = torch.empty((M, H, hd), dtype=q.dtype, device=q.device)
+        q_out = torch.empty(M, H, hd, dtype=q.dtype, device=q.device)
     else:
         ldqo = _stride(q_out, "q_out", M, H, hd, q.dtype, index)
     rc = lib().sd_norm_rope_append_q(cache._at, rows._at, M, H, _DTYPES[q.dtype], q.data_ptr(), ldq, k.data_ptr(), ldk,
@@ -231,9 +232,10 @@ def kv_read_q(cache: KVCacheQ, rows: KVRows, n_rows: int, dtype: torch.dtype = t
               stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """(k, v) [n_rows, heads, head_dim] of dtype at the rows' positions.  k_out, v_out: where they go."""
     index = cache._index
-    there = _elsewhere(cache.data, stream)
-    if there is not None:
-        with there:
+    if index < 0:
+        raise ValueError("a cache on a GPU is needed")
+    if stream is not None or index != _current_device():
+        with _elsewhere(cache.data, stream):
             return kv_read_q(cache, rows, n_rows, dtype, k_out, v_out)
     KV, hd = cache.n_kv_heads, cache.head_dim
     if dtype not in _DTYPES or n_rows < 0:
@@ -241,11 +243,11 @@ def kv_read_q(cache: KVCacheQ, rows: KVRows, n_rows: int, dtype: torch.dtype = t
     _same_device(cache, rows, index)
     ldk = ldv = KV * hd
     if k_out is None:
-        k_out = torch.empty((n_rows, KV, hd), dtype=dtype, device=cache.data.device)
+        k_out = torch.empty(n_rows, KV, hd, dtype=dtype, device=cache.data.device)
     else:
         ldk = _stride(k_out, "k_out", n_rows, KV, hd, dtype, index)
     if v_out is None:
-        v_out = torch.empty((n_rows, KV, hd), dtype=dtype, device=cache.data.device)
+        v_out = torch.empty(n_rows, KV, hd, dtype=dtype, device=cache.data.device)
     else:
         ldv = _stride(v_out, "v_out", n_rows, KV, hd, dtype, index)
     rc = lib().sd_kv_read_q(cache._at, rows._at, n_rows, _DTYPES[dtype], k_out.data_ptr(), ldk, v_out.data_ptr(), ldv,
@@ -260,9 +262,8 @@ def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = T
     """softmax(scale q K^T) V [rows, heads, head_dim] over the cached positions up to the row's own (causal) or all of its
     sequence's; scale: head_dim^-0.5 unless given.  Query heads share kv heads in runs.  out: where it goes."""
     M, H, hd, index = _shape(q)
-    there = _elsewhere(q, stream)
-    if there is not None:
-        with there:
+    if stream is not None or index != _current_device():
+        with _elsewhere(q, stream):
             return attention_q(q, cache, rows, causal, scale, out)
     KV = cache.n_kv_heads
     if hd != cache.head_dim or H % KV:
@@ -270,11 +271,14 @@ def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = T
     _same_device(cache, rows, index)
     ldq, ldo = _stride(q, "q", M, H, hd, q.dtype, index), H * hd
     if out is None:
-        out = torch.empty((M, H, hd), dtype=q.dtype, device=q.device)
+        out = torch.empty(M, H, hd, dtype=q.dtype, device=q.device)
     else:
         ldo = _stride(out, "out", M, H, hd, q.dtype, index)
     L = lib()
-    ws = L.sd_attention_q_workspace_bytes(M, H, KV, hd, rows._rows.n_seqs, rows.max_len)
+    sizes = (M, H, KV, hd)
+    ws = rows._workspace.get(sizes)
+    if ws is None:
+        ws = rows._workspace[sizes] = L.sd_attention_q_workspace_bytes(M, H, KV, hd, rows._rows.n_seqs, rows.max_len)
     work = torch.empty(ws, dtype=torch.uint8, device=q.device) if ws else None
     rc = L.sd_attention_q(cache._at, rows._at, M, H, _DTYPES[q.dtype], q.data_ptr(), ldq, out.data_ptr(), ldo, causal,
                           hd ** -0.5 if scale is None else scale, rows.max_len, work.data_ptr() if ws else None, ws,
