@@ -429,7 +429,8 @@ int sd_plan_gate_up_q(int M, int F, int K, int fast, sd_linear_q_plan *out);
  * multiple of 16 bytes.  1 <= n_kv_heads <= 1024, n_heads a multiple of it, at
  * most 1024 (0 where queries are left out), n_blocks <= 2^24, table_width <=
  * 2^20, 0 <= n_seqs <= 2^20, 0 <= M <= 2^20 (M = 0 and n_seqs = 0 enqueue
- * nothing and read no pointer). */
+ * nothing and read no pointer).  Calls whose launch would need 2^32 threads or
+ * more are refused (M or n_seqs times heads from 2^22 on may be). */
 typedef struct sd_kv_q_pool {
     void *data;
     int n_blocks, n_kv_heads, head_dim;
@@ -490,7 +491,10 @@ int sd_kv_read_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int dt
  * the formula has it (a key's in all of a head, a value block's in its 32
  * dimensions).  Sums and the softmax are in fp32.  out may not overlap q.  A length may
  * be anything up to 16 table_width: max_len (0: the table's width) only says
- * for which lengths the work is split. */
+ * for which lengths the work is split.  The workspace (16-byte aligned) is
+ * scratch of one call: what it held before does not matter, nothing in it is
+ * used after the call's work is done, and calls that may run at the same time
+ * (on two streams, in two graphs) need one each. */
 size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len);
 int sd_attention_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int n_heads, int dtype, const void *q, int ldq,
                    void *out, int ldo, int causal, float scale, int max_len, void *workspace, size_t workspace_bytes,

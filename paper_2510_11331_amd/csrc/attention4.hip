@@ -33,6 +33,7 @@
 #include "codes4.h"
 
 #include <float.h>
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -104,18 +105,30 @@ template <int PARTS> __device__ __forceinline__ void parts8(const float (&x)[8],
     }
 }
 
-// The vectors of workgroup `block`: sequence b, its first row, its rows n and the first of its vectors.  Sequence b has
-// ceil(n G / cap) workgroups; every wave adds them up by itself, 64 sequences at a time.
+// The vectors of workgroup `block`: sequence b, its first row, its rows n and the first of its vectors.
 struct Block4 { int b, row0, n, v0, len; };
+// Up to 64 sequences: sequence b has ceil(n G / cap) workgroups, which every wave adds up by itself.
+// More (a sum of all of them in each workgroup would cost as much as the attention does: 64 keys of 512 sequences 32 us,
+// of 4096 sequences 786 us): with u = gcd(G, cap) and C = cap / u, sequence b's workgroups are those from S(b) = floor((cu[b] G /
+// u + (C - 1) b) / C) on.  S(b + 1) - S(b) >= floor((n G / u - 1) / C) + 1 = ceil(n G / cap) for n >= 1, so they suffice; the
+// few between its last and S(b + 1) have nothing to do.  A wave looks at 64 values of S at a time.
+constexpr int SUMMED = 64;
+__host__ __device__ constexpr int common4(int a, int b) {
+  while (b) {
+    const int r = a % b;
+    a = b;
+    b = r;
+  }
+  return a;
+}
 __device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int cap, int block, Block4& o) {
   const int lane = threadIdx.x & 63;
-  for (int b0 = 0; b0 < s.B; b0 += 64) {
-    const int b = b0 + lane;
-    int lo = 0, hi = 0, len = 0;
-    if (b < s.B) {
-      lo = min(max(s.cu[b], 0), M);
-      hi = min(max(s.cu[b + 1], lo), M);
-      len = s.len[b];                            // (of all of them: not a second round of latency)
+  int lo = 0, hi = 0, len = 0, at, before;       // a lane's sequence; the lane that has the workgroup's, and its workgroups before this
+  if (s.B <= SUMMED) {
+    if (lane < s.B) {
+      lo = min(max(s.cu[lane], 0), M);
+      hi = min(max(s.cu[lane + 1], lo), M);
+      len = s.len[lane];                         // (of all of them: not a second round of latency)
     }
     const int mine = ((hi - lo) * G + cap - 1) / cap;
     int sum = mine;
@@ -124,19 +137,38 @@ __device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int ca
       const int up = __shfl_up(sum, k);
       if (lane >= k) sum += up;
     }
-    const int total = __builtin_amdgcn_readlane(sum, 63);
-    if (block < total) {
-      const int at = __builtin_ctzll(__ballot(sum > block));
-      o.b = b0 + at;
-      o.row0 = __builtin_amdgcn_readlane(lo, at);
-      o.n = __builtin_amdgcn_readlane(hi, at) - o.row0;
-      o.len = __builtin_amdgcn_readlane(len, at);
-      o.v0 = (block - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at))) * cap;
-      return (unsigned)o.v0 < (unsigned)(o.n * G);           // (row counts that overflow, of no valid cu)
-    }
-    block -= total;
+    const uint64_t past = __ballot(sum > block);
+    if (!past) return false;
+    at = __builtin_ctzll(past);
+    before = block - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at));
+    o.b = at;
+  } else {
+    const int u = common4(cap, G), C = cap / u;
+    int b0 = 0, b1 = s.B, step, start;           // S(b0) <= block < S(b1), where the workgroup is any sequence's
+    do {
+      step = (b1 - b0 + 63) / 64;
+      const int b = b0 + step * lane;
+      start = INT_MAX;
+      if (b < b1) {
+        lo = min(max(s.cu[b], 0), M);
+        hi = min(max(s.cu[b + 1], lo), M);
+        len = s.len[b];
+        start = (int)(((int64_t)lo * (G / u) + (int64_t)(C - 1) * b) / C);
+      }
+      const uint64_t past = __ballot(start > block);
+      at = past ? __builtin_ctzll(past) - 1 : 63;
+      if (at < 0) return false;
+      b0 += step * at;
+      b1 = min(b1, b0 + step);
+    } while (step > 1);
+    before = block - __builtin_amdgcn_readlane(start, at);
+    o.b = b0;
   }
-  return false;
+  o.row0 = __builtin_amdgcn_readlane(lo, at);
+  o.n = __builtin_amdgcn_readlane(hi, at) - o.row0;
+  o.len = __builtin_amdgcn_readlane(len, at);
+  o.v0 = before * cap;
+  return before < (o.n * G + cap - 1) / cap;
 }
 
 // keys that vector v of a sequence sees
@@ -566,12 +598,11 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 // is one fp16 part (off by 2^-12 of itself, an eighth of the output's own rounding) and half the products of the second
 // matrix are saved.  A workgroup that meets a value outside that range (or NaN) takes the rest of its keys as above.  fp32 outputs: values in
 // bf16 and three parts.
-template <typename T, int HD, int QT>
-__global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) {
+template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) {
+  using T = bf16_t;
   using P = Page4<HD>;
   using L4 = typename Load4<HD>::type;
-  constexpr int KS = HD / 32, DT = HD / 16, QP = QUERY_PARTS<T>, PP = WEIGHT_PARTS<T>;
-  constexpr bool F16 = sizeof(T) == 2;
+  constexpr int QT = 2, KS = HD / 32, DT = HD / 16;
   __shared__ u32x4 s_k[2][2][KS][64];            // [buffer][page][k-step][lane]
   __shared__ u32x4 s_v[3][DT][64];               // [buffer][tile][lane]: four keys of either page
   __shared__ int s_leave[3];                     // step + 1 that is not for the loop over LDS
@@ -593,7 +624,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   const int first = w.v0 + 16 * QT * wave, on = min(16 * QT, nv - 16 * QT * wave);
   const int mine_min = on > 0 ? sees(p, len, w.n, first, G) : 0;
   const int mine_max = on > 0 ? loop_keys(p, sees(p, len, w.n, first + on - 1, G)) : 0;
-  u32x4 q[QT][KS][QP];
+  u32x4 q[QT][KS][1];
   int vis[QT];
   float m[QT];
   f32x4 o[QT][DT], l[QT];                        // l: the weights' sum, four times, as the product with a tile of ones
@@ -668,7 +699,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
     [&]<int... B>(std::integer_sequence<int, B...>) {
       (([&] {
          uint32_t even[2], odd[2];
-         value_tiles<HD, B, 1, F16>(cs, s, even, odd);
+         value_tiles<HD, B, 1, true>(cs, s, even, odd);
          u32x2* const to = (u32x2*)&s_v[vb][half * (DT / 2) + 2 * B][lane] + mypage;
          to[0] = u32x2{even[0], even[1]};
          to[2 * 64] = u32x2{odd[0], odd[1]};
@@ -680,9 +711,8 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
   auto convert = [&](const Raw& a, int i, int kb, int vb) {
     put_keys(a, kb);
     put_values(a, vb);
-    // fp16: the four scales at once, E + 24 of 128 to 159 (a carry from a byte is of one that is outside); else only NaN
-    const bool outside = F16 ? ((a.vE + 0x18181818u) & 0xe0e0e0e0u) != 0x80808080u
-                             : (a.vE & 255u) == 255u || (a.vE >> 8 & 255u) == 255u || (a.vE >> 16 & 255u) == 255u || a.vE >> 24 == 255u;
+    // the four scales at once, E + 24 of 128 to 159 (a carry from a byte is of one that is outside)
+    const bool outside = ((a.vE + 0x18181818u) & 0xe0e0e0e0u) != 0x80808080u;
     if (a.none || __any(outside)) {
       bool leave = a.none;
 #pragma unroll
@@ -691,7 +721,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
         uint32_t codes;
         if constexpr (HD == 128) codes = a.vc[e];
         else codes = e & 1 ? a.vc[e / 2] >> 16 : a.vc[e / 2] & 0xffffu;
-        leave |= E == 255u || (F16 && E - 104u > 31u && (codes & 0x77777777u) != 0);      // (zeros have E = 1)
+        leave |= E == 255u || (E - 104u > 31u && (codes & 0x77777777u) != 0);      // (zeros have E = 1)
       }
       if (__any(leave) && lane == 0) s_leave[vb] = i + 1;
     }
@@ -713,9 +743,7 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int part = QP - 1; part >= 0; --part) z[u][t] = mfma_bf16(kf[s][t], q[u][s][part], z[u][t]);
+        for (int u = 0; u < QT; ++u) z[u][t] = mfma_bf16(kf[s][t], q[u][s][0], z[u][t]);
   };
   // Steps that all vectors see whole, while the workgroup meets no value outside fp16, no NaN and no page that is none.
   // Step i: its weights; the scores of step i + 1; its values; the conversion of step i + 2; the loads of step i + 4
@@ -748,36 +776,17 @@ __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) 
       scores();
 #pragma unroll
       for (int u = 0; u < QT; ++u) exp8(x[u]);
-      if constexpr (F16) {
-        u32x4 w8[QT];
+      u32x4 w8[QT];
 #pragma unroll
-        for (int u = 0; u < QT; ++u)
+      for (int u = 0; u < QT; ++u)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            w8[u][e] = __builtin_bit_cast(uint32_t, f16x2{(f16_t)x[u][2 * e], (f16_t)x[u][2 * e + 1]});
+        for (int e = 0; e < 4; ++e) w8[u][e] = __builtin_bit_cast(uint32_t, f16x2{(f16_t)x[u][2 * e], (f16_t)x[u][2 * e + 1]});
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int u = 0; u < QT; ++u) o[u][d] = mfma_f16(vf[d], w8[u], o[u][d]);
-        }
+        for (int u = 0; u < QT; ++u) o[u][d] = mfma_f16(vf[d], w8[u], o[u][d]);
 #pragma unroll
-        for (int u = 0; u < QT; ++u) l[u] = mfma_f16(u32x4{} + 0x3c003c00u, w8[u], l[u]);
-      } else {
-        u32x4 w8[QT][PP];
-#pragma unroll
-        for (int u = 0; u < QT; ++u) parts8<PP>(x[u], w8[u]);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-#pragma unroll
-          for (int u = 0; u < QT; ++u)
-#pragma unroll
-            for (int part = PP - 1; part >= 0; --part) o[u][d] = mfma_bf16(vf[d], w8[u][part], o[u][d]);
-        }
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int part = PP - 1; part >= 0; --part) l[u] = mfma_bf16(u32x4{} + 0x3f803f80u, w8[u][part], l[u]);
-      }
+      for (int u = 0; u < QT; ++u) l[u] = mfma_f16(u32x4{} + 0x3c003c00u, w8[u], l[u]);
       convert(raw[S], i + 2, S, vb == 0 ? 2 : vb - 1);     // (the buffers of steps i and i - 1)
       load(raw[S], i + 4);
       lds_barrier();
@@ -872,7 +881,12 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   Attn4Plan a{};
   const int64_t G = H / KV, nz = std::min(n_seqs, M);
   const int64_t vectors = (M + nz - 1) / nz * G;             // of an average sequence
-  auto blocks = [&](int64_t cap) { return (M * G - nz) / cap + nz; };   // sum of ceil(n G / cap) over nz sequences of M rows
+  // workgroups at most: the sum of ceil(n G / cap) over nz sequences of M rows, or what find_block numbers
+  auto blocks = [&](int64_t cap) {
+    if (n_seqs <= SUMMED) return (M * G - nz) / cap + nz;
+    const int64_t u = common4((int)cap, (int)G), C = cap / u;
+    return (M * (G / u) + (C - 1) * n_seqs) / C;
+  };
   auto typical = [&](int64_t cap) { return nz * ((vectors + cap - 1) / cap) * KV; };    // ... of alike sequences, and heads
   const int64_t steps = (max_len + 31) / 32;
   a.tile_kernel = dtype == 0 && vectors >= 128 && typical(128) >= 256;
@@ -906,7 +920,7 @@ template <typename T, int HD> static void launch_hd(const Attn4Plan& a, Attn4Par
   p.splits = a.splits;
   if constexpr (sizeof(T) == 2) {
     if (a.tile_kernel) {
-      attention4_tile_kernel<T, HD, 2><<<dim3((unsigned)a.blocks * p.KV), 256, 0, s>>>(p);
+      attention4_tile_kernel<HD><<<dim3((unsigned)a.blocks * p.KV), 256, 0, s>>>(p);
       return;
     }
     if (a.tiles == 2) launch_stream<T, HD, 2, 4>(a, p, s);

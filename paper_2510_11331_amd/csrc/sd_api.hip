@@ -1416,6 +1416,8 @@ static bool head_norm_ok(const sd_head_norm* n) {
   if (((uintptr_t)n->q_gain | (uintptr_t)n->k_gain) % esize(n->gain_dtype) || (uintptr_t)n->rope % 16) return false;
   return !n->rope || (n->n_pos >= 1 && n->n_pos <= KV4_MAX_BLOCKS);
 }
+// a grid holds less than 2^32 threads
+static bool kv_q_grid_ok(int M, int heads, int head_dim) { return (uint64_t)M * heads * (head_dim / 16) <= 0xffffff00u; }
 static void set_norm(Kv4Params& p, const sd_head_norm* n) {
   p.q_gain = n->q_gain;
   p.k_gain = n->k_gain;
@@ -1447,6 +1449,7 @@ int sd_norm_rope(int M, int n_heads, int n_kv_heads, int head_dim, int dtype, co
       !head_norm_ok(norm))
     return SD_EINVAL;
   if (M == 0) return SD_OK;
+  if (!kv_q_grid_ok(M, n_heads + n_kv_heads, head_dim)) return SD_EINVAL;
   if (!kv_q_rows_at(q, ldq, n_heads, head_dim, dtype) || !kv_q_rows_at(k, ldk, n_kv_heads, head_dim, dtype) ||
       !kv_q_rows_at(q_out, ldq_out, n_heads, head_dim, dtype) || !kv_q_rows_at(k_out, ldk_out, n_kv_heads, head_dim, dtype))
     return SD_EINVAL;
@@ -1476,6 +1479,7 @@ static int kv_write_q(Kv4Mode mode, const sd_kv_q_pool* pool, const sd_kv_rows* 
   const int KV = pool->n_kv_heads, hd = pool->head_dim;
   if (mode == KV4_BOTH && (n_heads < 1 || !kv_q_heads_ok(n_heads, KV, hd) || !head_norm_ok(norm))) return SD_EINVAL;
   if (M == 0 || rows->n_seqs == 0) return SD_OK;
+  if (!kv_q_grid_ok(M, n_heads + 2 * KV, hd)) return SD_EINVAL;
   if (!kv_q_rows_at(k, ldk, KV, hd, dtype) || !kv_q_rows_at(v, ldv, KV, hd, dtype) || !kv_q_arrays_ok(pool, rows)) return SD_EINVAL;
   Kv4Params p{};
   if (mode == KV4_BOTH) {
@@ -1515,6 +1519,7 @@ int sd_kv_read_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int dt
                  void* stream) {
   if (M < 0 || M > KV4_MAX_ROWS || !kv_q_pool_ok(pool) || !kv_q_rows_ok(rows) || !dtype_ok(dtype)) return SD_EINVAL;
   if (M == 0 || rows->n_seqs == 0) return SD_OK;
+  if (!kv_q_grid_ok(M, 2 * pool->n_kv_heads, pool->head_dim)) return SD_EINVAL;
   if (!kv_q_rows_at(k, ldk, pool->n_kv_heads, pool->head_dim, dtype) ||
       !kv_q_rows_at(v, ldv, pool->n_kv_heads, pool->head_dim, dtype) || !kv_q_arrays_ok(pool, rows))
     return SD_EINVAL;
@@ -1537,6 +1542,10 @@ static bool attention_q_sizes_ok(int M, int n_heads, int n_kv_heads, int head_di
          n_seqs <= KV4_MAX_ROWS && max_len >= 1;
 }
 
+static bool attention_q_grid_ok(const Attn4Plan& a, int KV) {
+  return (uint64_t)a.blocks * KV * a.splits * 64 * a.waves <= 0xffffffffu;
+}
+
 size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len) {
   if (!attention_q_sizes_ok(M, n_heads, n_kv_heads, head_dim, n_seqs, max_len)) return 0;
   size_t n = 0;
@@ -1549,6 +1558,7 @@ int sd_plan_attention_q(int M, int n_heads, int n_kv_heads, int head_dim, int n_
                         sd_attention_q_plan* out) {
   if (!out || !attention_q_sizes_ok(M, n_heads, n_kv_heads, head_dim, n_seqs, max_len) || !dtype_ok(dtype)) return SD_EINVAL;
   const Attn4Plan a = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, head_dim, M, n_heads, n_kv_heads, n_seqs, max_len);
+  if (!attention_q_grid_ok(a, n_kv_heads)) return SD_EINVAL;
   *out = sd_attention_q_plan{a.tile_kernel, 16 * a.tiles, a.waves, a.splits, a.stream};
   return SD_OK;
 }
@@ -1563,6 +1573,8 @@ int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int 
   if (!kv_q_rows_at(q, ldq, n_heads, hd, dtype) || !kv_q_rows_at(out, ldo, n_heads, hd, dtype) || !kv_q_arrays_ok(pool, rows))
     return SD_EINVAL;
   const int len = max_len ? std::min(max_len, 16 * rows->table_width) : 16 * rows->table_width;
+  const Attn4Plan plan = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, M, n_heads, KV, rows->n_seqs, len);
+  if (!attention_q_grid_ok(plan, KV)) return SD_EINVAL;
   const size_t need = sd_attention_q_workspace_bytes(M, n_heads, KV, hd, rows->n_seqs, len);
   if (need && (!workspace || (uintptr_t)workspace % 16 || workspace_bytes < need)) return SD_EINVAL;
   Attn4Params p{};
@@ -1578,7 +1590,6 @@ int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int 
   p.rows = kv_rows(rows);
   p.causal = causal != 0;
   p.scale = scale;
-  const Attn4Plan plan = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, M, n_heads, KV, rows->n_seqs, len);
   p.part_o = (float*)workspace;
   p.part_ml = p.part_o + (size_t)plan.splits * M * n_heads * hd;
   HIPCHK(launch_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, plan, p, (hipStream_t)stream));

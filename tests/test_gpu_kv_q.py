@@ -253,6 +253,41 @@ def test_norm_rope(M, H, KV, hd, dtype, gains, rotate):
         assert (np.abs(host(g) - want) <= np.abs(want) * (HALF[dtype] + (U32 if dtype == "bf16" else 0)) * 1.0001 + slack + 2.0 ** -149).all()
 
 
+@pytest.mark.parametrize("gains", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_gain_addresses(hd, gains):
+    """A gain is aligned to its entries only: the same result from any of them."""
+    import torch
+    from paper_2510_11331_amd import norm_rope
+    say("gain addresses", hd, gains)
+    r = np.random.default_rng(hd)
+    (q, _), (k, _) = heads(r, 7, 4, hd, "bf16"), heads(r, 7, 2, hd, "bf16")
+    g = t((1 + 0.1 * r.normal(size=hd)).astype(np.float32), gains)
+    want = norm_rope(q, k, q_gain=g, k_gain=g)
+    for at in range(1, 9):
+        room = torch.full((hd + 16,), float("nan"), dtype=g.dtype, device="cuda")
+        room[at:at + hd] = g
+        got = norm_rope(q, k, q_gain=room[at:at + hd], k_gain=room[at:at + hd])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_values_that_are_not_finite():
+    """Without a norm and a rotation a head's entries are what they were; a rotation mixes the two of a pair only."""
+    import torch
+    from paper_2510_11331_amd import norm_rope, rope_table
+    say("not finite")
+    q = torch.arange(128, dtype=torch.float32, device="cuda").repeat(3, 2, 1).contiguous()
+    q[0, 0, 3], q[0, 1, 70], q[1, 0, 127], q[2, 1, 0] = float("inf"), float("-inf"), float("nan"), -0.0
+    got = norm_rope(q, q[:, :1].contiguous())
+    assert torch.equal(torch.isnan(got[0]), torch.isnan(q))
+    assert torch.equal(got[0].nan_to_num(5.0, 6.0, 7.0).view(torch.int32), q.nan_to_num(5.0, 6.0, 7.0).view(torch.int32))
+    got = norm_rope(q, q[:, :1].contiguous(), torch.ones(3, dtype=torch.int32, device="cuda"), rope_table(2, 128))[0]
+    bad = torch.zeros(3, 2, 128, dtype=torch.bool, device="cuda")
+    for row, h, d in ((0, 0, 3), (0, 1, 6), (1, 0, 63)):
+        bad[row, h, d] = bad[row, h, d + 64] = True
+    assert torch.equal(~torch.isfinite(got), bad)
+
+
 def test_rope_table():
     from paper_2510_11331_amd import rope_table
     say("rope table")
@@ -482,6 +517,38 @@ def test_attention_plans(case):
     x = t(q.astype(np.float32), dtype)
     for causal in (True, False):
         close(host(attention_q(x, c.cache(), c.desc, causal)), *c.attention(host(x), causal), dtype)
+
+
+@pytest.mark.parametrize("H,KV", [(1, 1), (4, 1), (5, 1), (10, 2), (12, 1), (32, 1), (40, 1)])
+@pytest.mark.parametrize("seqs,dtype", [(64, "bf16"), (65, "fp32"), (200, "bf16"), (4096, "bf16"), (4097, "fp32"), (9000, "bf16")])
+def test_attention_many_sequences(seqs, dtype, H, KV):
+    """A workgroup finds its sequence among all: rows of 0 to 40 in any order, none for whole runs of them.  One token of
+    each sequence is cached, so that a row's output is that token's value."""
+    from paper_2510_11331_amd import KVRows, KVCacheQ, attention_q, kv_append_q
+    import torch
+    say("sequences", seqs, dtype, H, KV)
+    r = np.random.default_rng([seqs, H])
+    hd = 64
+    rows = r.choice([0, 0, 1, 1, 1, 1, 2, 3, 5, 17, 40][:11 if seqs < 1000 else 10], size=seqs)
+    rows[seqs // 3:seqs // 3 + 30] = 0
+    rows[0], rows[-1] = 1, 2
+    lengths, table = t(np.ones(seqs, dtype=np.int32)), t(np.arange(seqs, dtype=np.int32)[:, None])
+    cache = KVCacheQ(t(np.full((seqs, KV, 17 * hd), 0xff, dtype=np.uint8)))
+    x = t(r.integers(-3, 4, size=(seqs, KV, hd)).astype(np.float32), dtype)
+    kv_append_q(cache, x, x, KVRows(t(np.arange(seqs + 1, dtype=np.int32)), lengths, table))
+    cu = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
+    d = KVRows(t(cu), lengths, table)
+    torch.manual_seed(seqs)
+    q = torch.randn(int(cu[-1]), H, hd, dtype=dt(dtype), device="cuda")
+    want = x[t(np.repeat(np.arange(seqs), rows))].repeat_interleave(H // KV, 1).float()
+    # The values are codes; a weight w over the sum w: w, its sum's reciprocal and the product are each rounded to fp32, in
+    # bf16 w has 16 bits more, and an integer up to 3 off by 2^-15 of itself rounds to itself.
+    slack = want.abs() * (2.0 ** -21 if dtype == "fp32" else 0)
+    assert ((attention_q(q, cache, d, False).float() - want).abs() <= slack).all()
+    last = torch.zeros(len(q), dtype=torch.bool, device="cuda")
+    last[t(cu[1:][rows > 0].astype(np.int64)) - 1] = True
+    want *= last[:, None, None]                          # causal: each sequence's last row sees its token, the others nothing
+    assert ((attention_q(q, cache, d).float() - want).abs() <= slack).all()
 
 
 @pytest.mark.parametrize("hd", [64, 128])

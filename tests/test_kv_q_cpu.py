@@ -98,6 +98,12 @@ def test_calls_refuse():
     at = dict(pool="pool", rows="rows", M=5, H=4, dtype=BF, q=A, ldq=256, out=A, ldo=256, causal=1, scale=0.125, max_len=48, ws=A, n=n)
     check(L.sd_attention_q, at, [dict(M=-1), dict(M=big), dict(H=0), dict(H=6), dict(dtype=2), dict(max_len=-1), *heads("q", "ldq"),
                                  *heads("out", "ldo")], [dict(M=0, q=None)])
+    # grids that no launch has
+    wide, M = dict(pool, n_kv_heads=1024), 1 << 20
+    for f, a in ((L.sd_kv_append_q, ap), (L.sd_kv_read_q, ap), (L.sd_norm_rope_append_q, {**both, "H": 1024}), (L.sd_attention_q, {**at, "H": 1024})):
+        assert call(f, {k: 65536 if k[:2] == "ld" else v for k, v in {**a, "M": M}.items()}, p=wide, r=dict(rows, n_seqs=M)) == E, f.__name__
+    assert call(L.sd_norm_rope, {**nr, "M": M, "H": 1024, "KV": 1024, **dict.fromkeys(("ldq", "ldk", "ldqo", "ldko"), 65536)}) == E
+    assert L.sd_plan_attention_q(M, 1024, 1024, 64, M, 16, BF, C.byref(_lib.AttentionQPlan())) == E
     assert L.sd_rope_table(0, 64, 1e4, None, None) == OK
     for bad in ((-1, 64, 1e4, A), (4, 32, 1e4, A), (4, 64, 0.0, A), (4, 64, float("nan"), A), (4, 64, 1e4, None), (4, 64, 1e4, A + 8),
                 ((1 << 24) + 1, 64, 1e4, A)):
@@ -169,6 +175,8 @@ def test_plans():
             for B in (1, 2, 7, 16, 33, 64, 200):
                 for n in (1, 2, 5, 17, 100, 700, 2048):
                     for H, KV in ((1, 1), (8, 1), (40, 5), (32, 8), (32, 32), (64, 8), (128, 128), (640, 64)):
+                        if B * n * H > 1 << 27:                   # (past a grid's threads)
+                            continue
                         for length in (16, 500, 1500, 1600, 3000, 9000, 33000, 400000):
                             k = kvplans.kind(kvplans.plan(B * n, H, KV, hd, dtype, B, length), hd, dtype)
                             for part, have in zip(parts(k), (first, second)):
