@@ -10,10 +10,14 @@
 // S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_16x16x32_bf16.  A code times its
 // scale is a bf16 number (two significant bits; scales of 2^-126 to 2^126), so
 // v_cvt_scalef32_pk_bf16_fp4 loses nothing, and neither do the products with
-// bf16 queries.  fp32 queries enter as three bf16 parts (24 bits), weights as two
-// for bf16 outputs (16 bits or more: an error of a quarter of a percent of the output's own
-// rounding) and as three for fp32 ones.  Scores, the running maximum, the
-// weights' sum and the output are fp32.
+// bf16 queries.  fp32 queries enter as three bf16 parts (all 24 bits).  Weights
+// enter as two for bf16 outputs, off by at most 2^-15 of themselves where the
+// output's own rounding is 2^-8, and as three (exact) for fp32 ones.  Scores, the
+// running maximum, the weights' sum and the output are fp32.
+//
+// Why matrix instructions for one row of keys: 16 query vectors cost as much as
+// one, and there the conversion of the codes, which everything needs, is the
+// larger part; the vector unit's own products would add to it.
 //
 // A wave takes 32 keys (two pages) at a time.  Lane (r, g) = (lane % 16, lane /
 // 16) loads key r's dimensions (hd / 4) g .. as they lie in the page: they are
@@ -30,6 +34,20 @@
 // The running maximum moves only when a score passes it by 2^8: the weights stay
 // far inside fp32, and the usual step needs neither a reduction over lanes nor
 // a rescaling of the output.
+//
+// Measured (a call in a replayed graph; the plain read rate of this memory is 6.8
+// TB/s, a large bf16 product runs at 1.17 PFLOP/s):
+//   64 sequences of 8192 keys, a row of 32 heads on 8, hd 128, bf16: 95 us, 6.0 TB/s
+//   8 sequences of 1044 keys, 5 rows of 32 heads on 32, bf16: 11.2 us, 3.3 TB/s
+//   32 ragged ones up to 2176 keys, 5 rows of 32 heads on 32, fp32: 33.9 us
+//   1 of 32763 keys, 5 rows of 32 heads on 8, bf16: 21.4 us (16.4 and the join 5)
+//   1 of 520 keys, a row of 32 heads on 8, hd 64: 6.2 us
+//   2048 rows on 4095 keys, 32 heads on 32, bf16: 110 us, 0.94 PFLOP/s
+// Short calls are bound by the chain of latencies (the sequence, its page ids,
+// the pages, the waves' join): 5 us whatever their size.  fp32 ones by the matrix
+// unit: three parts of queries and of weights.  Decoding at length by memory.
+// Prefill by the issue of instructions, which matrix and vector instructions of a
+// SIMD share.
 #include "codes4.h"
 
 #include <float.h>
@@ -495,9 +513,8 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
   for (; left > 0; --left, key0 += stride) step.template operator()<true>();
 }
 
-
 // waves that a SIMD is to hold at once, for which the compiler keeps to so many registers
-template <typename T, int QT> constexpr int MIN_WAVES = QT == 1 ? (sizeof(T) == 2 ? 4 : 3) : QT == 2 ? 2 : 1;
+template <typename T, int QT> constexpr int MIN_WAVES = QT == 2 ? 2 : sizeof(T) == 2 ? 4 : 3;
 
 template <typename T, int HD, int QT, int WAVES, bool NT>
 __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_stream_kernel(Attn4Params p) {
@@ -591,13 +608,21 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
   }
 }
 
-// Prefill: 64 QT vectors a workgroup, 16 QT a wave, and the keys in LDS: each wave converts a quarter of a step's 32 keys
-// for all four, while they take the step before it.
+// Prefill: 128 vectors a workgroup, 32 a wave, and the keys in LDS: each wave converts a quarter of a step's 32 keys for all
+// four, while they take the step before it.  Without sharing, a wave's conversions cost as much as its products: 2048 rows
+// on 4095 keys of 32 heads take 157 us that way and 110 us this way.
 //
-// bf16 outputs: the values are held as fp16, which their codes times scales of 2^-23 to 2^8 are exactly, so that a weight
-// is one fp16 part (off by 2^-12 of itself, an eighth of the output's own rounding) and half the products of the second
-// matrix are saved.  A workgroup that meets a value outside that range (or NaN) takes the rest of its keys as above.  fp32 outputs: values in
-// bf16 and three parts.
+// bf16 only.  The values are held as fp16, which their codes times scales of 2^-23 to 2^8 are exactly, so that a weight is
+// one fp16 part (off by 2^-12 of itself where the output's own rounding is 2^-8) and half the products of the second matrix
+// are saved.  A workgroup that meets a value outside that range, NaN or a missing page leaves the loop and takes the rest of
+// its keys as above.  (fp32 vectors would need three parts of either operand here too: 63 to 74 us against 49 for 3
+// sequences of 600 rows.)
+//
+// Counters: of the SIMDs' cycles the products take 40 % and vector instructions 48 %, and while one is issued the other is
+// not.  Taken out of the loop one at a time (of 133 us, at an earlier step), the conversions are worth 24, the maximum test 9,
+// the exponentials 8, the barrier 8.  The rare paths lie outside the loop because their code there kept the accumulators from
+// staying in place.  Tried and worse: waves' priorities raised around the products (146), eight waves of 16 vectors, two
+// waves of 64 (registers spill).
 template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kernel(Attn4Params p) {
   using T = bf16_t;
   using P = Page4<HD>;
@@ -818,7 +843,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
 }
 
 // Joins the ranges of a vector in their order: hd / 4 lanes of four dimensions for each of PARTS runs of 8 ranges, then
-// the runs.  No load waits for another.
+// the runs.  No load waits for another, so that it is a launch and one round of latency: 5 us for 160 vectors of 32 ranges.
 template <typename T, int HD, int PARTS> __global__ __launch_bounds__(256) void attention4_join_kernel(Attn4Params p) {
   constexpr int LANES = HD / 4, EACH = 256 / (LANES * PARTS);       // vectors of a workgroup
   __shared__ __attribute__((aligned(16))) float s_o[PARTS > 1 ? 256 : 1][4];
@@ -877,6 +902,7 @@ template <typename T, int HD, int PARTS> __global__ __launch_bounds__(256) void 
   store4((T*)p.out + (size_t)row * p.ldo + h * HD + d, O);
 }
 
+// Every rule with what was measured on both sides of it (us, in a replayed graph; hd 128 and bf16 unless said).
 Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, int max_len) {
   Attn4Plan a{};
   const int64_t G = H / KV, nz = std::min(n_seqs, M);
@@ -889,18 +915,37 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   };
   auto typical = [&](int64_t cap) { return nz * ((vectors + cap - 1) / cap) * KV; };    // ... of alike sequences, and heads
   const int64_t steps = (max_len + 31) / 32;
+
+  // Keys shared in LDS pay where a workgroup's 128 vectors are there and every CU has one: 2048 rows of 32 heads on 32,
+  // 4095 keys, 111 shared and 157 not; 512 rows of 4 vectors each, 8192 keys, 99 and 100; 128 rows, 30 and 16.
   a.tile_kernel = dtype == 0 && vectors >= 128 && typical(128) >= 256;
+  // Two tiles read and convert the keys once for 32 vectors, and leave half the workgroups: 32 sequences of 20 vectors and
+  // 4000 keys, 40 with two tiles and 44 with one; 8 of 8192 keys, 25.7 and 26.5; but 4 of 8192 keys, 25.1 and 20.4; 32 of
+  // 1000 keys on average, hd 64, 15.5 and 12.5.
   a.tiles = a.tile_kernel ? 8 : vectors > 16 && dtype == 0 && typical(16) * steps >= 28 * 1024 ? 2 : 1;
   a.blocks = (int)blocks(16 * a.tiles);
   const int64_t items = typical(16 * a.tiles);
+  // Eight waves shorten a workgroup's loop over its keys, four leave less to join and more workgroups to a CU.  256
+  // workgroups of 1044 keys: 12.1 with eight and 13.2 with four; 2560 of 1024 keys 76 and 82; 2560 of 600 keys 58.6 and 55.3;
+  // fp32, whose waves need a third of a SIMD's registers, 1024 of 1100 keys 42.8 and 34.7.
   a.waves = a.tile_kernel || a.tiles == 2 || (dtype == 1 && hd == 128 && items >= 512) || (items >= 1024 && steps < 24) ? 4 : 8;
+  // Ranges of keys fill the card where there are few workgroups; the join's launch costs 4 to 5.  8 workgroups: of 4000 keys
+  // 12.0 with 16 ranges and 20 with one, of 2000 keys 11.1 with 7 and 11.7 to 12.5 with one, of 32768 keys 16.7 with 64 and 17.2
+  // with 32; of 131072 keys 36 and 44.  128 workgroups of 4096 keys 18.1 with two ranges and 22.1 with one, of two tiles and
+  // 8192 keys 40.2 with four and 66.2 with one; but 160 of 4096 keys 25.7 and 23.8, 256 of 8192 keys 57.2 and 54.6.  A little
+  // over one workgroup to a CU leaves most CUs idle for the last: 288 of 16384 keys 124 and 140, 384 of 8192 keys 83 and 86
+  // (320 of 4096 keys 44.5 and 44.3).
   a.splits = 1;
   if (items <= 64 && max_len >= 1536) {
     a.waves = 4;
     a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / items, max_len / 256, 64}));
   } else if (items <= 128 && max_len >= 2560) {
     a.splits = a.waves == 8 ? 2 : 4;
+  } else if (a.waves == 8 && items > 256 && items <= 384 && max_len >= 8192) {
+    a.splits = 2;
   }
+  // Pages that one workgroup reads once, of a cache that does not fit the last-level cache (256 MiB) twice over, are loaded
+  // past it: 64 sequences of 8192 keys 99.7 and 108.9 without; what does fit loses by it (36 MB: 14.1 and 12.8).
   a.stream = !a.tile_kernel && vectors <= 16 * a.tiles && (double)nz * max_len * KV * 17 * hd / 16 > 536870912.0;
   return a;
 }

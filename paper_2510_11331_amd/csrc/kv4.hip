@@ -7,13 +7,27 @@
 //   (y_i, y_{i + hd/2}) -> (y_i c - y_{i + hd/2} s, y_{i + hd/2} c + y_i s)
 //
 // Everything is bound by memory (a value is read once and written once; about
-// seven operations on it).  hd / 16 lanes take a head, a lane the 8 entries
-// from 8 i and the 8 from hd / 2 + 8 i: the two entries that a rotation mixes
-// are in one lane, a scale's block of 32 in four neighbouring ones, and every
-// access to a row is of 16 bytes.  The norm and the rotation are in 64 bits,
-// which the vector unit does at the rate of 32: a code is then a function of
-// the input alone, not of an order of sums.  What is stored is rounded to fp32
-// and from there to its type or its code; the first step is off by 2^-24.
+// seven operations on it), or in small calls by its latency.  hd / 16 lanes
+// take a head, a lane 8 entries of either half of it, from 8 i and from hd / 2 +
+// 8 i: the two entries that a rotation mixes are in one lane, a scale's block
+// of 32 in four neighbouring ones, and every access to a row is of 16 bytes.
+// Where nothing is quantised, fp32 heads are taken as two groups of four a half,
+// hd / 4 apart, so that neighbouring lanes' 16 bytes are neighbours in memory
+// (2048 rows of 80 heads of 128: 41.7 -> 37.8 us).
+//
+// The norm and the rotation are in 64 bits, which the vector unit does at the
+// rate of 32: a result is then a function of the input, whatever the order of a
+// sum (but for one in about 2^28).  What is stored is rounded to fp32, off by
+// 2^-24, and from there to its type or its code.
+//
+// Measured (times of a call in a replayed graph): norms and rotation of 2048
+// fp32 rows of 80 heads of 128, 168 MB, 37.8 us, 4.5 TB/s (a copy of 1 GiB runs at
+// 5.1); of one bf16 row of 40 heads of 64, 3.2 us, a launch and two rounds of
+// memory latency.  40 bf16 rows of 96 heads of 128 (32 of them queries, returned)
+// into the cache and the same rows back, 8.3 us; 2048 fp32 rows of 16 heads of
+// 128 into the cache and back, 38 MB in 14.3 us, of which the two launches are
+// half.  Up to 4096 cached positions of each of 8 sequences, 8 heads of 128, into
+// bf16: 83 MB in 19.9 us, 4.2 TB/s.
 #include "codes4.h"
 
 namespace sd {
@@ -21,13 +35,14 @@ namespace sd {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+// 8 entries of a row; of fp32, two groups of four that lie APART entries apart
+template <typename T, int APART = 4> __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   if constexpr (sizeof(T) == 2) {
     const u32x4 u = *(const u32x4*)p;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
   } else {
-    const u32x4 u = ((const u32x4*)p)[0], w = ((const u32x4*)p)[1];
+    const u32x4 u = *(const u32x4*)p, w = *(const u32x4*)(p + APART);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       x[e] = __uint_as_float(u[e]);
@@ -35,29 +50,29 @@ template <typename T> __device__ __forceinline__ void load8(const T* p, float (&
     }
   }
 }
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+template <typename T, int APART = 4> __device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
   if constexpr (sizeof(T) == 2) {
     u32x4 u;
 #pragma unroll
     for (int e = 0; e < 4; ++e) u[e] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x[2 * e], (__bf16)x[2 * e + 1]});
     *(u32x4*)p = u;
   } else {
-    ((u32x4*)p)[0] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
-    ((u32x4*)p)[1] = u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
+    *(u32x4*)p = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+    *(u32x4*)(p + APART) = u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
   }
 }
 
-// 8 entries of a gain, which is aligned to its entries only (wide loads of any address are within the memory unit's rules)
-__device__ __forceinline__ void gain8(const void* g, int bf16, int i, float (&x)[8]) {
-  typedef uint16_t halves8 __attribute__((ext_vector_type(8), aligned(2)));
+// 8 entries of a gain in the same two groups; it is aligned to its entries only (the memory unit takes wide loads of any
+// address)
+template <int APART> __device__ __forceinline__ void gain8(const void* g, int bf16, int i, float (&x)[8]) {
+  typedef uint16_t halves4 __attribute__((ext_vector_type(4), aligned(2)));
   typedef float floats4 __attribute__((ext_vector_type(4), aligned(4)));
   if (bf16) {
-    const halves8 a = *(const halves8*)((const bf16_t*)g + i);
+    const halves4 a = *(const halves4*)((const bf16_t*)g + i), b = *(const halves4*)((const bf16_t*)g + i + APART);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = bf2f(a[e]);
+    for (int e = 0; e < 4; ++e) x[e] = bf2f(a[e]), x[4 + e] = bf2f(b[e]);
   } else {
-    const floats4* const f = (const floats4*)((const float*)g + i);
-    const floats4 a = f[0], b = f[1];
+    const floats4 a = *(const floats4*)((const float*)g + i), b = *(const floats4*)((const float*)g + i + APART);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
   }
@@ -74,9 +89,11 @@ __device__ __forceinline__ double rsqrt64(double x) {
 template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) void kv4_kernel(Kv4Params p) {
   using P = Page4<HD>;
   constexpr int LANES = HD / 16;
+  constexpr bool WIDE = MODE == KV4_HEADS && sizeof(T) == 4;
+  constexpr int APART = WIDE ? HD / 4 : 4;
   const int per_row = (MODE == KV4_HEADS || MODE == KV4_BOTH ? p.H : 0) + (MODE == KV4_HEADS ? 1 : 2) * p.KV;
   const int64_t item = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  const int i = threadIdx.x % LANES;
+  const int i = threadIdx.x % LANES, i8 = WIDE ? 4 * i : 8 * i;
   __shared__ Places s_places;
   if constexpr (MODE != KV4_HEADS) {
     s_places.load(p.rows);
@@ -94,7 +111,7 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
                          : what == 1 ? (const T*)p.k + (size_t)row * p.ldk
                                      : (const T*)p.v + (size_t)row * p.ldv;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) load8(src + h * HD + half * (HD / 2) + 8 * i, x[half]);
+    for (int half = 0; half < 2; ++half) load8<T, APART>(src + h * HD + half * (HD / 2) + i8, x[half]);
   }
 
   int b = 0, pos = 0, page = -1;
@@ -137,15 +154,15 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
     const void* const gain = what == 0 ? p.q_gain : p.k_gain;
     float g[2][8];
     if (gain) {
-      gain8(gain, p.gain_bf16, 8 * i, g[0]);
-      gain8(gain, p.gain_bf16, HD / 2 + 8 * i, g[1]);
+      gain8<APART>(gain, p.gain_bf16, i8, g[0]);
+      gain8<APART>(gain, p.gain_bf16, HD / 2 + i8, g[1]);
     }
     float4 w[4] = {};
     if (p.rope) {
       const bool in = (unsigned)pos < (unsigned)p.n_pos;
-      const float4* const cs = (const float4*)(p.rope + ((size_t)(in ? pos : 0) * (HD / 2) + 8 * i) * 2);
+      const float4* const cs = (const float4*)(p.rope + ((size_t)(in ? pos : 0) * (HD / 2) + i8) * 2);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = in ? cs[e] : make_float4(NAN, NAN, NAN, NAN);
+      for (int e = 0; e < 4; ++e) w[e] = in ? cs[e < 2 ? e : e - 2 + APART / 2] : make_float4(NAN, NAN, NAN, NAN);
     }
     double r = 1.0;
     if (gain) {
@@ -173,7 +190,7 @@ template <typename T, int HD, Kv4Mode MODE> __global__ __launch_bounds__(256) vo
     if (MODE == KV4_HEADS || what == 0) {
       T* const out = what == 0 ? (T*)p.q_out + (size_t)row * p.ldqo : (T*)p.k_out + (size_t)row * p.ldko;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) store8(out + h * HD + half * (HD / 2) + 8 * i, x[half]);
+      for (int half = 0; half < 2; ++half) store8<T, APART>(out + h * HD + half * (HD / 2) + i8, x[half]);
     }
   }
   if (MODE == KV4_HEADS || what == 0) return;
