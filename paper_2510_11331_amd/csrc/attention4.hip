@@ -39,7 +39,7 @@
 // TB/s, a large bf16 product runs at 1.17 PFLOP/s):
 //   64 sequences of 8192 keys, a row of 32 heads on 8, hd 128, bf16: 95 us, 6.0 TB/s
 //   8 sequences of 1044 keys, 5 rows of 32 heads on 32, bf16: 11.2 us, 3.3 TB/s
-//   32 ragged ones up to 2176 keys, 5 rows of 32 heads on 32, fp32: 33.9 us
+//   32 ragged ones up to 2176 keys, 5 rows of 32 heads on 32, fp32: 29.2 us
 //   1 of 32763 keys, 5 rows of 32 heads on 8, bf16: 21.4 us (16.4 and the join 5)
 //   1 of 520 keys, a row of 32 heads on 8, hd 64: 6.2 us
 //   2048 rows on 4095 keys, 32 heads on 32, bf16: 110 us, 0.94 PFLOP/s
@@ -125,10 +125,11 @@ template <int PARTS> __device__ __forceinline__ void parts8(const float (&x)[8],
 
 // The vectors of workgroup `block`: sequence b, its first row, its rows n and the first of its vectors.
 struct Block4 { int b, row0, n, v0, len; };
-// Up to 64 sequences: sequence b has ceil(n G / cap) workgroups, which every wave adds up by itself.
+// Up to 64 sequences: sequence b has ceil(n G / cap) workgroups, which every wave adds up by itself, in the order of the
+// sequences or, sorted, the longest first.
 // More (a sum of all of them in each workgroup would cost as much as the attention does: 64 keys of 512 sequences 32 us,
-// of 4096 sequences 786 us): with u = gcd(G, cap) and C = cap / u, sequence b's workgroups are those from S(b) = floor((cu[b] G /
-// u + (C - 1) b) / C) on.  S(b + 1) - S(b) >= floor((n G / u - 1) / C) + 1 = ceil(n G / cap) for n >= 1, so they suffice; the
+// of 4096 sequences 786 us; so 25 and 198): with u = gcd(G, cap) and C = cap / u, sequence b's workgroups are those from S(b) =
+// floor((cu[b] G / u + (C - 1) b) / C) on.  S(b + 1) - S(b) >= floor((n G / u - 1) / C) + 1 = ceil(n G / cap) for n >= 1, so they suffice; the
 // few between its last and S(b + 1) have nothing to do.  A wave looks at 64 values of S at a time.
 constexpr int SUMMED = 64;
 __host__ __device__ constexpr int common4(int a, int b) {
@@ -139,14 +140,29 @@ __host__ __device__ constexpr int common4(int a, int b) {
   }
   return a;
 }
-__device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int cap, int block, Block4& o) {
+__device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int cap, int block, bool sorted, Block4& o) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, hi = 0, len = 0, at, before;       // a lane's sequence; the lane that has the workgroup's, and its workgroups before this
+  int lo = 0, hi = 0, len = 0;                   // of a lane's sequence
+  int at, before;                                // the lane that has the workgroup's, and that one's workgroups before this
   if (s.B <= SUMMED) {
     if (lane < s.B) {
       lo = min(max(s.cu[lane], 0), M);
       hi = min(max(s.cu[lane + 1], lo), M);
       len = s.len[lane];                         // (of all of them: not a second round of latency)
+    }
+    int b = lane;
+    if (sorted) {
+      const int keys = min(max(len, 0), 1 << 24), near = __builtin_amdgcn_readfirstlane(keys);
+      if (__any(lane < s.B && abs(keys - near) > near / 4)) {         // lane k takes the sequence that k longer ones go before
+        const int key = lane < s.B ? keys * 64 + 63 - lane : -1 - lane;
+        int rank = 0;
+#pragma unroll 16
+        for (int j = 0; j < 64; ++j) rank += __builtin_amdgcn_readlane(key, j) > key;
+        lo = __builtin_amdgcn_ds_permute(4 * rank, lo);
+        hi = __builtin_amdgcn_ds_permute(4 * rank, hi);
+        len = __builtin_amdgcn_ds_permute(4 * rank, len);
+        b = __builtin_amdgcn_ds_permute(4 * rank, lane);
+      }
     }
     const int mine = ((hi - lo) * G + cap - 1) / cap;
     int sum = mine;
@@ -159,7 +175,7 @@ __device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int ca
     if (!past) return false;
     at = __builtin_ctzll(past);
     before = block - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at));
-    o.b = at;
+    o.b = __builtin_amdgcn_readlane(b, at);
   } else {
     const int u = common4(cap, G), C = cap / u;
     int b0 = 0, b1 = s.B, step, start;           // S(b0) <= block < S(b1), where the workgroup is any sequence's
@@ -531,7 +547,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
   const int guess = min(block, p.rows.B - 1), guess_page = 2 * wave + 2 * WAVES * (lane / 2) + (lane & 1);
   const int guess_id = p.splits == 1 && guess_page < p.rows.W ? p.rows.table[(size_t)guess * p.rows.W + guess_page] : -1;
   Block4 w;
-  if (!find_block(p.rows, p.M, G, 16 * QT, block, w)) return;
+  if (!find_block(p.rows, p.M, G, 16 * QT, block, p.sorted, w)) return;
   const int len = w.len;
   const int nv = min(16 * QT, w.n * G - w.v0);   // vectors of this workgroup
   const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
@@ -639,7 +655,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
   // the rows that see most go first; where all workgroups run at once, two to a CU, a long one meets a short one there
   const int block = order >= part && (int64_t)p.blocks * p.KV <= 512 ? order - part : p.blocks - 1 - order;
   Block4 w;
-  if (!find_block(p.rows, p.M, G, 64 * QT, block, w)) return;
+  if (!find_block(p.rows, p.M, G, 64 * QT, block, false, w)) return;
   const int len = w.len;
   const int nv = min(64 * QT, w.n * G - w.v0);
   const int n_max = loop_keys(p, max(0, sees(p, len, w.n, w.v0 + nv - 1, G)));
@@ -946,6 +962,12 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   }
   // Pages that one workgroup reads once, of a cache that does not fit the last-level cache (256 MiB) twice over, are loaded
   // past it: 64 sequences of 8192 keys 99.7 and 108.9 without; what does fit loses by it (36 MB: 14.1 and 12.8).
+  // Where a workgroup's keys take long and not all workgroups run at once, the longest sequences go first, if some is over a
+  // quarter longer or shorter than the first (finding the order costs each of them about 0.5): up to 8192 keys, lengths
+  // evenly spread, 64 sequences on 8 heads 57.3 and 62.3 as they come; up to 4096 keys 36.0 and 39.9, 48 of them 30.5 and 36.7;
+  // fp32, 32 of 5 rows on 32 heads, up to 2176 keys 50.8 and 53.4; alike ones 91.4 and 90.9, 56.0 and 55.0.  Up to 1024 keys, 64
+  // sequences on 32 heads: 48.4 and 45.4.
+  a.sorted = !a.tile_kernel && n_seqs > 1 && n_seqs <= SUMMED && items > 256 && steps * (dtype == 1 ? 2 : 1) >= 128;
   a.stream = !a.tile_kernel && vectors <= 16 * a.tiles && (double)nz * max_len * KV * 17 * hd / 16 > 536870912.0;
   return a;
 }
@@ -963,6 +985,7 @@ template <typename T, int HD, int QT, int WAVES> static void launch_stream(const
 template <typename T, int HD> static void launch_hd(const Attn4Plan& a, Attn4Params p, hipStream_t s) {
   p.blocks = a.blocks;
   p.splits = a.splits;
+  p.sorted = a.sorted;
   if constexpr (sizeof(T) == 2) {
     if (a.tile_kernel) {
       attention4_tile_kernel<HD><<<dim3((unsigned)a.blocks * p.KV), 256, 0, s>>>(p);

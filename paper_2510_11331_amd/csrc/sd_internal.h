@@ -334,13 +334,15 @@ struct Attn4Params {
   KvRows rows;
   int causal;
   float scale;
+  bool sorted;             // longest sequences first
   int blocks, splits;      // workgroups of vectors at most, ranges of the keys
   float* part_o;           // their outputs [splits, M, H, hd] and (maximum, sum) (more than one)
   float* part_ml;
 };
 // How it runs: tiles of 16 query vectors and waves of a workgroup, workgroups of such vectors at most, ranges of the keys;
-// tile_kernel: keys shared in LDS; stream: loads that leave the caches to others
-struct Attn4Plan { int tiles, waves, blocks, splits; bool tile_kernel, stream; };
+// tile_kernel: keys shared in LDS; stream: loads that leave the caches to others; sorted: longest sequences
+// first
+struct Attn4Plan { int tiles, waves, blocks, splits; bool tile_kernel, stream, sorted; };
 Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, int max_len);
 size_t attention4_part_floats(const Attn4Plan& a, int M, int H, int hd);
 

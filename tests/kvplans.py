@@ -22,6 +22,9 @@ CASES = [
     ("two key ranges", [1] * 16, [2 * n for n in FEW], 32, 8, 128, "bf16", 170, (0, 16, 8, 2, 0)),
     ("two key ranges, fp32", [2] * 16, [2 * n for n in FEW], 32, 8, 128, "fp32", 170, (0, 16, 8, 2, 0)),
     ("two key ranges, a little over a workgroup to a CU", [1] * 36, (FEW * 3)[:36], 32, 8, 128, "bf16", 520, (0, 16, 8, 2, 0)),
+    ("longest first", [1] * 40, [1, 0] + (FEW * 3)[:38], 32, 8, 128, "bf16", 300, (0, 16, 8, 1, 0)),
+    ("longest first, workgroups of a sequence apart", [3, 17, 0, 9] * 16, [n + 16 for n in FEW] * 4, 24, 3, 64, "bf16", 300, (0, 32, 4, 1, 0)),
+    ("longest first, fp32", [1, 5] * 32, [n + 4 for n in FEW[::-1]] * 4, 16, 8, 128, "fp32", 140, (0, 16, 4, 1, 0)),
     ("streamed", [1] * 32, (FEW * 2)[:32], 32, 8, 128, "bf16", 1100, (0, 16, 8, 1, 1)),
     ("streamed, 64 dimensions", [1] * 32, (FEW * 2)[:32], 16, 16, 64, "bf16", 1100, (0, 16, 8, 1, 1)),
     ("streamed, two tiles", [4] * 32, [n + 3 for n in FEW] * 2, 40, 8, 128, "bf16", 1100, (0, 32, 4, 1, 1)),
