@@ -13,7 +13,7 @@
 // of 32 in four neighbouring ones, and every access to a row is of 16 bytes.
 // Where nothing is quantised, fp32 heads are taken as two groups of four a half,
 // hd / 4 apart, so that neighbouring lanes' 16 bytes are neighbours in memory
-// (2048 rows of 80 heads of 128: 41.7 -> 37.8 us).
+// (2048 rows of 80 heads of 128: 41.7 -> 37.5 us).
 //
 // The norm and the rotation are in 64 bits, which the vector unit does at the
 // rate of 32: a result is then a function of the input, whatever the order of a
@@ -21,7 +21,7 @@
 // 2^-24, and from there to its type or its code.
 //
 // Measured (times of a call in a replayed graph): norms and rotation of 2048
-// fp32 rows of 80 heads of 128, 168 MB, 37.8 us, 4.5 TB/s (a copy of 1 GiB runs at
+// fp32 rows of 80 heads of 128, 168 MB, 37.5 us, 4.5 TB/s (a copy of 1 GiB runs at
 // 5.1); of one bf16 row of 40 heads of 64, 3.2 us, a launch and two rounds of
 // memory latency.  40 bf16 rows of 96 heads of 128 (32 of them queries, returned)
 // into the cache and the same rows back, 8.3 us; 2048 fp32 rows of 16 heads of
