@@ -129,8 +129,9 @@ struct Block4 { int b, row0, n, v0, len; };
 // sequences or, sorted, the longest first.
 // More (a sum of all of them in each workgroup would cost as much as the attention does: 64 keys of 512 sequences 32 us,
 // of 4096 sequences 786 us; so 25 and 198): with u = gcd(G, cap) and C = cap / u, sequence b's workgroups are those from S(b) =
-// floor((cu[b] G / u + (C - 1) b) / C) on.  S(b + 1) - S(b) >= floor((n G / u - 1) / C) + 1 = ceil(n G / cap) for n >= 1, so they suffice; the
-// few between its last and S(b + 1) have nothing to do.  A wave looks at 64 values of S at a time.
+// floor((cu[b] G / u + (C - 1) min(b, cu[b])) / C) on.  Where n >= 1 the minimum grows by at least one, so that S(b + 1) - S(b) >=
+// floor((n G / u - 1) / C) + 1 = ceil(n G / cap): they suffice, the few between its last and S(b + 1) have nothing to do, and
+// sequences without rows cost none but those.  A wave looks at 64 values of S at a time.
 constexpr int SUMMED = 64;
 __host__ __device__ constexpr int common4(int a, int b) {
   while (b) {
@@ -187,7 +188,7 @@ __device__ __forceinline__ bool find_block(const KvRows& s, int M, int G, int ca
         lo = min(max(s.cu[b], 0), M);
         hi = min(max(s.cu[b + 1], lo), M);
         len = s.len[b];
-        start = (int)(((int64_t)lo * (G / u) + (int64_t)(C - 1) * b) / C);
+        start = (int)(((int64_t)lo * (G / u) + (int64_t)(C - 1) * min(b, lo)) / C);
       }
       const uint64_t past = __ballot(start > block);
       at = past ? __builtin_ctzll(past) - 1 : 63;
@@ -927,7 +928,7 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   auto blocks = [&](int64_t cap) {
     if (n_seqs <= SUMMED) return (M * G - nz) / cap + nz;
     const int64_t u = common4((int)cap, (int)G), C = cap / u;
-    return (M * (G / u) + (C - 1) * n_seqs) / C;
+    return (M * (G / u) + (C - 1) * nz) / C;
   };
   auto typical = [&](int64_t cap) { return nz * ((vectors + cap - 1) / cap) * KV; };    // ... of alike sequences, and heads
   const int64_t steps = (max_len + 31) / 32;

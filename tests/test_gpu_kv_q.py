@@ -58,7 +58,9 @@ class Case:
     def fill(self, r, sizes=1.0):
         """All positions get keys and values."""
         for b, n in enumerate(self.lengths):
-            p = np.arange(max(n, 0))
+            if n <= 0:
+                continue
+            p = np.arange(n)
             x = r.normal(size=(2, len(p), self.KV, self.hd)).astype(np.float32) * sizes
             self.pool.put(*self.at(b, p), x[0], x[1])
 
@@ -71,6 +73,8 @@ class Case:
         out, err = np.zeros(q.shape), np.zeros((2, *q.shape))
         scale = self.hd ** -0.5 if scale is None else scale
         for b, (n, m) in enumerate(zip(self.rows, self.lengths)):
+            if not n:
+                continue
             m = max(m, 0)
             k, v = self.pool.get(*self.at(b, np.arange(m)))
             s = slice(self.cu[b], self.cu[b] + n)
@@ -549,6 +553,27 @@ def test_attention_many_sequences(seqs, dtype, H, KV):
     last[t(cu[1:][rows > 0].astype(np.int64)) - 1] = True
     want *= last[:, None, None]                          # causal: each sequence's last row sees its token, the others nothing
     assert ((attention_q(q, cache, d).float() - want).abs() <= slack).all()
+
+
+@pytest.mark.parametrize("seqs", [65, 300, 4500])
+@pytest.mark.parametrize("rows", [[1], [1, 3], [5, 1, 20, 2, 2], [70, 1]])
+@pytest.mark.parametrize("H,KV", [(4, 1), (5, 1), (16, 2), (64, 2)])
+def test_attention_few_of_many_sequences(seqs, rows, H, KV):
+    """Slots of which most have no rows, at either end and in any order; their keys are split into ranges."""
+    from paper_2510_11331_amd import attention_q
+    say("few of", seqs, rows, H, KV)
+    r = np.random.default_rng([seqs, H, len(rows)])
+    for where in ("first", "last", "any"):
+        at = {"first": np.arange(len(rows)), "last": seqs - 1 - np.arange(len(rows))[::-1],
+              "any": np.sort(r.choice(seqs, size=len(rows), replace=False))}[where]
+        n, m = np.zeros(seqs, dtype=int), np.zeros(seqs, dtype=int)
+        n[at] = rows
+        m[at] = r.integers(100, 700, size=len(rows))
+        m[r.integers(0, seqs, size=3)] += 16
+        c = Case(r, n.tolist(), m.tolist(), KV, 64, width=400)
+        c.fill(r)
+        q, q64 = heads(r, c.M, H, 64, "bf16")
+        close(host(attention_q(q, c.cache(), c.desc)), *c.attention(q64), "bf16")
 
 
 @pytest.mark.parametrize("hd", [64, 128])
