@@ -934,7 +934,8 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   const int64_t steps = (max_len + 31) / 32;
 
   // Keys shared in LDS pay where a workgroup's 128 vectors are there and every CU has one: 2048 rows of 32 heads on 32,
-  // 4095 keys, 111 shared and 157 not; 512 rows of 4 vectors each, 8192 keys, 99 and 100; 128 rows, 30 and 16.
+  // 4095 keys, 111 shared and 157 not; 512 rows of 4 vectors each, 8192 keys, 99 and 100; 128 rows, 30 and 16; with 128 such
+  // workgroups (2 sequences of 974 rows, 8 heads on 4, 1156 keys) 47.5 and 22.2.
   a.tile_kernel = dtype == 0 && vectors >= 128 && typical(128) >= 256;
   // Two tiles read and convert the keys once for 32 vectors, and leave half the workgroups: 32 sequences of 20 vectors and
   // 4000 keys, 40 with two tiles and 44 with one; 8 of 8192 keys, 25.7 and 26.5; but 4 of 8192 keys, 25.1 and 20.4; 32 of
@@ -942,10 +943,15 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
   a.tiles = a.tile_kernel ? 8 : vectors > 16 && dtype == 0 && typical(16) * steps >= 28 * 1024 ? 2 : 1;
   a.blocks = (int)blocks(16 * a.tiles);
   const int64_t items = typical(16 * a.tiles);
-  // Eight waves shorten a workgroup's loop over its keys, four leave less to join and more workgroups to a CU.  256
-  // workgroups of 1044 keys: 12.1 with eight and 13.2 with four; 2560 of 1024 keys 76 and 82; 2560 of 600 keys 58.6 and 55.3;
-  // fp32, whose waves need a third of a SIMD's registers, 1024 of 1100 keys 42.8 and 34.7.
-  a.waves = a.tile_kernel || a.tiles == 2 || (dtype == 1 && hd == 128 && items >= 512) || (items >= 1024 && steps < 24) ? 4 : 8;
+  // Eight waves shorten a workgroup's loop over its keys; four leave less to join, and a CU takes twice as many of them (two
+  // of eight waves, 512 on the card; of fp32, whose waves need a third of a SIMD's registers, one and 256), so that what does
+  // not fit at once as eight and does as four takes one round instead of two.  256 workgroups of 1044 keys: 12.1 with eight
+  // and 13.2 with four; 576 of 1024 keys 21.9 and 19.1, of 2048 keys 41.0 and 37.1, of ragged 4096 keys 40.0 and 43.1; 1024 of
+  // 1000 keys 33.4 and 30.7; 2560 of 1024 keys 76 and 82, of 600 keys 58.6 and 55.3; 864 of 489 keys, fp32, hd 64, 19.6 and
+  // 12.6; fp32, 384 of 1024 keys 22.1 and 18.0, 1024 of 1100 keys 42.8 and 34.7.
+  const bool wide = dtype == 1 && hd == 128;
+  const bool four = (wide && items >= 512) || (items > (wide ? 256 : 512) && items <= 1024 && steps < 128) || (items >= 1024 && steps < 24);
+  a.waves = a.tile_kernel || a.tiles == 2 || four ? 4 : 8;
   // Ranges of keys fill the card where there are few workgroups; the join's launch costs 4 to 5.  8 workgroups: of 4000 keys
   // 12.0 with 16 ranges and 20 with one, of 2000 keys 11.1 with 7 and 11.7 to 12.5 with one, of 32768 keys 16.7 with 64 and 17.2
   // with 32; of 131072 keys 36 and 44.  128 workgroups of 4096 keys 18.1 with two ranges and 22.1 with one, of two tiles and
