@@ -17,7 +17,8 @@ q, k, v are [rows, heads, head_dim], bfloat16 or float32, head_dim 64 or 128; a
 head's entries and a row's heads are adjacent, the rows may lie apart (views of
 one QKV product).  Every call enqueues on `stream` (default: the current stream
 of the tensors' device) and returns new tensors unless it is given some to write
-to.  Arguments that the kernels do not cover raise ValueError, or SDError where
+to; what it uses may be dropped as soon as it returns, as on the current stream.
+Arguments that the kernels do not cover raise ValueError, or SDError where
 only the library sees it (sizes past its limits, addresses or strides off 16
 bytes, eps <= 0), before anything is enqueued.
 """
@@ -141,6 +142,14 @@ def _shape(x: torch.Tensor) -> Tuple[int, int, int, int]:
     return (*shape, index)
 
 
+def _keep(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> None:
+    """Memory that a call on a stream of the caller's choice uses is not given away before the call's work is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor] = None, rope: Optional[torch.Tensor] = None,
               q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-5,
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
@@ -151,7 +160,9 @@ def norm_rope(q: torch.Tensor, k: torch.Tensor, positions: Optional[torch.Tensor
     M, H, hd, index = _shape(q)
     if stream is not None or index != _current_device():
         with _elsewhere(q, stream):
-            return norm_rope(q, k, positions, rope, q_gain, k_gain, eps, q_out, k_out)
+            out = norm_rope(q, k, positions, rope, q_gain, k_gain, eps, q_out, k_out)
+        _keep(stream, q, k, positions, rope, q_gain, k_gain, q_out, k_out)
+        return out
     KV = k.shape[1] if k.dim() == 3 else 0
     if KV < 1 or H % KV:
         raise ValueError("k: [rows, heads, head_dim], its heads a divisor of the query heads")
@@ -188,7 +199,8 @@ def kv_append_q(cache: KVCacheQ, k: torch.Tensor, v: torch.Tensor, rows: KVRows,
     M, KV, hd, index = _shape(k)
     if stream is not None or index != _current_device():
         with _elsewhere(k, stream):
-            return kv_append_q(cache, k, v, rows)
+            kv_append_q(cache, k, v, rows)
+        return _keep(stream, k, v, cache.data, rows.cu_rows, rows.lengths, rows.table)
     if KV != cache.n_kv_heads or hd != cache.head_dim:
         raise ValueError(f"k: [rows, {cache.n_kv_heads}, {cache.head_dim}]")
     _same_device(cache, rows, index)
@@ -207,7 +219,9 @@ def norm_rope_append_q(cache: KVCacheQ, q: torch.Tensor, k: torch.Tensor, v: tor
     M, H, hd, index = _shape(q)
     if stream is not None or index != _current_device():
         with _elsewhere(q, stream):
-            return norm_rope_append_q(cache, q, k, v, rows, rope, q_gain, k_gain, eps, q_out)
+            out = norm_rope_append_q(cache, q, k, v, rows, rope, q_gain, k_gain, eps, q_out)
+        _keep(stream, q, k, v, rope, q_gain, k_gain, q_out, cache.data, rows.cu_rows, rows.lengths, rows.table)
+        return out
     KV = cache.n_kv_heads
     if hd != cache.head_dim or H % KV:
         raise ValueError(f"q: heads of {cache.head_dim}, a multiple of {KV}")
@@ -236,7 +250,9 @@ def kv_read_q(cache: KVCacheQ, rows: KVRows, n_rows: int, dtype: torch.dtype = t
         raise ValueError("a cache on a GPU is needed")
     if stream is not None or index != _current_device():
         with _elsewhere(cache.data, stream):
-            return kv_read_q(cache, rows, n_rows, dtype, k_out, v_out)
+            out = kv_read_q(cache, rows, n_rows, dtype, k_out, v_out)
+        _keep(stream, k_out, v_out, cache.data, rows.cu_rows, rows.lengths, rows.table)
+        return out
     KV, hd = cache.n_kv_heads, cache.head_dim
     if dtype not in _DTYPES or n_rows < 0:
         raise ValueError("at least 0 rows, bfloat16 or float32")
@@ -264,7 +280,9 @@ def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = T
     M, H, hd, index = _shape(q)
     if stream is not None or index != _current_device():
         with _elsewhere(q, stream):
-            return attention_q(q, cache, rows, causal, scale, out)
+            given, out = out, attention_q(q, cache, rows, causal, scale, out)
+        _keep(stream, q, given, cache.data, rows.cu_rows, rows.lengths, rows.table)
+        return out
     KV = cache.n_kv_heads
     if hd != cache.head_dim or H % KV:
         raise ValueError(f"q: heads of {cache.head_dim}, a multiple of {KV}")

@@ -748,6 +748,47 @@ def test_streams():
         assert all(torch.equal(a, b) for a, b in zip(o, want))
 
 
+def test_stream_keeps_memory():
+    """Inputs that are dropped while the call's stream has not come to them yet: their memory is not given away."""
+    import torch
+    from paper_2510_11331_amd import KVCacheQ, KVRows, attention_q, kv_append_q, kv_read_q, norm_rope, norm_rope_append_q, rope_table
+    say("memory on another stream")
+    r = np.random.default_rng(12)
+    H, KV, hd = 8, 8, 128
+    c = Case(r, [9] * 8, [100 + 7 * i for i in range(8)], KV, hd)
+    c.fill(r)
+    host_x = torch.from_numpy(r.normal(size=(c.M, H + 2 * KV, hd)).astype(np.float32))
+    side = torch.cuda.Stream()
+
+    def inputs():
+        x = host_x.cuda()
+        q, k, v = (y.contiguous() for y in x.split([H, KV, KV], 1))
+        d = KVRows(*(y.clone() for y in (c.desc.cu_rows, c.desc.lengths, c.desc.table)))
+        return q, k, v, KVCacheQ(c.cache().data.clone()), d, rope_table(1024, hd), torch.ones(hd, device="cuda"), t(c.pos.astype(np.int32))
+
+    def calls(s, q, k, v, cache, d, rope, g, pos):
+        a = norm_rope(q, k, pos, rope, g, g, stream=s)
+        b = norm_rope_append_q(cache, q, k, v, d, rope, g, g, stream=s)
+        o = attention_q(b, cache, d, stream=s)
+        kv_append_q(cache, k, v, d, stream=s)
+        return [*a, b, o, attention_q(q, cache, d, stream=s), *kv_read_q(cache, d, c.M, stream=s)]
+
+    want = calls(None, *inputs())
+    torch.cuda.synchronize()
+    for _ in range(3):
+        args = inputs()
+        sizes = [x.numel() * x.element_size() for x in args[:3]] + [args[3].data.numel()] + [x.numel() * 4 for x in args[5:]]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = calls(side, *args)
+        del args
+        other = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(2)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del other, got
+
+
 def test_no_rows():
     """Calls without rows or sequences return at once; a pass of more rows than its sequences have leaves the rest."""
     import torch
