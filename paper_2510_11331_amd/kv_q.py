@@ -88,13 +88,17 @@ def rope_table(n_pos: int, head_dim: int, theta: float = 10000.0, device="cuda",
     """(cos, sin) of position theta^(-2 i / head_dim): float32 [n_pos, head_dim / 2, 2]."""
     if n_pos < 0 or head_dim not in (64, 128) or not theta > 0:
         raise ValueError("n_pos >= 0, head_dim 64 or 128, theta > 0")
-    out = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
-    there = _elsewhere(out, stream)
-    if there is not None:
-        with there:
-            check(lib().sd_rope_table(n_pos, head_dim, theta, out.data_ptr(), _raw_stream(out.get_device())), "sd_rope_table")
-        return out
-    check(lib().sd_rope_table(n_pos, head_dim, theta, out.data_ptr(), _raw_stream(out.get_device())), "sd_rope_table")
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError("tensors on a GPU are needed")
+    index = _current_device() if device.index is None else device.index
+    if stream is not None and stream.device.index != index:
+        raise ValueError("the stream is of another device than the table")
+    if stream is not None or index != _current_device():
+        with torch.cuda.device(index) if stream is None else torch.cuda.stream(stream):
+            return rope_table(n_pos, head_dim, theta, torch.device("cuda", index))
+    out = torch.empty((n_pos, head_dim // 2, 2), dtype=torch.float32, device=torch.device("cuda", index))
+    check(lib().sd_rope_table(n_pos, head_dim, theta, out.data_ptr(), _raw_stream(index)), "sd_rope_table")
     return out
 
 
