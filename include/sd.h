@@ -489,7 +489,9 @@ int sd_kv_read_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int dt
  * A row that sees nothing is zero.  NaN and infinities in positions that a row
  * does not see do not reach it; a NaN that it sees is in its output as
  * the formula has it (a key's in all of a head, a value block's in its 32
- * dimensions).  Sums and the softmax are in fp32.  out may not overlap q.  A length may
+ * dimensions).  Scores, their products with |scale| log2(e), sums and the softmax
+ * are in fp32: any of these within its range gives finite outputs of finite
+ * values.  out may not overlap q.  A length may
  * be anything up to 16 table_width: max_len (0: the table's width) only says
  * for which lengths the work is split.  The workspace (16-byte aligned) is
  * scratch of one call: what it held before does not matter, nothing in it is

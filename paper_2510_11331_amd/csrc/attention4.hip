@@ -268,14 +268,21 @@ __device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&
   }
 }
 
+// A weight's logarithm is z c - m of one rounding, m the rounded z c of a maximum.  From |m| = FAR on that rounding is no
+// longer small against 1 (2^-4 there; past 2^32 it alone takes a weight out of fp32's range, past 2^29 out of fp16's): the
+// product is rounded first, as m's was, and the largest key's weight is 1 again.
+constexpr float FAR = 1048576.f;
+// what a step's largest logarithm may be before the maximum moves: 8, and with a far m in the wave nothing
+constexpr int NEAR_LIMIT = 0x41000000, FAR_LIMIT = -1;
 // Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> the logarithms x of their weights, with the running maxima
 // m, and what goes with these: the weights' sums l and the outputs o.  edge: vector t sees the keys below vis[t] only.
 template <int QT, int DT, typename L>
 __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float c, int key, const int (&vis)[QT], float (&m)[QT],
-                                      L (&l)[QT], f32x4 (&o)[QT][DT], float (&x)[QT][8]) {
-  auto over = [&](int t) {                       // in powers of two over the maximum
+                                      int& limit, L (&l)[QT], f32x4 (&o)[QT][DT], float (&x)[QT][8]) {
+  auto over = [&](int t, bool far) {             // in powers of two over the maximum
+#pragma clang fp contract(off)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[t][e] = fmaf(z[t][e / 4][e % 4], c, -m[t]);
+    for (int e = 0; e < 8; ++e) x[t][e] = far ? z[t][e / 4][e % 4] * c - m[t] : fmaf(z[t][e / 4][e % 4], c, -m[t]);
     if (edge) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -286,11 +293,12 @@ __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float 
   int top = 0;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    over(t);
+    over(t, false);
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, __float_as_int(x[t][e]));
   }
-  if (__any(top > 0x41000000)) {                 // 8.0
+  if (__any(top > limit)) {
+    bool any_far = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float most = -FLT_MAX;
@@ -301,8 +309,11 @@ __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float 
       l[t] *= old;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[t][d] *= old;
-      over(t);
+      const bool far = fabsf(to) >= FAR;
+      over(t, far);
+      any_far |= far && to > -FLT_MAX;           // (the maximum of nothing yet)
     }
+    limit = __any(any_far) ? FAR_LIMIT : NEAR_LIMIT;
   }
 }
 __device__ __forceinline__ void exp8(float (&x)[8]) {
@@ -471,6 +482,7 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
     vE[1] = page_load<uint32_t>(b1, off_vs);
   };
 
+  int limit = FAR_LIMIT;
   int key0 = first, left = steps, at = 0;       // at: of the step after this one, within ids
   // EDGE: some key of the step is not seen by all vectors, or a page is none
   auto step = [&]<bool EDGE>() {
@@ -506,7 +518,7 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
 
     u32x4 w8[QT][PP];
     float x[QT][8];
-    weigh(EDGE, z, c, key0 + 4 * g, vis, m, l, o, x);
+    weigh(EDGE, z, c, key0 + 4 * g, vis, m, limit, l, o, x);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       exp8(x[u]);
@@ -803,7 +815,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
     lds_barrier();
     read_keys(0);
     scores();
-    int vb = 0, leave = s_leave[0];
+    int vb = 0, leave = s_leave[0], limit = NEAR_LIMIT;
     lds_barrier();
     auto next = [&]<int S>() {                   // step i, S = i % 2
       if (i >= full || __builtin_amdgcn_readfirstlane(leave) == i + 1) return false;
@@ -811,7 +823,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
       read_keys(1 - S);
       leave = s_leave[after];
       float x[QT][8];
-      weigh(false, z, c, 0, vis, m, l, o, x);
+      weigh(false, z, c, 0, vis, m, limit, l, o, x);
       u32x4 vf[DT];
 #pragma unroll
       for (int d = 0; d < DT; ++d) vf[d] = s_v[vb][d][lane];

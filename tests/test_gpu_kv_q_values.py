@@ -1,0 +1,98 @@
+"""Attention over the 4-bit cache at the ends of its numbers' range: scores, weights and values."""
+import numpy as np
+import pytest
+
+import kvplans
+from kvref import HALF
+from sdcase import say
+from test_gpu_kv_q import Case, host, t
+
+pytestmark = pytest.mark.gpu
+
+KERNELS = [  # name, rows, lengths, heads, kv heads, head_dim, type, pages that the table is wide, plan
+    ("one key", [1], [1], 4, 2, 64, "bf16", 1, (0, 16, 8, 1, 0)),
+    ("one key, fp32", [1], [1], 4, 2, 128, "fp32", 1, (0, 16, 8, 1, 0)),
+    ("waves of 8", [5, 1, 3], [600, 33, 1000], 8, 2, 128, "bf16", 64, (0, 16, 8, 1, 0)),
+    ("waves of 8, fp32", [5, 1, 3], [600, 33, 1000], 8, 2, 64, "fp32", 64, (0, 16, 8, 1, 0)),
+    ("two tiles", [9] * 16, [9 + 37 * i for i in range(16)], 32, 8, 128, "bf16", 150, (0, 32, 4, 1, 0)),
+    ("key ranges", [2], [9000], 16, 2, 64, "bf16", 600, (0, 16, 4, 37, 0)),
+    ("key ranges, fp32", [3], [1500], 16, 4, 64, "fp32", 110, (0, 16, 4, 6, 0)),
+    ("shared", [520, 520], [700, 555], 32, 16, 128, "bf16", 44, (1, 128, 4, 1, 0)),
+    ("shared, 64 dimensions", [520, 520], [700, 555], 32, 16, 64, "bf16", 44, (1, 128, 4, 1, 0)),
+]
+kernels = pytest.mark.parametrize("kernel", KERNELS, ids=lambda k: k[0])
+
+
+def case_of(r, kernel):
+    name, rows, lengths, H, KV, hd, dtype, width, plan = kernel
+    assert kvplans.plan(sum(rows), H, KV, hd, dtype, len(rows), 16 * width) == plan
+    return Case(r, rows, lengths, KV, hd, width=width), H, dtype
+
+
+def put(c, b, k, v):
+    c.pool.put(*c.at(b, np.arange(c.lengths[b])), k.astype(np.float32), v.astype(np.float32))
+
+
+@kernels
+@pytest.mark.parametrize("power", [17, 21, 29, 30, 33, 40, 100])
+@pytest.mark.parametrize("scale", [1.0, -0.37])
+def test_large_scores(kernel, power, scale):
+    """Scores from 2^17 on that are exact in fp32 and lie far apart or are equal: the output is the mean of the values whose
+    scores are the largest.
+
+    Equal scores have equal weights.  bf16 calls enter a weight into the product as two bf16 parts, off by 2^-15 of it;
+    fp32 ones as it is.  The kernel that shares its keys enters it as one fp16 number, off by 2^-11 of it, but for a
+    workgroup's last keys: weights (1 + d) w with |d| <= 2^-11 make a mean that is off by at most 2 2^-11 / (1 - 2^-11) of the
+    mean of the values' magnitudes, a little over 2^-10.  The sums of n weights and of n values are of as many roundings,
+    their quotient of two more."""
+    from paper_2510_11331_amd import attention_q
+    say("large scores", kernel[0], power, scale)
+    r = np.random.default_rng([power, len(kernel[0])])
+    c, H, dtype = case_of(r, kernel)
+    KV, hd, G = c.KV, c.hd, H // c.KV
+    numbers = np.array([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6])
+    q = np.zeros((c.M, H, hd))
+    q[:, :, 5] = r.choice([-1.75, -1.5, -1.0, 1.0, 1.25, 1.5], size=(c.M, H)) * 2.0 ** power
+    want, far = np.zeros(q.shape), np.zeros(q.shape)
+    for b, (n, m) in enumerate(zip(c.rows, c.lengths)):
+        k, v = np.zeros((m, KV, hd)), r.choice(numbers, size=(m, KV, hd))
+        k[:, :, 5] = r.choice(numbers, size=(m, KV))
+        put(c, b, k, v)
+        s = slice(c.cu[b], c.cu[b] + n)
+        seen = np.arange(m)[None] <= c.pos[s][:, None]
+        for h in range(H):
+            z = np.where(seen, np.sign(scale) * q[s, h, 5][:, None] * k[:, h // G, 5][None], -np.inf)
+            top = (z == z.max(1, keepdims=True)).astype(float)
+            count = top.sum(1, keepdims=True)
+            want[s, h] = top @ v[:, h // G] / count
+            a = top @ np.abs(v[:, h // G]) / count
+            form = 0.0 if dtype == "fp32" else 2.0 ** -14 if kernel[8][0] == 0 else 1.001 * 2.0 ** -10
+            far[s, h] = a * form + a * (count + 4) * 2.0 ** -23
+    got = host(attention_q(t(q.astype(np.float32), dtype), c.cache(), c.desc, scale=scale))
+    bad = ~(np.abs(got - want) <= far + np.abs(want) * HALF[dtype] * 1.001)
+    assert not bad.any(), (bad.sum(), np.isnan(got).sum(), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+@kernels
+@pytest.mark.parametrize("size", [1e5, 1e7, 1e9, 1e10, 1e14, 1e30])
+def test_large_scores_of_any_query(kernel, size):
+    """Any finite scores: every dimension of an output lies between the smallest and the largest of the values seen, but
+    for the roundings of weights (2^-11 at most, 2^-10 of the values with their sum's), sums and outputs."""
+    from paper_2510_11331_amd import attention_q
+    say("any large scores", kernel[0], size)
+    r = np.random.default_rng([int(np.log2(size)), len(kernel[0])])
+    c, H, dtype = case_of(r, kernel)
+    G = H // c.KV
+    q = t((r.normal(size=(c.M, H, c.hd)) * np.exp(r.normal(size=(c.M, H, 1)))).astype(np.float32), dtype)
+    lo, hi = np.zeros(q.shape), np.zeros(q.shape)
+    for b, (n, m) in enumerate(zip(c.rows, c.lengths)):
+        x = r.normal(size=(2, m, c.KV, c.hd))
+        put(c, b, x[0], x[1])
+        v = c.pool.get(*c.at(b, np.arange(m)))[1]
+        s, pos = slice(c.cu[b], c.cu[b] + n), c.pos[c.cu[b]:c.cu[b] + n]
+        lo[s], hi[s] = (np.repeat(f.accumulate(v)[pos], G, 1) for f in (np.minimum, np.maximum))
+    for scale in (size, -size):
+        got = host(attention_q(q, c.cache(), c.desc, scale=scale))
+        slack = np.maximum(np.abs(lo), np.abs(hi)) * (2.0 ** -10 + HALF[dtype])
+        bad = ~((got >= lo - slack) & (got <= hi + slack))
+        assert not bad.any(), (bad.sum(), np.isnan(got).sum(), np.argwhere(bad)[:4].tolist(), got[bad][:4], lo[bad][:4], hi[bad][:4])
