@@ -406,8 +406,10 @@ int sd_plan_gate_up_q(int M, int F, int K, int fast, sd_linear_q_plan *out);
  * negatives, code + 8) with a power-of-two scale 2^(E - 127), E a byte, per
  * 32 dimensions of one token and head.  E is the smallest E >= 1 with amax <= 6
  * 2^(E - 127), amax the block's largest magnitude; a code is the value times
- * 2^(127 - E) rounded to nearest even (fp32 values past 1.75 2^127 become
- * infinities).  A block with a NaN or an infinity gets E = 255 and reads as NaN.
+ * 2^(127 - E) rounded to nearest even.  A block with a NaN, an infinity or a
+ * value that would be rounded to one (from 1.75 2^127 on) gets E = 255 and reads
+ * as NaN.  (Codes of 2^128 or more, E = 253 or 254, are written by no call; they
+ * read as infinities, and the attention may take them as 1.5 2^127.)
  *   Pool  uint8 [n_blocks, n_kv_heads, 17 head_dim], 16-byte aligned; head_dim
  *     64 or 128.  A page holds 16 tokens; of one head: key codes [16 tokens]
  *     [head_dim / 2], value codes [token / 4][16][token % 4][head_dim / 32],

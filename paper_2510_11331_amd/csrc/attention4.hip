@@ -376,18 +376,34 @@ __device__ __forceinline__ void add_values(const typename Load4<HD>::type (&c)[2
 
 // Values that not every vector sees must be finite: their weights are zero where they are not seen, and a NaN that a
 // vector does see is put into its output by put_nan.  key: the lane's first; no: pages that are none.  Whether there was
-// such a NaN.
-__device__ __forceinline__ bool clean_scales(uint32_t (&E)[2], int key, int n_max, uint32_t no) {
+// such a NaN; large: whether there is a scale whose largest codes are infinities.
+__device__ __forceinline__ bool clean_scales(uint32_t (&E)[2], int key, int n_max, uint32_t no, bool& large) {
   bool nan = false;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool is_nan = (E[t] >> (8 * e) & 255u) == 255u, none = key + 16 * t + e >= n_max || (no >> t & 1);
+      const uint32_t E8 = E[t] >> (8 * e) & 255u;
+      const bool is_nan = E8 == 255u, none = key + 16 * t + e >= n_max || (no >> t & 1);
       nan |= is_nan && !none;
       if (is_nan || none) E[t] = (E[t] & ~(255u << (8 * e))) | 127u << (8 * e);
+      else large |= E8 >= 253u;
     }
   return nan;
+}
+// Codes whose numbers are infinities (4 and 6 with E = 253, 2 to 6 with E = 254; nothing writes them) as the largest number
+// that is none: 3 or 1.5, both the odd code below the first.
+template <int HD> __device__ __forceinline__ void clean_codes(typename Load4<HD>::type (&c)[2], const uint32_t (&E)[2]) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t E8 = E[t] >> (8 * e) & 255u;
+      const uint32_t w = c[t][HD == 128 ? e : e / 2];
+      const uint32_t mine = HD == 128 ? 0x11111111u : 0x1111u << (16 * (e % 2));
+      const uint32_t inf = (E8 == 253u ? w >> 2 & w >> 1 : E8 == 254u ? w >> 2 : 0u) & mine;
+      c[t][HD == 128 ? e : e / 2] = (w & ~(7u * inf)) | inf * (E8 == 253u ? 5u : 3u);
+    }
 }
 // the value blocks of NaN among the step's keys; all of a lane's outputs are of scale block (hd / 4) g / 32
 template <int HD, int QT>
@@ -526,7 +542,9 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
       parts8<PP>(x[u], w8[u]);
     }
 
-    const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here);
+    bool large = false;
+    const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here, large);
+    if (EDGE && __any(large)) clean_codes<HD>(vc, vE);
     add_values<HD>(vc, vE, w8, o);
     load_v();
     if (EDGE && __any(nan)) put_nan<HD>(here, no_here, key0, n_max, g, vis, o);

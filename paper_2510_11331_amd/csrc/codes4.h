@@ -5,7 +5,8 @@
 // 2^(E - 127) per block of 32 dimensions of one token and head.  E is the
 // smallest E >= 1 with amax <= 6 2^(E - 127): scaling and rounding to a code
 // are then functions of the value alone, without a division.  A block with a
-// NaN or an infinity has E = 255, whose scale is an infinity: the conversion
+// NaN or an infinity, or a value that would be rounded to one (from 1.75 2^127
+// on, to 4 2^126), has E = 255, whose scale is an infinity: the conversion
 // instruction makes NaN of all 32 codes.
 //
 // A page holds 16 tokens of one kv head in 17 hd bytes:
@@ -35,9 +36,9 @@ template <int HD> struct Page4 {
   __device__ __forceinline__ static int value_scale(int t, int b) { return VS + b * 16 + t; }
 };
 
-// E of a block whose largest magnitude has the given bits (255 from infinity on)
+// E of a block whose largest magnitude has the given bits (255 from 1.75 2^127 on)
 __device__ __forceinline__ uint32_t block_exp4(uint32_t amax) {
-  if (amax >= 0x7f800000u) return 255u;
+  if (amax >= 0x7f600000u) return 255u;
   const int e = (int)((amax + 0x3fffffu) >> 23) - 2;   // the fraction past 1.5 carries
   return (uint32_t)(e < 1 ? 1 : e);
 }

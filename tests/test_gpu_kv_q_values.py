@@ -5,7 +5,7 @@ import pytest
 import kvplans
 from kvref import HALF
 from sdcase import say
-from test_gpu_kv_q import Case, host, t
+from test_gpu_kv_q import Case, close, host, t
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +96,75 @@ def test_large_scores_of_any_query(kernel, size):
         slack = np.maximum(np.abs(lo), np.abs(hi)) * (2.0 ** -10 + HALF[dtype])
         bad = ~((got >= lo - slack) & (got <= hi + slack))
         assert not bad.any(), (bad.sum(), np.isnan(got).sum(), np.argwhere(bad)[:4].tolist(), got[bad][:4], lo[bad][:4], hi[bad][:4])
+
+
+@kernels
+@pytest.mark.parametrize("E", [252, 253, 254])
+def test_values_at_the_end_of_the_range(kernel, E):
+    """Tokens of the pass's own rows with 6 2^(E - 127) and its negative among 32 zeros: from E = 253 on these are infinities
+    in bf16 and fp32.  They reach no output but the rows' that see the token, in their dimension."""
+    from paper_2510_11331_amd import attention_q
+    say("end of the range", kernel[0], E)
+    r = np.random.default_rng([E, len(kernel[0])])
+    c, H, dtype = case_of(r, kernel)
+    c.fill(r)
+    KV, hd, G = c.KV, c.hd, H // c.KV
+    q = t(r.normal(size=(c.M, H, hd)).astype(np.float32), dtype)
+    put_in, reached = [], np.zeros((c.M, H, hd), bool)
+    for b, (n, m) in enumerate(zip(c.rows, c.lengths)):
+        for pos in np.unique(m - n + r.integers(min(1, n - 1), n, size=3)):
+            page, tok = c.at(b, pos)
+            kvh, block, dims = r.integers(KV), r.integers(hd // 32), r.choice(16, size=2, replace=False) * 2
+            bytes_of = c.pool.bytes[page, kvh]
+            codes = c.pool.vc[tok, block * 16:block * 16 + 16]
+            bytes_of[codes] = 0
+            bytes_of[c.pool.vs[tok, block]] = 127
+            put_in.append((bytes_of, codes[dims // 2], c.pool.vs[tok, block]))
+            rows = c.cu[b] + np.arange(n)[c.pos[c.cu[b]:c.cu[b] + n] >= pos]
+            reached[np.ix_(rows, np.arange(kvh * G, kvh * G + G), block * 32 + dims)] = True
+    want, err = c.attention(host(q))
+    for bytes_of, codes, scale in put_in:
+        bytes_of[codes] = 7, 15
+        bytes_of[scale] = E
+    got = host(attention_q(q, c.cache(), c.desc))
+    close(got[~reached], want[~reached], err[:, ~reached], dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_appended_values_at_the_end_of_the_range(hd, dtype):
+    """What would be rounded to an infinity is kept as an infinity is, as NaN, and reaches the rows that see it only; the
+    next smaller value is a number."""
+    from paper_2510_11331_amd import attention_q, kv_append_q, kv_read_q
+    say("appended at the range's end", hd, dtype)
+    r = np.random.default_rng(hd)
+    end = 1.75 * 2.0 ** 127
+    below = end * (1 - 2.0 ** -8) if dtype == "bf16" else float(np.nextafter(np.float32(end), np.float32(0)))
+    for value, is_nan in ((1.9 * 2.0 ** 127, True), (-end, True), (-below, False)):
+        c = Case(r, [20], [50], 2, hd)
+        c.fill(r)
+        x = t(r.normal(size=(2, 20, 2, hd)).astype(np.float32), dtype)
+        x[1, 19, 1, 40] = value
+        x[0, 18, 0, hd - 1] = value
+        cache = c.cache()
+        kv_append_q(cache, x[0], x[1], c.desc)
+        got = [host(y) for y in kv_read_q(cache, c.desc, 20, x.dtype)]
+        v = got[1][19, 1, 32:64]
+        k = got[0][18, 0, hd - 32:]
+        if is_nan:
+            assert np.isnan(v).all() and np.isnan(k).all()
+        else:
+            assert v[8] == k[31] == -1.5 * 2.0 ** 127 and (np.delete(v, 8) == 0).all() and (k[:31] == 0).all()
+        assert np.isfinite(got[1][:19]).all() and np.isfinite(got[0][:18]).all() and np.isfinite(got[0][19]).all()
+        q = t(r.normal(size=(20, 4, hd)).astype(np.float32), dtype)
+        page, tok = c.at(0, np.array([48, 49]))
+        c.pool.bytes[:] = cache.data.cpu().numpy()
+        c.pool.bytes[page[0], 0, c.pool.ks[tok[0], -1]] = c.pool.bytes[page[1], 1, c.pool.vs[tok[1], 1]] = 1   # for the reference
+        want, err = c.attention(host(q))
+        out = host(attention_q(q, cache, c.desc))
+        ok = np.ones(out.shape, bool)
+        ok[18:, :2] = False                                              # that key's rows
+        ok[19, 2:, 32:64] = False                                        # that value's
+        close(out[ok], want[ok], err[:, ok], dtype)
+        if is_nan:
+            assert np.isnan(out[18:, :2]).all() and np.isnan(out[19, 2:, 32:64]).all()
