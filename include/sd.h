@@ -493,12 +493,13 @@ int sd_kv_read_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int dt
  * the formula has it (a key's in all of a head, a value block's in its 32
  * dimensions).  Scores, their products with |scale| log2(e), sums and the softmax
  * are in fp32: any of these within its range gives finite outputs of finite
- * values.  out may not overlap q.  A length may
- * be anything up to 16 table_width: max_len (0: the table's width) only says
- * for which lengths the work is split.  The workspace (16-byte aligned) is
- * scratch of one call: what it held before does not matter, nothing in it is
- * used after the call's work is done, and calls that may run at the same time
- * (on two streams, in two graphs) need one each. */
+ * values.  out may not overlap q.  A length may be anything up to 16 table_width:
+ * max_len (0: 16 table_width) only says for which lengths the work is split.  The
+ * workspace's bytes are those for the call's max_len or a larger one (16
+ * table_width where the call passes 0); dtypes need the same.  It (16-byte
+ * aligned) is scratch of one call: what it held before does not matter, nothing in
+ * it is used after the call's work is done, and calls that may run at the same
+ * time (on two streams, in two graphs) need one each. */
 size_t sd_attention_q_workspace_bytes(int M, int n_heads, int n_kv_heads, int head_dim, int n_seqs, int max_len);
 int sd_attention_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int n_heads, int dtype, const void *q, int ldq,
                    void *out, int ldo, int causal, float scale, int max_len, void *workspace, size_t workspace_bytes,

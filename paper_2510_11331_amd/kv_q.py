@@ -62,9 +62,9 @@ class KVRows:
     """The rows of a pass.  cu_rows [n + 1]: sequence b has the rows cu_rows[b] .. cu_rows[b + 1] - 1; lengths [n]: its
     tokens with these rows, which are its last ones; table [n, width]: the pages of its positions 16 i .. 16 i + 15.  All
     int32 on the GPU, read when a call runs: a captured pass follows what is written to them.  max_len: the longest length
-    that the work is to be split for (default: what the table holds)."""
+    that the work is to be split for (default: what the table holds); it may be set between two calls."""
 
-    __slots__ = ("cu_rows", "lengths", "table", "max_len", "_index", "_rows", "_at", "_workspace")
+    __slots__ = ("cu_rows", "lengths", "table", "_max_len", "_index", "_rows", "_at", "_workspace")
 
     def __init__(self, cu_rows: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, max_len: Optional[int] = None):
         n = lengths.shape[0] if lengths.dim() == 1 else -1
@@ -73,13 +73,22 @@ class KVRows:
         for t in (cu_rows, lengths, table):
             if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != table.get_device():
                 raise ValueError("cu_rows, lengths, table: contiguous int32 on one device")
-        if max_len is not None and max_len < 1:
-            raise ValueError("max_len: at least 1")
         self.cu_rows, self.lengths, self.table = cu_rows, lengths, table
-        self.max_len = min(16 * table.shape[1], max_len or 16 * table.shape[1])
+        self.max_len = max_len
         self._index = table.get_device()
         self._rows = KvRows(cu_rows.data_ptr(), lengths.data_ptr(), table.data_ptr(), n, table.shape[1])
         self._at = C.addressof(self._rows)
+
+    @property
+    def max_len(self) -> int:
+        return self._max_len
+
+    @max_len.setter
+    def max_len(self, n: Optional[int]) -> None:
+        if n is not None and n < 1:
+            raise ValueError("max_len: at least 1")
+        most = 16 * self.table.shape[1]
+        self._max_len = min(most, n or most)
         self._workspace = {}                       # bytes of an attention's workspace, by (rows, heads, kv heads, head_dim)
 
 
@@ -300,10 +309,10 @@ def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = T
     sizes = (M, H, KV, hd)
     ws = rows._workspace.get(sizes)
     if ws is None:
-        ws = rows._workspace[sizes] = L.sd_attention_q_workspace_bytes(M, H, KV, hd, rows._rows.n_seqs, rows.max_len)
+        ws = rows._workspace[sizes] = L.sd_attention_q_workspace_bytes(M, H, KV, hd, rows._rows.n_seqs, rows._max_len)
     work = torch.empty(ws, dtype=torch.uint8, device=q.device) if ws else None
     rc = L.sd_attention_q(cache._at, rows._at, M, H, _DTYPES[q.dtype], q.data_ptr(), ldq, out.data_ptr(), ldo, causal,
-                          hd ** -0.5 if scale is None else scale, rows.max_len, work.data_ptr() if ws else None, ws,
+                          hd ** -0.5 if scale is None else scale, rows._max_len, work.data_ptr() if ws else None, ws,
                           _raw_stream(index))
     if rc != SD_OK:
         check(rc, "sd_attention_q")

@@ -47,3 +47,55 @@ def test_rope_table_takes_memory_on_its_stream(where, monkeypatch):
     assert out.shape == (4, 32, 2)
     want = [] if where == "here" else [where]
     assert seen == [("take", want), ("write", want)]
+
+
+def rows_of(width, max_len=None):
+    from paper_2510_11331_amd import KVRows
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    return KVRows(i32(2), i32(1), i32(1, width), max_len)
+
+
+@needs_lib
+def test_max_len_between_calls(monkeypatch):
+    """max_len may be set between two calls: each gets the workspace that its own max_len needs."""
+    from paper_2510_11331_amd import KVCacheQ, _lib, kv_q
+    real, seen = _lib.lib(), []
+    cache, rows = KVCacheQ(torch.zeros(4, 8, 17 * 128, dtype=torch.uint8)), rows_of(2048, 500)
+
+    class Lib:
+        sd_attention_q_workspace_bytes = real.sd_attention_q_workspace_bytes
+
+        @staticmethod
+        def sd_attention_q(pool, rows, M, H, dtype, q, ldq, out, ldo, causal, scale, max_len, work, size, stream):
+            seen.append((max_len, size))
+            return _lib.SD_OK if size >= real.sd_attention_q_workspace_bytes(M, H, 8, 128, 1, max_len) else _lib.SD_EINVAL
+
+    monkeypatch.setattr(kv_q, "lib", lambda: Lib)
+    monkeypatch.setattr(kv_q, "_raw_stream", lambda index: None)
+    monkeypatch.setattr(kv_q, "_current_device", lambda: -1)
+    monkeypatch.setattr(kv_q, "_shape", lambda x: (*x.shape, -1))          # (host tensors stand for the GPU's)
+    q = torch.zeros(1, 32, 128, dtype=torch.bfloat16)
+    for n, given in ((500, 500), (32768, 32768), (16, 16), (32768, 10 ** 6), (1, 1), (32768, None), (16000, 16000)):
+        if (n, given) != (500, 500):
+            rows.max_len = given
+        assert rows.max_len == n
+        kv_q.attention_q(q, cache, rows)
+        assert seen[-1] == (n, real.sd_attention_q_workspace_bytes(1, 32, 8, 128, 1, n))
+    for bad in (0, -1):
+        with pytest.raises(ValueError):
+            rows.max_len = bad
+    assert rows.max_len == 16000
+
+
+@needs_lib
+def test_workspace_grows_with_max_len():
+    """A workspace for a length is enough for every shorter one, and so for a call whose table ends before max_len."""
+    from paper_2510_11331_amd import _lib
+    need = _lib.lib().sd_attention_q_workspace_bytes
+    lengths = [1, 16, 255, 256, 1000, 1535, 1536, 2048, 2559, 2560, 4000, 8191, 8192, 14336, 20000, 33000, 70000, 131072, 10 ** 6, 1 << 24]
+    for hd in (64, 128):
+        for B in (1, 2, 3, 4, 5, 7, 8, 12, 16, 31, 33, 36, 48, 64, 65, 200, 1000):
+            for n in (1, 2, 3, 5, 9, 17, 40, 130, 700):
+                for H, KV in ((1, 1), (8, 1), (8, 8), (17, 1), (20, 5), (40, 5), (32, 8), (32, 32), (64, 8)):
+                    sizes = [need(B * n, H, KV, hd, B, x) for x in lengths]
+                    assert sizes == sorted(sizes), (hd, B, n, H, KV, sizes)
