@@ -37,9 +37,10 @@ _DTYPES = {torch.bfloat16: SD_DTYPE_BF16, torch.float32: SD_DTYPE_F32}
 
 
 class KVCacheQ:
-    """A pool of pages: `data` is uint8 [n_blocks, n_kv_heads, 17 head_dim] on the GPU."""
+    """A pool of pages: `data` is uint8 [n_blocks, n_kv_heads, 17 head_dim] on the GPU.  The calls go by its address: the
+    fields are read-only."""
 
-    __slots__ = ("data", "n_blocks", "n_kv_heads", "head_dim", "_index", "_pool", "_at")
+    __slots__ = ("_data", "_heads", "_hd", "_index", "_pool", "_at")
 
     def __init__(self, data: torch.Tensor):
         if data.dim() != 3 or data.dtype != torch.uint8 or not data.is_contiguous() or data.shape[2] not in (17 * 64, 17 * 128):
@@ -47,7 +48,7 @@ class KVCacheQ:
         n, kv, hd = data.shape[0], data.shape[1], data.shape[2] // 17
         if data.numel() == 0 or lib().sd_kv_q_bytes(n, kv, hd) != data.numel():
             raise ValueError(f"no cache of {n} pages of {kv} heads")
-        self.data, self.n_blocks, self.n_kv_heads, self.head_dim = data, n, kv, hd
+        self._data, self._heads, self._hd = data, kv, hd
         self._index = data.get_device()
         self._pool = KvQPool(data.data_ptr(), n, kv, hd)
         self._at = C.addressof(self._pool)
@@ -57,14 +58,20 @@ class KVCacheQ:
         """A cache whose pages hold nothing yet: only positions that were written may be read."""
         return cls(torch.empty((n_blocks, n_kv_heads, 17 * head_dim), dtype=torch.uint8, device=device))
 
+    data = property(lambda self: self._data)
+    n_blocks = property(lambda self: self._pool.n_blocks)
+    n_kv_heads = property(lambda self: self._heads)
+    head_dim = property(lambda self: self._hd)
+
 
 class KVRows:
     """The rows of a pass.  cu_rows [n + 1]: sequence b has the rows cu_rows[b] .. cu_rows[b + 1] - 1; lengths [n]: its
     tokens with these rows, which are its last ones; table [n, width]: the pages of its positions 16 i .. 16 i + 15.  All
     int32 on the GPU, read when a call runs: a captured pass follows what is written to them.  max_len: the longest length
-    that the work is to be split for (default: what the table holds); it may be set between two calls."""
+    that the work is to be split for (default: what the table holds); it may be set between two calls.  The calls go by the
+    tensors' addresses: these fields are read-only."""
 
-    __slots__ = ("cu_rows", "lengths", "table", "_max_len", "_index", "_rows", "_at", "_workspace")
+    __slots__ = ("_cu_rows", "_lengths", "_table", "_max_len", "_index", "_rows", "_at", "_workspace")
 
     def __init__(self, cu_rows: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor, max_len: Optional[int] = None):
         n = lengths.shape[0] if lengths.dim() == 1 else -1
@@ -73,11 +80,15 @@ class KVRows:
         for t in (cu_rows, lengths, table):
             if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != table.get_device():
                 raise ValueError("cu_rows, lengths, table: contiguous int32 on one device")
-        self.cu_rows, self.lengths, self.table = cu_rows, lengths, table
+        self._cu_rows, self._lengths, self._table = cu_rows, lengths, table
         self.max_len = max_len
         self._index = table.get_device()
         self._rows = KvRows(cu_rows.data_ptr(), lengths.data_ptr(), table.data_ptr(), n, table.shape[1])
         self._at = C.addressof(self._rows)
+
+    cu_rows = property(lambda self: self._cu_rows)
+    lengths = property(lambda self: self._lengths)
+    table = property(lambda self: self._table)
 
     @property
     def max_len(self) -> int:
@@ -87,7 +98,7 @@ class KVRows:
     def max_len(self, n: Optional[int]) -> None:
         if n is not None and n < 1:
             raise ValueError("max_len: at least 1")
-        most = 16 * self.table.shape[1]
+        most = 16 * self._table.shape[1]
         self._max_len = min(most, n or most)
         self._workspace = {}                       # bytes of an attention's workspace, by (rows, heads, kv heads, head_dim)
 
@@ -213,9 +224,9 @@ def kv_append_q(cache: KVCacheQ, k: torch.Tensor, v: torch.Tensor, rows: KVRows,
     if stream is not None or index != _current_device():
         with _elsewhere(k, stream):
             kv_append_q(cache, k, v, rows)
-        return _keep(stream, k, v, cache.data, rows.cu_rows, rows.lengths, rows.table)
-    if KV != cache.n_kv_heads or hd != cache.head_dim:
-        raise ValueError(f"k: [rows, {cache.n_kv_heads}, {cache.head_dim}]")
+        return _keep(stream, k, v, cache._data, rows._cu_rows, rows._lengths, rows._table)
+    if KV != cache._heads or hd != cache._hd:
+        raise ValueError(f"k: [rows, {cache._heads}, {cache._hd}]")
     _same_device(cache, rows, index)
     ldk, ldv = _stride(k, "k", M, KV, hd, k.dtype, index), _stride(v, "v", M, KV, hd, k.dtype, index)
     rc = lib().sd_kv_append_q(cache._at, rows._at, M, _DTYPES[k.dtype], k.data_ptr(), ldk, v.data_ptr(), ldv, _raw_stream(index))
@@ -233,11 +244,11 @@ def norm_rope_append_q(cache: KVCacheQ, q: torch.Tensor, k: torch.Tensor, v: tor
     if stream is not None or index != _current_device():
         with _elsewhere(q, stream):
             out = norm_rope_append_q(cache, q, k, v, rows, rope, q_gain, k_gain, eps, q_out)
-        _keep(stream, q, k, v, rope, q_gain, k_gain, q_out, cache.data, rows.cu_rows, rows.lengths, rows.table)
+        _keep(stream, q, k, v, rope, q_gain, k_gain, q_out, cache._data, rows._cu_rows, rows._lengths, rows._table)
         return out
-    KV = cache.n_kv_heads
-    if hd != cache.head_dim or H % KV:
-        raise ValueError(f"q: heads of {cache.head_dim}, a multiple of {KV}")
+    KV = cache._heads
+    if hd != cache._hd or H % KV:
+        raise ValueError(f"q: heads of {cache._hd}, a multiple of {KV}")
     _same_device(cache, rows, index)
     ldq = _stride(q, "q", M, H, hd, q.dtype, index)
     ldk, ldv = _stride(k, "k", M, KV, hd, q.dtype, index), _stride(v, "v", M, KV, hd, q.dtype, index)
@@ -262,21 +273,21 @@ def kv_read_q(cache: KVCacheQ, rows: KVRows, n_rows: int, dtype: torch.dtype = t
     if index < 0:
         raise ValueError("a cache on a GPU is needed")
     if stream is not None or index != _current_device():
-        with _elsewhere(cache.data, stream):
+        with _elsewhere(cache._data, stream):
             out = kv_read_q(cache, rows, n_rows, dtype, k_out, v_out)
-        _keep(stream, k_out, v_out, cache.data, rows.cu_rows, rows.lengths, rows.table)
+        _keep(stream, k_out, v_out, cache._data, rows._cu_rows, rows._lengths, rows._table)
         return out
-    KV, hd = cache.n_kv_heads, cache.head_dim
+    KV, hd = cache._heads, cache._hd
     if dtype not in _DTYPES or n_rows < 0:
         raise ValueError("at least 0 rows, bfloat16 or float32")
     _same_device(cache, rows, index)
     ldk = ldv = KV * hd
     if k_out is None:
-        k_out = torch.empty(n_rows, KV, hd, dtype=dtype, device=cache.data.device)
+        k_out = torch.empty(n_rows, KV, hd, dtype=dtype, device=cache._data.device)
     else:
         ldk = _stride(k_out, "k_out", n_rows, KV, hd, dtype, index)
     if v_out is None:
-        v_out = torch.empty(n_rows, KV, hd, dtype=dtype, device=cache.data.device)
+        v_out = torch.empty(n_rows, KV, hd, dtype=dtype, device=cache._data.device)
     else:
         ldv = _stride(v_out, "v_out", n_rows, KV, hd, dtype, index)
     rc = lib().sd_kv_read_q(cache._at, rows._at, n_rows, _DTYPES[dtype], k_out.data_ptr(), ldk, v_out.data_ptr(), ldv,
@@ -294,11 +305,11 @@ def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = T
     if stream is not None or index != _current_device():
         with _elsewhere(q, stream):
             given, out = out, attention_q(q, cache, rows, causal, scale, out)
-        _keep(stream, q, given, cache.data, rows.cu_rows, rows.lengths, rows.table)
+        _keep(stream, q, given, cache._data, rows._cu_rows, rows._lengths, rows._table)
         return out
-    KV = cache.n_kv_heads
-    if hd != cache.head_dim or H % KV:
-        raise ValueError(f"q: heads of {cache.head_dim}, a multiple of {KV}")
+    KV = cache._heads
+    if hd != cache._hd or H % KV:
+        raise ValueError(f"q: heads of {cache._hd}, a multiple of {KV}")
     _same_device(cache, rows, index)
     ldq, ldo = _stride(q, "q", M, H, hd, q.dtype, index), H * hd
     if out is None:

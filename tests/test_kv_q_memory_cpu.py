@@ -88,6 +88,17 @@ def test_max_len_between_calls(monkeypatch):
 
 
 @needs_lib
+def test_tensors_of_handles_stay():
+    """The calls read addresses taken when a handle was made: its tensors and sizes cannot be exchanged."""
+    from paper_2510_11331_amd import KVCacheQ
+    cache, rows = KVCacheQ(torch.zeros(4, 2, 17 * 64, dtype=torch.uint8)), rows_of(3)
+    for handle, names in ((cache, ("data", "n_blocks", "n_kv_heads", "head_dim")), (rows, ("cu_rows", "lengths", "table"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(handle, name, getattr(handle, name))
+
+
+@needs_lib
 def test_workspace_grows_with_max_len():
     """A workspace for a length is enough for every shorter one, and so for a call whose table ends before max_len."""
     from paper_2510_11331_amd import _lib
