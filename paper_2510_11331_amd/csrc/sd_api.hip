@@ -1406,6 +1406,21 @@ static bool kv_q_rows_ok(const sd_kv_rows* r) {
 static bool kv_q_rows_at(const void* p, int ld, int heads, int head_dim, int dtype) {
   return p && (uintptr_t)p % 16 == 0 && ld >= heads * head_dim && ((size_t)ld * esize(dtype)) % 16 == 0;
 }
+// whether M rows of so many bytes, strides apart, have a byte in common with those at b
+static bool kv_q_rows_meet(const void* a, size_t lda, const void* b, size_t ldb, int M, size_t bytes) {
+  uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  if (x + (M - 1) * lda + bytes <= y || y + (M - 1) * ldb + bytes <= x) return false;
+  if (lda == ldb) {                              // one lies between the rows of the other, or some row meets another
+    const size_t d = x < y ? (y - x) % lda : (x - y) % lda;
+    return d < bytes || lda - d < bytes;
+  }
+  for (int i = 0, j = 0; i < M && j < M;) {
+    if (x + bytes <= y) ++i, x += lda;
+    else if (y + bytes <= x) ++j, y += ldb;
+    else return true;
+  }
+  return false;
+}
 static bool kv_q_arrays_ok(const sd_kv_q_pool* pool, const sd_kv_rows* r) {
   return pool->data && (uintptr_t)pool->data % 16 == 0 && r->cu_rows && r->lengths && r->table &&
          ((uintptr_t)r->cu_rows | (uintptr_t)r->lengths | (uintptr_t)r->table) % 4 == 0;
@@ -1572,6 +1587,8 @@ int sd_attention_q(const sd_kv_q_pool* pool, const sd_kv_rows* rows, int M, int 
   if (M == 0 || rows->n_seqs == 0) return SD_OK;
   if (!kv_q_rows_at(q, ldq, n_heads, hd, dtype) || !kv_q_rows_at(out, ldo, n_heads, hd, dtype) || !kv_q_arrays_ok(pool, rows))
     return SD_EINVAL;
+  const size_t size = esize(dtype);
+  if (kv_q_rows_meet(q, ldq * size, out, ldo * size, M, n_heads * hd * size)) return SD_EINVAL;
   const int len = max_len ? std::min(max_len, 16 * rows->table_width) : 16 * rows->table_width;
   const Attn4Plan plan = plan_attention4(dtype == SD_DTYPE_F32 ? 1 : 0, hd, M, n_heads, KV, rows->n_seqs, len);
   if (!attention_q_grid_ok(plan, KV)) return SD_EINVAL;

@@ -20,7 +20,7 @@ of the tensors' device) and returns new tensors unless it is given some to write
 to; what it uses may be dropped as soon as it returns, as on the current stream.
 Arguments that the kernels do not cover raise ValueError, or SDError where
 only the library sees it (sizes past its limits, addresses or strides off 16
-bytes, eps <= 0), before anything is enqueued.
+bytes, eps <= 0, attention on its own queries), before anything is enqueued.
 """
 from __future__ import annotations
 
@@ -300,7 +300,8 @@ def kv_read_q(cache: KVCacheQ, rows: KVRows, n_rows: int, dtype: torch.dtype = t
 def attention_q(q: torch.Tensor, cache: KVCacheQ, rows: KVRows, causal: bool = True, scale: Optional[float] = None,
                 out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """softmax(scale q K^T) V [rows, heads, head_dim] over the cached positions up to the row's own (causal) or all of its
-    sequence's; scale: head_dim^-0.5 unless given.  Query heads share kv heads in runs.  out: where it goes."""
+    sequence's; scale: head_dim^-0.5 unless given.  Query heads share kv heads in runs.  out: where it goes (memory that
+    overlaps no input; on q is refused)."""
     M, H, hd, index = _shape(q)
     if stream is not None or index != _current_device():
         with _elsewhere(q, stream):

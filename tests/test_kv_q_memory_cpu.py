@@ -110,3 +110,59 @@ def test_workspace_grows_with_max_len():
                 for H, KV in ((1, 1), (8, 1), (8, 8), (17, 1), (20, 5), (40, 5), (32, 8), (32, 32), (64, 8)):
                     sizes = [need(B * n, H, KV, hd, B, x) for x in lengths]
                     assert sizes == sorted(sizes), (hd, B, n, H, KV, sizes)
+
+
+@needs_lib
+def test_attention_refuses_outputs_on_its_queries():
+    """Other workgroups may still read a query when an output is written: also partly on it, or between its rows.  (The
+    pointers are never dereferenced.)"""
+    import ctypes as C
+    from paper_2510_11331_amd import _lib
+    L, A = _lib.lib(), 1 << 24
+    pool, rows = _lib.KvQPool(1 << 20, 9, 2, 64), _lib.KvRows(1 << 20, 1 << 20, 1 << 20, 2, 3)
+    row = 4 * 64 * 2                                                        # bytes of a row of 4 heads in bf16
+
+    def refused(M, out, ldq=4 * 64, ldo=4 * 64):
+        return L.sd_attention_q(C.addressof(pool), C.addressof(rows), M, 4, _lib.SD_DTYPE_BF16, A, ldq, A + out, ldo, 1, 0.1, 48,
+                                1 << 20, 1 << 20, None) == _lib.SD_EINVAL
+
+    for M in (1, 2, 7):
+        for at in (0, 16, row - 16, (M - 1) * row, M * row - 16, -16, 16 - row, 16 - M * row):
+            assert refused(M, at), (M, at)
+    wide = 8 * 64                                                           # rows with as much between them
+    for M in (2, 7):
+        for at in (0, 16, row - 16, row + 16, 2 * row, 2 * row - 16, -16, -row + 16, -row - 16, -2 * row, (M - 1) * 2 * row):
+            assert refused(M, at, wide, wide), (M, at)
+        # of other strides: the output's second row on the query's third, its last row on the query's first
+        assert refused(5, 4 * row - 3 * row, wide, 3 * 4 * 64) and refused(5, -4 * 3 * row, wide, 3 * 4 * 64)
+        assert refused(3, -2 * row, 4 * 64, 4 * 64)
+
+
+@needs_lib
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the call that is not refused would run")
+def test_attention_refusals_with_outputs_apart():
+    """Each argument that is refused, in a call that is not refused without it (which then finds no GPU)."""
+    import ctypes as C
+    from paper_2510_11331_amd import _lib
+    L, E, A = _lib.lib(), _lib.SD_EINVAL, 1 << 20
+    pool = dict(data=A, n_blocks=3000, n_kv_heads=8, head_dim=128)
+    rows = dict(cu_rows=A, lengths=A, table=A, n_seqs=1, table_width=2048)
+    n = L.sd_attention_q_workspace_bytes(5, 32, 8, 128, 1, 32768)
+    assert n > 0
+    good = dict(M=5, H=32, dtype=_lib.SD_DTYPE_BF16, q=A, ldq=4096, out=2 * A, ldo=4096, causal=1, scale=0.1, max_len=0, ws=4 * A, n=n)
+
+    def call(p={}, r={}, **a):
+        keep = _lib.KvQPool(*{**pool, **p}.values()), _lib.KvRows(*{**rows, **r}.values())
+        return L.sd_attention_q(C.addressof(keep[0]), C.addressof(keep[1]), *{**good, **a}.values(), None)
+
+    for fine in ({}, dict(out=A + 5 * 4096 * 2), dict(out=A - 5 * 4096 * 2), dict(ldq=8192, out=A + 4096 * 2, ldo=8192), dict(max_len=1000, ws=None, n=0)):
+        assert call(**fine) not in (E, _lib.SD_OK), fine
+    for bad in (dict(M=-1), dict(M=(1 << 20) + 1), dict(H=0), dict(H=33), dict(H=1032), dict(dtype=2), dict(q=None), dict(q=A + 8), dict(ldq=4088),
+                dict(ldq=4100), dict(out=None), dict(out=2 * A + 8), dict(ldo=4088), dict(ldo=4100), dict(max_len=-1), dict(ws=None),
+                dict(ws=4 * A + 8), dict(n=n - 1), dict(n=0)):
+        assert call(**bad) == E, bad
+    for bad in (dict(data=None), dict(data=A + 8), dict(n_blocks=0), dict(n_kv_heads=0), dict(head_dim=96)):
+        assert call(p=bad) == E, bad
+    for bad in (dict(cu_rows=None), dict(lengths=A + 1), dict(table=None), dict(n_seqs=-1), dict(table_width=0), dict(table_width=(1 << 20) + 1)):
+        assert call(r=bad) == E, bad
+    assert call(M=0, q=None) == call(r=dict(n_seqs=0)) == _lib.SD_OK
