@@ -272,11 +272,14 @@ __device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&
 // longer small against 1 (2^-4 there; past 2^32 it alone takes a weight out of fp32's range, past 2^29 out of fp16's): the
 // product is rounded first, as m's was, and the largest key's weight is 1 again.
 constexpr float FAR = 1048576.f;
-// what a step's largest logarithm may be before the maximum moves: 8, and with a far m in the wave nothing
-constexpr int NEAR_LIMIT = 0x41000000, FAR_LIMIT = -1;
+// What a step's largest logarithm may be before the maximum moves: 8 more than the maximum's own, UP, and with a far m in the
+// wave nothing.  (As the bits of a float: 8, 15.)
+constexpr int FAR_LIMIT = -1;
+template <int UP> constexpr int NEAR_LIMIT = UP ? 0x41700000 : 0x41000000;
 // Scores z of keys key .. key + 3 and key + 16 .. key + 19 -> the logarithms x of their weights, with the running maxima
 // m, and what goes with these: the weights' sums l and the outputs o.  edge: vector t sees the keys below vis[t] only.
-template <int QT, int DT, typename L>
+// UP: m is so much below the maximum, 0 or 7.
+template <int UP, int QT, int DT, typename L>
 __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float c, int key, const int (&vis)[QT], float (&m)[QT],
                                       int& limit, L (&l)[QT], f32x4 (&o)[QT][DT], float (&x)[QT][8]) {
   auto over = [&](int t, bool far) {             // in powers of two over the maximum
@@ -304,7 +307,7 @@ __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float 
       float most = -FLT_MAX;
 #pragma unroll
       for (int e = 0; e < 8; ++e) most = fmaxf(most, x[t][e] == -INFINITY ? -FLT_MAX : z[t][e / 4][e % 4] * c);
-      const float to = fmaxf(m[t], quad_max(most)), old = __builtin_amdgcn_exp2f(m[t] - to);
+      const float to = fmaxf(m[t], quad_max(most) - UP), old = __builtin_amdgcn_exp2f(m[t] - to);
       m[t] = to;
       l[t] *= old;
 #pragma unroll
@@ -313,7 +316,7 @@ __device__ __forceinline__ void weigh(bool edge, const f32x4 (&z)[QT][2], float 
       over(t, far);
       any_far |= far && to > -FLT_MAX;           // (the maximum of nothing yet)
     }
-    limit = __any(any_far) ? FAR_LIMIT : NEAR_LIMIT;
+    limit = __any(any_far) ? FAR_LIMIT : NEAR_LIMIT<UP>;
   }
 }
 __device__ __forceinline__ void exp8(float (&x)[8]) {
@@ -534,7 +537,7 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
 
     u32x4 w8[QT][PP];
     float x[QT][8];
-    weigh(EDGE, z, c, key0 + 4 * g, vis, m, limit, l, o, x);
+    weigh<0>(EDGE, z, c, key0 + 4 * g, vis, m, limit, l, o, x);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
       exp8(x[u]);
@@ -660,10 +663,12 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 // on 4095 keys of 32 heads take 157 us that way and 110 us this way.
 //
 // bf16 only.  The values are held as fp16, which their codes times scales of 2^-23 to 2^8 are exactly, so that a weight is
-// one fp16 part (off by 2^-12 of itself where the output's own rounding is 2^-8) and half the products of the second matrix
-// are saved.  A workgroup that meets a value outside that range, NaN or a missing page leaves the loop and takes the rest of
-// its keys as above.  (fp32 vectors would need three parts of either operand here too: 63 to 74 us against 49 for 3
-// sequences of 600 rows.)
+// one fp16 part and half the products of the second matrix are saved.  It is off by 2^-11 of itself, where the output's own
+// rounding is 2^-8.  Weights reach 2^15, and the largest so far is 2^7 at least: so they are that exact down to 2^-21 of the
+// largest, and what is left out is below 2^-32 of it (with 1 for the largest, thousands of keys of 2^-25 each were).
+// A workgroup that meets a value outside that range, NaN or a missing page leaves the loop and takes the rest of its keys as
+// above.  (fp32 vectors would need three parts of either operand here too: 63 to 74 us against 49 for 3 sequences of 600
+// rows.)
 //
 // Counters: of the SIMDs' cycles the products take 40 % and vector instructions 48 %, and while one is issued the other is
 // not.  Taken out of the loop one at a time (of 133 us, at an earlier step), the conversions are worth 24, the maximum test 9,
@@ -675,6 +680,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
   using P = Page4<HD>;
   using L4 = typename Load4<HD>::type;
   constexpr int QT = 2, KS = HD / 32, DT = HD / 16;
+  constexpr int UP = 7;                          // weights of up to 2^15
   __shared__ u32x4 s_k[2][2][KS][64];            // [buffer][page][k-step][lane]
   __shared__ u32x4 s_v[3][DT][64];               // [buffer][tile][lane]: four keys of either page
   __shared__ int s_leave[3];                     // step + 1 that is not for the loop over LDS
@@ -833,7 +839,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
     lds_barrier();
     read_keys(0);
     scores();
-    int vb = 0, leave = s_leave[0], limit = NEAR_LIMIT;
+    int vb = 0, leave = s_leave[0], limit = NEAR_LIMIT<UP>;
     lds_barrier();
     auto next = [&]<int S>() {                   // step i, S = i % 2
       if (i >= full || __builtin_amdgcn_readfirstlane(leave) == i + 1) return false;
@@ -841,7 +847,7 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
       read_keys(1 - S);
       leave = s_leave[after];
       float x[QT][8];
-      weigh(false, z, c, 0, vis, m, limit, l, o, x);
+      weigh<UP>(false, z, c, 0, vis, m, limit, l, o, x);
       u32x4 vf[DT];
 #pragma unroll
       for (int d = 0; d < DT; ++d) vf[d] = s_v[vb][d][lane];
@@ -872,7 +878,13 @@ template <int HD> __global__ __launch_bounds__(256, 2) void attention4_tile_kern
   // the others (behind the first keys that some vector does not see, 128 at most per head of a row): each wave by itself
   float sums[QT];
 #pragma unroll
-  for (int t = 0; t < QT; ++t) sums[t] = g == 0 ? l[t][0] : 0.f;
+  for (int t = 0; t < QT; ++t) {
+    const float to = m[t] + UP, by = __builtin_amdgcn_exp2f(m[t] - to);       // (of m as it is rounded)
+    m[t] = to;
+    sums[t] = g == 0 ? l[t][0] * by : 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] *= by;
+  }
   take_keys<T, HD, QT, false, false>(p, kvh, w.b, 32 * i, 32, mine_max, mine_min, mine_max, q, c, vis, m, sums, o, false, 0);
 
 #pragma unroll

@@ -168,3 +168,38 @@ def test_appended_values_at_the_end_of_the_range(hd, dtype):
         close(out[ok], want[ok], err[:, ok], dtype)
         if is_nan:
             assert np.isnan(out[18:, :2]).all() and np.isnan(out[19, 2:, 32:64]).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kernel", ["shared", "waves of 8"])
+@pytest.mark.parametrize("power", [13, 22.6, 24.4, 26.7])
+def test_many_small_weights(kernel, hd, power):
+    """One key outweighs each of the others by 2^power, and its value is zero: the outputs are what the others' weights add up
+    to.
+
+    A weight of the kernel that shares its keys is one fp16 number, 2^7 of the largest: off by 2^-11 of it, or by 2^-32 of
+    the largest where it is below fp16's normal numbers (half of 2^-24, of 2^7); relative errors of the weights are the
+    outputs' twice over, with the sum that they are divided by.  Elsewhere it is two bf16 parts, off by 2^-15.  The scores are
+    of one product; with their scale and the exponential's argument they are off by a few roundings of 27, 2^-18 in all."""
+    from paper_2510_11331_amd import attention_q
+    say("small weights", kernel, hd, power)
+    r = np.random.default_rng([hd, int(10 * power)])
+    rows, lengths, H, KV, shared = ([520, 520], [3900, 2970], 32, 16, 1) if kernel == "shared" else ([2, 2], [3900, 2970], 32, 16, 0)
+    c = Case(r, rows, lengths, KV, hd)
+    assert kvplans.plan(sum(rows), H, KV, hd, "bf16", 2, 16 * c.table.shape[1])[0] == shared
+    for b, m in enumerate(lengths):
+        k, v = np.zeros((m, KV, hd)), r.choice([0.5, 1, 1.5, 2, 3, 4, 6], size=(m, KV, hd)) * r.choice([1, -1], size=(1, KV, hd))
+        k[0, :, 5], v[0] = 6, 0
+        put(c, b, k, v)
+    q = np.zeros((c.M, H, hd))
+    q[:, :, 5] = 1
+    got = host(attention_q(t(q.astype(np.float32), "bf16"), c.cache(), c.desc, scale=power * np.log(2) / 6))
+    for b, (n, m) in enumerate(zip(rows, lengths)):
+        v = c.pool.get(*c.at(b, np.arange(m)))[1]
+        sums, count = np.cumsum(v, 0), np.arange(m)[:, None, None]
+        want = (sums / (2.0 ** power + count))[m - n:].repeat(H // KV, 1)
+        here = got[c.cu[b]:c.cu[b] + n]
+        slack = np.abs(want) * (2 * (2.0 ** -11 if shared else 2.0 ** -15) + 2.0 ** -18 + (m / 2 + 128) * 2.0 ** -23 + HALF["bf16"])
+        slack += shared * 2.0 ** -32 * m * 6
+        bad = ~(np.abs(here - want) <= slack * 1.001)
+        assert not bad.any(), (bad.sum(), np.argwhere(bad)[:4].tolist(), here[bad][:4], want[bad][:4], slack[bad][:4])
