@@ -973,7 +973,7 @@ Attn4Plan plan_attention4(int dtype, int hd, int M, int H, int KV, int n_seqs, i
     return (M * (G / u) + (C - 1) * nz) / C;
   };
   auto typical = [&](int64_t cap) { return nz * ((vectors + cap - 1) / cap) * KV; };    // ... of alike sequences, and heads
-  const int64_t steps = (max_len + 31) / 32;
+  const int64_t steps = ((int64_t)max_len + 31) / 32;
 
   // Keys shared in LDS pay where a workgroup's 128 vectors are there and every CU has one: 2048 rows of 32 heads on 32,
   // 4095 keys, 111 shared and 157 not; 512 rows of 4 vectors each, 8192 keys, 99 and 100; 128 rows, 30 and 16; with 128 such

@@ -166,3 +166,22 @@ def test_attention_refusals_with_outputs_apart():
     for bad in (dict(cu_rows=None), dict(lengths=A + 1), dict(table=None), dict(n_seqs=-1), dict(table_width=0), dict(table_width=(1 << 20) + 1)):
         assert call(r=bad) == E, bad
     assert call(M=0, q=None) == call(r=dict(n_seqs=0)) == _lib.SD_OK
+
+
+@needs_lib
+def test_longest_max_len():
+    """A max_len that no table reaches is as good as one that a table does: the same plan, and a workspace that is enough."""
+    import ctypes as C
+    from paper_2510_11331_amd import _lib
+    L = _lib.lib()
+    for hd in (64, 128):
+        for B in (1, 2, 4, 8, 16, 36, 64):
+            for n in (1, 5, 17):
+                for H, KV in ((1, 1), (8, 1), (20, 5), (32, 8), (40, 5)):
+                    plans = []
+                    for x in (1 << 24, 2 ** 31 - 31, 2 ** 31 - 1):
+                        assert L.sd_attention_q_workspace_bytes(B * n, H, KV, hd, B, x) == L.sd_attention_q_workspace_bytes(B * n, H, KV, hd, B, 1 << 24)
+                        p = _lib.AttentionQPlan()
+                        assert L.sd_plan_attention_q(B * n, H, KV, hd, B, x, 0, C.byref(p)) == _lib.SD_OK
+                        plans.append((p.shared, p.vectors, p.waves, p.key_ranges, p.streamed))
+                    assert plans[1] == plans[0] and plans[2] == plans[0]
