@@ -377,26 +377,25 @@ __device__ __forceinline__ void add_values(const typename Load4<HD>::type (&c)[2
   }(std::make_integer_sequence<int, HD / 32>{});
 }
 
-// Values that not every vector sees must be finite: their weights are zero where they are not seen, and a NaN that a
-// vector does see is put into its output by put_nan.  key: the lane's first; no: pages that are none.  Whether there was
-// such a NaN; large: whether there is a scale whose largest codes are infinities.
-__device__ __forceinline__ bool clean_scales(uint32_t (&E)[2], int key, int n_max, uint32_t no, bool& large) {
-  bool nan = false;
+// Values that not every vector sees must be finite: their weights are zero where they are not seen.  Scales of keys behind
+// the last (key: the lane's first) and of pages that are none (no) become 1; whether there is one of 253 or more among the
+// others, whose codes may be infinities or NaN.
+__device__ __forceinline__ bool clean_scales(uint32_t (&E)[2], int key, int n_max, uint32_t no) {
+  uint32_t large = 0;
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int t = 0; t < 2; ++t) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t E8 = E[t] >> (8 * e) & 255u;
-      const bool is_nan = E8 == 255u, none = key + 16 * t + e >= n_max || (no >> t & 1);
-      nan |= is_nan && !none;
-      if (is_nan || none) E[t] = (E[t] & ~(255u << (8 * e))) | 127u << (8 * e);
-      else large |= E8 >= 253u;
-    }
-  return nan;
+    for (int e = 0; e < 4; ++e)
+      if (key + 16 * t + e >= n_max || (no >> t & 1)) E[t] = (E[t] & ~(255u << (8 * e))) | 127u << (8 * e);
+    large |= ((E[t] & 0x7f7f7f7fu) + 0x03030303u) & E[t] & 0x80808080u;      // (four bytes at once)
+  }
+  return large != 0;
 }
-// Codes whose numbers are infinities (4 and 6 with E = 253, 2 to 6 with E = 254; nothing writes them) as the largest number
-// that is none: 3 or 1.5, both the odd code below the first.
-template <int HD> __device__ __forceinline__ void clean_codes(typename Load4<HD>::type (&c)[2], const uint32_t (&E)[2]) {
+// Of these, NaN (255) becomes a number; put_nan puts it into the outputs of the vectors that see it.  Codes whose numbers are
+// infinities (4 and 6 with E = 253, 2 to 6 with E = 254; nothing writes them) become the largest number that is none: 3 or
+// 1.5, both the odd code below the first.  Whether there was a NaN.
+template <int HD> __device__ __forceinline__ bool clean_codes(typename Load4<HD>::type (&c)[2], uint32_t (&E)[2]) {
+  bool nan = false;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -406,7 +405,10 @@ template <int HD> __device__ __forceinline__ void clean_codes(typename Load4<HD>
       const uint32_t mine = HD == 128 ? 0x11111111u : 0x1111u << (16 * (e % 2));
       const uint32_t inf = (E8 == 253u ? w >> 2 & w >> 1 : E8 == 254u ? w >> 2 : 0u) & mine;
       c[t][HD == 128 ? e : e / 2] = (w & ~(7u * inf)) | inf * (E8 == 253u ? 5u : 3u);
+      if (E8 == 255u) E[t] ^= 128u << (8 * e);
+      nan |= E8 == 255u;
     }
+  return nan;
 }
 // the value blocks of NaN among the step's keys; all of a lane's outputs are of scale block (hd / 4) g / 32
 template <int HD, int QT>
@@ -545,12 +547,11 @@ __device__ __forceinline__ void take_keys(const Attn4Params& p, int kvh, int b, 
       parts8<PP>(x[u], w8[u]);
     }
 
-    bool large = false;
-    const bool nan = EDGE && clean_scales(vE, key0 + 4 * g, n_max, no_here, large);
-    if (EDGE && __any(large)) clean_codes<HD>(vc, vE);
+    bool nan = false;
+    if (EDGE && __any(clean_scales(vE, key0 + 4 * g, n_max, no_here))) nan = __any(clean_codes<HD>(vc, vE));
     add_values<HD>(vc, vE, w8, o);
     load_v();
-    if (EDGE && __any(nan)) put_nan<HD>(here, no_here, key0, n_max, g, vis, o);
+    if (nan) put_nan<HD>(here, no_here, key0, n_max, g, vis, o);
   };
 
   if (left > 0) {
