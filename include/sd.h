@@ -492,8 +492,8 @@ int sd_kv_read_q(const sd_kv_q_pool *pool, const sd_kv_rows *rows, int M, int dt
  * does not see do not reach it; a NaN that it sees is in its output as
  * the formula has it (a key's in all of a head, a value block's in its 32
  * dimensions).  Scores, their products with |scale| log2(e), sums and the softmax
- * are in fp32: any of these within its range gives finite outputs of finite
- * values.  out may not overlap q (SD_EINVAL).  A length may be anything up to 16 table_width:
+ * are in fp32: scores and products within its range, and values below 2^96, give
+ * finite outputs.  out may not overlap q (SD_EINVAL).  A length may be anything up to 16 table_width:
  * max_len (0: 16 table_width) only says for which lengths the work is split.  The
  * workspace's bytes are those for the call's max_len or a larger one (16
  * table_width where the call passes 0); dtypes need the same.  It (16-byte

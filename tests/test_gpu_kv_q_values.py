@@ -99,6 +99,27 @@ def test_large_scores_of_any_query(kernel, size):
 
 
 @kernels
+def test_large_values(kernel):
+    """Values of up to 2^96: outputs between the smallest and the largest of those seen, as above."""
+    from paper_2510_11331_amd import attention_q
+    say("large values", kernel[0])
+    r = np.random.default_rng(len(kernel[0]))
+    c, H, dtype = case_of(r, kernel)
+    q = t(r.normal(size=(c.M, H, c.hd)).astype(np.float32), dtype)
+    lo, hi = np.zeros(q.shape), np.zeros(q.shape)
+    for b, (n, m) in enumerate(zip(c.rows, c.lengths)):
+        x = r.normal(size=(2, m, c.KV, c.hd))
+        put(c, b, 4 * x[0], np.clip(x[1] / 2, -1, 1) * 2.0 ** 95.9)
+        v = c.pool.get(*c.at(b, np.arange(m)))[1]
+        s, pos = slice(c.cu[b], c.cu[b] + n), c.pos[c.cu[b]:c.cu[b] + n]
+        lo[s], hi[s] = (np.repeat(f.accumulate(v)[pos], H // c.KV, 1) for f in (np.minimum, np.maximum))
+    got = host(attention_q(q, c.cache(), c.desc))
+    slack = np.maximum(np.abs(lo), np.abs(hi)) * (2.0 ** -10 + HALF[dtype])
+    bad = ~((got >= lo - slack) & (got <= hi + slack))
+    assert not bad.any(), (bad.sum(), np.isnan(got).sum(), np.argwhere(bad)[:4].tolist(), got[bad][:4], lo[bad][:4], hi[bad][:4])
+
+
+@kernels
 @pytest.mark.parametrize("E", [252, 253, 254])
 def test_values_at_the_end_of_the_range(kernel, E):
     """Tokens of the pass's own rows with 6 2^(E - 127) and its negative among 32 zeros: from E = 253 on these are infinities
