@@ -12,8 +12,9 @@
 // v_cvt_scalef32_pk_bf16_fp4 loses nothing, and neither do the products with
 // bf16 queries.  fp32 queries enter as three bf16 parts (all 24 bits).  Weights
 // enter as two for bf16 outputs, off by at most 2^-15 of themselves where the
-// output's own rounding is 2^-8, and as three (exact) for fp32 ones.  Scores, the
-// running maximum, the weights' sum and the output are fp32.
+// output's own rounding is 2^-8, and as three (exact) for fp32 ones (the prefill
+// kernel's: below).  Scores, the running maximum, the weights' sum and the output
+// are fp32.
 //
 // Why matrix instructions for one row of keys: 16 query vectors cost as much as
 // one, and there the conversion of the codes, which everything needs, is the
@@ -36,18 +37,18 @@
 // a rescaling of the output.
 //
 // Measured (a call in a replayed graph; the plain read rate of this memory is 6.8
-// TB/s, a large bf16 product runs at 1.17 PFLOP/s):
+// TB/s, a large bf16 product runs at 1.57 PFLOP/s):
 //   64 sequences of 8192 keys, a row of 32 heads on 8, hd 128, bf16: 95 us, 6.0 TB/s
-//   8 sequences of 1044 keys, 5 rows of 32 heads on 32, bf16: 11.2 us, 3.3 TB/s
-//   32 ragged ones up to 2176 keys, 5 rows of 32 heads on 32, fp32: 29.2 us
-//   1 of 32763 keys, 5 rows of 32 heads on 8, bf16: 21.4 us (16.4 and the join 5)
-//   1 of 520 keys, a row of 32 heads on 8, hd 64: 6.2 us
-//   2048 rows on 4095 keys, 32 heads on 32, bf16: 110 us, 0.94 PFLOP/s
+//   8 sequences of 1044 keys, 5 rows of 32 heads on 32, bf16: 11.4 us, 3.3 TB/s
+//   32 ragged ones up to 2176 keys, 5 rows of 32 heads on 32, fp32: 29.1 us
+//   1 of 32763 keys, 5 rows of 32 heads on 8, bf16: 21.9 us (16.5 and the join 5)
+//   1 of 520 keys, a row of 32 heads on 8, hd 64: 6.3 us
+//   2048 rows on 4095 keys, 32 heads on 32, bf16: 111 us, 0.93 PFLOP/s
 // Short calls are bound by the chain of latencies (the sequence, its page ids,
-// the pages, the waves' join): 5 us whatever their size.  fp32 ones by the matrix
-// unit: three parts of queries and of weights.  Decoding at length by memory.
-// Prefill by the issue of instructions, which matrix and vector instructions of a
-// SIMD share.
+// the pages, the waves' join): 5 us whatever their size.  fp32 ones of few rows by
+// the instructions of three parts of queries and of weights (vector units 0.57,
+// matrix units 0.24 of the cycles).  Decoding at length by memory.  Prefill by no
+// unit alone (below).
 #include "codes4.h"
 
 #include <float.h>
@@ -661,7 +662,7 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 
 // Prefill: 128 vectors a workgroup, 32 a wave, and the keys in LDS: each wave converts a quarter of a step's 32 keys for all
 // four, while they take the step before it.  Without sharing, a wave's conversions cost as much as its products: 2048 rows
-// on 4095 keys of 32 heads take 157 us that way and 110 us this way.
+// on 4095 keys of 32 heads take 157 us that way and 111 us this way.
 //
 // bf16 only.  The values are held as fp16, which their codes times scales of 2^-23 to 2^8 are exactly, so that a weight is
 // one fp16 part and half the products of the second matrix are saved.  It is off by 2^-11 of itself, where the output's own
@@ -671,8 +672,8 @@ __global__ __launch_bounds__(64 * WAVES, (MIN_WAVES<T, QT>)) void attention4_str
 // above.  (fp32 vectors would need three parts of either operand here too: 63 to 74 us against 49 for 3 sequences of 600
 // rows.)
 //
-// Counters: of the SIMDs' cycles the products take 40 % and vector instructions 48 %, and while one is issued the other is
-// not.  Taken out of the loop one at a time (of 133 us, at an earlier step), the conversions are worth 24, the maximum test 9,
+// Counters: of the SIMDs' cycles the products take 42 % and vector instructions 51 %; the waves, two to a SIMD, wait to issue
+// for 32 % of theirs and for loads, LDS and barriers for 22 %.  Taken out of the loop one at a time (of 133 us, at an earlier step), the conversions are worth 24, the maximum test 9,
 // the exponentials 8, the barrier 8.  The rare paths lie outside the loop because their code there kept the accumulators from
 // staying in place.  Tried and worse: waves' priorities raised around the products (146), eight waves of 16 vectors, two
 // waves of 64 (registers spill).
