@@ -269,10 +269,12 @@ __device__ __forceinline__ void load_query(const T* src, bool negative, u32x4 (&
   }
 }
 
-// A weight's logarithm is z c - m of one rounding, m the rounded z c of a maximum.  From |m| = FAR on that rounding is no
-// longer small against 1 (2^-4 there; past 2^32 it alone takes a weight out of fp32's range, past 2^29 out of fp16's): the
-// product is rounded first, as m's was, and the largest key's weight is 1 again.
-constexpr float FAR = 1048576.f;
+// A weight's logarithm is z c - m of one rounding, m the rounded z c of a maximum (less UP).  m's own rounding is the same for
+// all weights; up to |m| = FAR it is at most 4, small against their range.  Past 2^32 it would take the largest weight out of
+// fp32's, past 2^29 out of fp16's: from FAR on the product is rounded as m's was, and the largest key's weight is 1 again.
+// (There neighbouring floats z lie 8 apart in z c, so that this is the scores' own rounding; from 2^20 on, tried first, it
+// took bits from scores that are close.)
+constexpr float FAR = 134217728.f;
 // What a step's largest logarithm may be before the maximum moves: 8 more than the maximum's own, UP, and with a far m in the
 // wave nothing.  (As the bits of a float: 8, 15.)
 constexpr int FAR_LIMIT = -1;

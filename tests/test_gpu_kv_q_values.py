@@ -34,7 +34,7 @@ def put(c, b, k, v):
 
 
 @kernels
-@pytest.mark.parametrize("power", [17, 21, 29, 30, 33, 40, 100])
+@pytest.mark.parametrize("power", [17, 21, 24, 25, 26, 29, 33, 40, 100])
 @pytest.mark.parametrize("scale", [1.0, -0.37])
 def test_large_scores(kernel, power, scale):
     """Scores from 2^17 on that are exact in fp32 and lie far apart or are equal: the output is the mean of the values whose
@@ -68,6 +68,42 @@ def test_large_scores(kernel, power, scale):
             a = top @ np.abs(v[:, h // G]) / count
             form = 0.0 if dtype == "fp32" else 2.0 ** -14 if kernel[8][0] == 0 else 1.001 * 2.0 ** -10
             far[s, h] = a * form + a * (count + 4) * 2.0 ** -23
+    got = host(attention_q(t(q.astype(np.float32), dtype), c.cache(), c.desc, scale=scale))
+    bad = ~(np.abs(got - want) <= far + np.abs(want) * HALF[dtype] * 1.001)
+    assert not bad.any(), (bad.sum(), np.isnan(got).sum(), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+@kernels
+@pytest.mark.parametrize("power", [10, 16, 18, 20, 21, 22])
+@pytest.mark.parametrize("scale", [1.0, -0.7])
+def test_close_scores(kernel, power, scale):
+    """Scores that lie by 0 to 12 apart at 2^power, all of them exact in fp32: the weights are those of the differences.
+
+    What the logarithm of a weight is off by does not depend on the scores' size: a rounding of itself, and the two of its
+    factor scale log2(e), 2^-22 of 12 1.5 or less; the exponential and a move of the maximum are off by a few steps more, so
+    that 2^-17 holds them all twice over.  The forms of a weight are those of the test above."""
+    from paper_2510_11331_amd import attention_q
+    say("close scores", kernel[0], power, scale)
+    r = np.random.default_rng([power, len(kernel[0])])
+    c, H, dtype = case_of(r, kernel)
+    KV, hd, G = c.KV, c.hd, H // c.KV
+    numbers = np.array([-6, -4, -3, -2, -1.5, -1, -0.5, 0, 0.5, 1, 1.5, 2, 3, 4, 6])
+    q = np.zeros((c.M, H, hd))
+    q[:, :, 5], q[:, :, 40] = r.choice([-1, 1], size=(c.M, H)) * 2.0 ** power, r.choice([-1, 1], size=(c.M, H))
+    want, far = np.zeros(q.shape), np.zeros(q.shape)
+    for b, (n, m) in enumerate(zip(c.rows, c.lengths)):
+        k, v = np.zeros((m, KV, hd)), r.choice(numbers, size=(m, KV, hd))
+        k[:, :, 5], k[:, :, 40] = 1, r.choice(numbers, size=(m, KV))
+        put(c, b, k, v)
+        s = slice(c.cu[b], c.cu[b] + n)
+        seen = np.arange(m)[None] <= c.pos[s][:, None]
+        for h in range(H):
+            d = q[s, h, 40][:, None] * k[:, h // G, 40][None] * scale
+            w = np.where(seen, np.exp(d - np.where(seen, d, -np.inf).max(1, keepdims=True)), 0.0)
+            w /= w.sum(1, keepdims=True)
+            want[s, h] = w @ v[:, h // G]
+            form = 0.0 if dtype == "fp32" else 2.0 ** -14 if kernel[8][0] == 0 else 1.001 * 2.0 ** -10
+            far[s, h] = (w @ np.abs(v[:, h // G])) * (form + 2.0 ** -16 + (seen.sum(1, keepdims=True) / 2 + 128) * 2.0 ** -22)
     got = host(attention_q(t(q.astype(np.float32), dtype), c.cache(), c.desc, scale=scale))
     bad = ~(np.abs(got - want) <= far + np.abs(want) * HALF[dtype] * 1.001)
     assert not bad.any(), (bad.sum(), np.isnan(got).sum(), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
